@@ -656,6 +656,62 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
                        const void* dCTX, void* dQKV, void* workspace, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Language models on packed sequences (fusion rules table rows "Embedding" and "MultiheadAttention"; appendix "Fused Loss").
+ * Each model's R rows hold nseq sequences of any lengths back to back: sequence s is rows [seq_offsets[b][s],
+ * seq_offsets[b][s + 1]) of model b, seq_offsets: device int32 [B][nseq + 1], non-decreasing, in [0, R].  Sequences may be
+ * empty, and every model has its own.  Rows in front of the first and behind the last sequence belong to none: nothing of them is
+ * read, and what the calls return per row is left as it was there (clear it once where a later call reads it).  Offsets are
+ * taken into [0, R]; if they are not in order the results are not defined, but nothing outside the tensors is touched.
+ * Results are the same bit for bit on every run.
+ *
+ * attention_packed: softmax(scale q k^T) v within each sequence (causal != 0: row i sees rows up to itself), without a
+ *   score-sized tensor.  Grouped heads: query head h reads key head h / (Hq / Hkv); Hq a multiple of Hkv (EINVAL), heads of d
+ *   columns, d <= 128 (EUNSUPPORTED).  Q, CTX, dCTX, dQ hold Hq heads, K, V, dK, dV Hkv; storage dtype; element (b, r, h, c) at
+ *   s[0] b + s[1] r + s[2] h + c with element strides s[3] (host): qs for Q, kvs for K and V, cs for CTX and dCTX, dqs for dQ,
+ *   dkvs for dK and dV.  Packed projections [R][q | k | v] are three pointers with one set of strides.  Rows in 16-byte pieces (d
+ *   and strides multiples of 8 bf16 / 4 fp32, pointers 16-byte aligned) take wide loads; any others are taken element by element.
+ *   scale > 0 and finite (EINVAL).  LSE [B][Hq][R] fp32: log of the sum of exponentials of each row, which the backward call reads.
+ *   bwd: all three gradients, from the forward call's CTX and LSE; dK and dV sum over the heads of a group.  Workspace
+ *   hfta_attention_packed_bwd_workspace_bytes, 4-byte aligned (EWORKSPACE).  Outputs may not overlap inputs.
+ *   A value that is not finite reaches the rows that see it (an infinity as an infinity or a NaN) and no others.
+ * embedding_packed_fwd: out[b,r,:] = scale * table[b, idx[b,r], :] + pos[min(r - start of r's sequence, S - 1), :] (pos fp32 [S][E] or
+ *   NULL); storage dtype; indices clamped to [0, V).
+ * embedding_bwd_sorted: dtable[b,v,:] (fp32, fully written) = scale * sum over r with idx[b,r] == v of dY[b,r,:], any number of rows:
+ *   they are sorted by token first.  seq_offsets NULL: all rows; otherwise those of a sequence.  Sums of up to 32 rows are
+ *   taken in order of r, longer ones in fixed stretches.  Workspace hfta_embedding_bwd_sorted_workspace_bytes, 16-byte aligned (EWORKSPACE).
+ * seq_logps: token_logps[b,r] = log softmax(logits[b,r])[labels[b,r]] (fp32 [B][R]; 0 for a negative label, whose row of logits is
+ *   not read) and logps[b,s] (fp32 [B][nseq]), their sums over each sequence, formed in 64 bits.  A label >= K gives NaN.
+ * preference_loss: pairs of sequences (2p: preferred, 2p + 1: not), npairs per model, seq_offsets [B][2 npairs + 1].  With L_s as logps
+ *   above, returned in logps [B][2 npairs], ref_logps [B][2 npairs] the same of a reference model, and t_p = beta[b] ((L_2p -
+ *   ref_2p) - (L_2p+1 - ref_2p+1)):   loss[b] = mean over p of -(1 - eps) log sigma(t_p) - eps log sigma(-t_p),  eps =
+ *   label_smoothing[b];   beta, label_smoothing: fp32 [B] (label_smoothing NULL: 0).  dlogits: the gradient, storage dtype, 0 in rows with a negative
+ *   label; it may be logits itself.  A label >= K makes its model's loss and its pair's gradient NaN.  Workspace
+ *   hfta_preference_loss_workspace_bytes, 4-byte aligned (EWORKSPACE).
+ * EUNSUPPORTED above 65535 models (attention: above 2^31 - 1 workgroups).
+ * ---------------------------------------------------------------------- */
+int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
+                              const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, float scale,
+                              int causal, void* CTX, const int64_t cs[3], float* LSE, void* stream);
+size_t hfta_attention_packed_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype);
+int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
+                              const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, float scale,
+                              int causal, const void* CTX, const void* dCTX, const int64_t cs[3], const float* LSE,
+                              void* dQ, const int64_t dqs[3], void* dK, void* dV, const int64_t dkvs[3],
+                              void* workspace, size_t ws_bytes, void* stream);
+int hfta_embedding_packed_fwd(int B, int R, int V, int E, int nseq, int dtype, const void* table, const int32_t* idx,
+                              const int32_t* seq_offsets, float scale, const float* pos, int S, void* out, void* stream);
+size_t hfta_embedding_bwd_sorted_workspace_bytes(int B, int R, int V, int E);
+int hfta_embedding_bwd_sorted(int B, int R, int V, int E, int nseq, int dtype, const void* dY, const int32_t* idx,
+                              const int32_t* seq_offsets, float scale, float* dtable, void* workspace, size_t ws_bytes,
+                              void* stream);
+int hfta_seq_logps(int B, int R, int K, int nseq, int dtype, const void* logits, const int32_t* labels, const int32_t* seq_offsets,
+                   float* token_logps, float* logps, void* stream);
+size_t hfta_preference_loss_workspace_bytes(int B, int R, int npairs);
+int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void* logits, const int32_t* labels,
+                         const int32_t* seq_offsets, const float* ref_logps, const float* beta, const float* label_smoothing,
+                         float* loss, float* logps, void* dlogits, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Fused Adadelta over the same parameter-major arena, and the fused step learning-rate schedule
  * (section "Our Proposal: HFTA", paragraph on optimizers and learning-rate schedulers: each
  * hyper-parameter becomes a vector with one entry per model).  Arguments as hfta_adam_step_multi;

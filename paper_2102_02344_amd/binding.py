@@ -105,6 +105,15 @@ _SIGS = {
     "hfta_attention_fwd": (_i, [_i] * 6 + [_p, _p, _p, _i, _p]),
     "hfta_attention_bwd_workspace_bytes": (_sz, [_i] * 6),
     "hfta_attention_bwd": (_i, [_i] * 6 + [_p, _p, _p, _p, _p, _sz, _p]),
+    "hfta_attention_packed_fwd": (_i, [_i] * 7 + [_p, _s4, _p, _p, _s4, _p, _f, _i, _p, _s4, _p, _p]),
+    "hfta_attention_packed_bwd_workspace_bytes": (_sz, [_i] * 7),
+    "hfta_attention_packed_bwd": (_i, [_i] * 7 + [_p, _s4, _p, _p, _s4, _p, _f, _i, _p, _p, _s4, _p, _p, _s4, _p, _p, _s4, _p, _sz, _p]),
+    "hfta_embedding_packed_fwd": (_i, [_i] * 6 + [_p, _p, _p, _f, _p, _i, _p, _p]),
+    "hfta_embedding_bwd_sorted_workspace_bytes": (_sz, [_i] * 4),
+    "hfta_embedding_bwd_sorted": (_i, [_i] * 6 + [_p, _p, _p, _f, _p, _p, _sz, _p]),
+    "hfta_seq_logps": (_i, [_i] * 5 + [_p] * 6),
+    "hfta_preference_loss_workspace_bytes": (_sz, [_i] * 3),
+    "hfta_preference_loss": (_i, [_i] * 5 + [_p] * 10 + [_sz, _p]),
     "hfta_adadelta_step_multi": (_i, [_i, _i, _s4, _i] + [_p] * 9 + [_p]),
     "hfta_steplr": (_i, [_i, _p, _p, _p, _i, _p, _p]),
     "hfta_add_sample_bias": (_i, [_i] * 5 + [_p] * 7),
@@ -735,3 +744,54 @@ def point_transform_bwd(B, Nb, Ci, Co, L, dtype, X, xs, T, dY, dys, dX, dxs, dT,
     _check(_lib.hfta_point_transform_bwd(B, Nb, Ci, Co, L, dtype, _ptr(X), None if xs is None else _strides(xs), _ptr(T),
                                          _ptr(dY), _strides(dys), _ptr(dX), None if dxs is None else _strides(dxs),
                                          _ptr(dT), _stream(stream)), "hfta_point_transform_bwd")
+
+
+def attention_packed_fwd(B, R, nseq, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, seq_offsets, scale, causal, CTX, cs, LSE, stream=None):
+    _check(_lib.hfta_attention_packed_fwd(B, R, nseq, Hq, Hkv, d, dtype, _ptr(Q), _strides(qs, 3), _ptr(K), _ptr(V), _strides(kvs, 3),
+                                          _ptr(seq_offsets), scale, causal, _ptr(CTX), _strides(cs, 3), _ptr(LSE), _stream(stream)),
+           "hfta_attention_packed_fwd")
+
+
+def attention_packed_bwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype) -> int:
+    return _lib.hfta_attention_packed_bwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype)
+
+
+def attention_packed_bwd(B, R, nseq, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, seq_offsets, scale, causal, CTX, dCTX, cs, LSE, dQ, dqs, dK,
+                         dV, dkvs, workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_attention_packed_bwd(B, R, nseq, Hq, Hkv, d, dtype, _ptr(Q), _strides(qs, 3), _ptr(K), _ptr(V), _strides(kvs, 3),
+                                          _ptr(seq_offsets), scale, causal, _ptr(CTX), _ptr(dCTX), _strides(cs, 3), _ptr(LSE),
+                                          _ptr(dQ), _strides(dqs, 3), _ptr(dK), _ptr(dV), _strides(dkvs, 3), wp, wb, _stream(stream)),
+           "hfta_attention_packed_bwd")
+
+
+def embedding_packed_fwd(B, R, V, E, nseq, dtype, table, idx, seq_offsets, scale, pos, S, out, stream=None):
+    _check(_lib.hfta_embedding_packed_fwd(B, R, V, E, nseq, dtype, _ptr(table), _ptr(idx), _ptr(seq_offsets), scale, _ptr(pos), S,
+                                          _ptr(out), _stream(stream)), "hfta_embedding_packed_fwd")
+
+
+def embedding_bwd_sorted_workspace_bytes(B, R, V, E) -> int:
+    return _lib.hfta_embedding_bwd_sorted_workspace_bytes(B, R, V, E)
+
+
+def embedding_bwd_sorted(B, R, V, E, nseq, dtype, dY, idx, seq_offsets, scale, dtable, workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_embedding_bwd_sorted(B, R, V, E, nseq, dtype, _ptr(dY), _ptr(idx), _ptr(seq_offsets), scale, _ptr(dtable), wp, wb,
+                                          _stream(stream)), "hfta_embedding_bwd_sorted")
+
+
+def seq_logps(B, R, K, nseq, dtype, logits, labels, seq_offsets, token_logps, logps, stream=None):
+    _check(_lib.hfta_seq_logps(B, R, K, nseq, dtype, _ptr(logits), _ptr(labels), _ptr(seq_offsets), _ptr(token_logps), _ptr(logps),
+                               _stream(stream)), "hfta_seq_logps")
+
+
+def preference_loss_workspace_bytes(B, R, npairs) -> int:
+    return _lib.hfta_preference_loss_workspace_bytes(B, R, npairs)
+
+
+def preference_loss(B, R, K, npairs, dtype, logits, labels, seq_offsets, ref_logps, beta, label_smoothing, loss, logps, dlogits,
+                    workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_preference_loss(B, R, K, npairs, dtype, _ptr(logits), _ptr(labels), _ptr(seq_offsets), _ptr(ref_logps), _ptr(beta),
+                                     _ptr(label_smoothing), _ptr(loss), _ptr(logps), _ptr(dlogits), wp, wb, _stream(stream)),
+           "hfta_preference_loss")

@@ -1,0 +1,298 @@
+// Log-probabilities of packed sequences, and the loss of preferred pairs with the gradient of its logits (appendix
+// "Fused Loss": a model's loss is the mean over its own pairs, its hyper-parameters are entries of device arrays).
+//
+//   lp_r = z_r[y_r] - log sum_k exp z_r[k],   L_s = sum of lp_r over the rows of sequence s that have a label
+//   t_p = beta ((L_2p - ref_2p) - (L_2p+1 - ref_2p+1)),  loss = mean_p (1 - eps) softplus(-t_p) + eps softplus(t_p)
+//   dz_r[k] = c_s (1[k = y_r] - softmax(z_r)_k),  c_2p = -c_2p+1 = -beta ((1 - eps) sigma(-t_p) - eps sigma(t_p)) / pairs
+//
+// Bound by memory: the gradient's factor needs the whole sequence, so rows with a label are read twice and every row of
+// a sequence is written once; rows without one are not read.  A workgroup takes a row, with 16-byte pieces from its first
+// aligned element on.  Sums over a sequence are taken in 64 bits: the loss is a difference of long sums.
+#include "packed_rows.h"
+
+namespace hfta {
+namespace {
+
+constexpr float PF_LOG2E = 1.4426950408889634f;
+
+// A row of K values: `head` up to the first 16-byte boundary, nv whole pieces, `tail` past the last
+template <typename T> struct PfRow {
+  static constexpr int EPP = 16 / (int)sizeof(T);
+  int head, nv, tail;
+  __device__ __forceinline__ PfRow(const T* z, int K) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
+    head = off ? min(K, EPP - off) : 0;
+    nv = (K - head) / EPP;
+    tail = K - head - nv * EPP;
+  }
+};
+__device__ __forceinline__ void pf_unpack(const uint4& v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void pf_unpack(const uint4& v, float (&x)[4]) {
+  x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ uint4 pf_pack(const float (&x)[8]) {
+  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+__device__ __forceinline__ uint4 pf_pack(const float (&x)[4]) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ float pf_exp(float x, float top) { return __builtin_amdgcn_exp2f(fmaf(x, PF_LOG2E, -top * PF_LOG2E)); }
+
+// rows [lo, hi) of sequence s
+__device__ __forceinline__ void pf_rows(const int32_t* off, int s, int R, int& lo, int& hi) {
+  lo = min(max(off[s], 0), R);
+  hi = min(max(off[s + 1], 0), R);
+}
+
+// ------------------------------------------------------------------ rows: log-sum-exp and the label's log-probability
+template <typename T>
+__global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logits, const int32_t* __restrict__ labels,
+                                                      const int32_t* __restrict__ off, int nseq, float* __restrict__ lse,
+                                                      float* __restrict__ lp, int R, int K) {
+  constexpr int EPP = PfRow<T>::EPP, NV = 4;
+  __shared__ float sm[4], ss[4];
+  const int r = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
+  const int64_t row = (int64_t)b * R + r;
+  off += (int64_t)b * (nseq + 1);
+  if (r < off[0] || r >= off[nseq]) return;
+  const int y = labels[row];
+  if (y < 0) {
+    if (t == 0) lp[row] = 0.f;
+    return;
+  }
+  const T* z = logits + row * K;
+  const PfRow<T> g(z, K);
+  const uint4* zv = reinterpret_cast<const uint4*>(z + g.head);
+  float m = -INFINITY, s = 0.f;
+  auto take = [&](float mt, auto&& each) {          // joins values with maximum mt
+    const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.f : mn;
+    s *= pf_exp(m, mu);
+    m = mn;
+    each(mu);
+  };
+  for (int v0 = t; v0 < g.nv; v0 += 256 * NV) {
+    float x[NV][EPP];
+    float mt = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (v0 + 256 * j < g.nv) pf_unpack(zv[v0 + 256 * j], x[j]);
+      else
+#pragma unroll
+        for (int e = 0; e < EPP; ++e) x[j][e] = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < EPP; ++e) mt = fmaxf(mt, x[j][e]);
+    take(mt, [&](float mu) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < EPP; ++e) s += pf_exp(x[j][e], mu);
+    });
+  }
+  if (t < g.head + g.tail) {
+    const float x = Elem<T>::load(z + (t < g.head ? t : K - g.tail + t - g.head));
+    take(x, [&](float mu) { s += pf_exp(x, mu); });
+  }
+  float M = m;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  if ((t & 63) == 0) sm[t >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  const float Mu = M == -INFINITY ? 0.f : M;
+  s = wave_sum(s * pf_exp(m, Mu));
+  if ((t & 63) == 0) ss[t >> 6] = s;
+  __syncthreads();
+  if (t == 0) {
+    const float rest = logf((ss[0] + ss[1]) + (ss[2] + ss[3]));
+    if (lse) lse[row] = M + rest;
+    lp[row] = (label_score(z, y, K) - M) - rest;     // the two large terms first: what is left is rounded once
+  }
+}
+
+// a wavefront's sum over rows [lo, hi), in 64 bits
+__device__ __forceinline__ double pf_sum(const float* lp, int lo, int hi, int lane) {
+  double v = 0;
+  for (int i = lo + lane; i < hi; i += 64) v += (double)lp[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+__global__ __launch_bounds__(256) void pf_seq_kernel(const float* __restrict__ lp, const int32_t* __restrict__ off, int nseq,
+                                                     float* __restrict__ logps, int R) {
+  const int b = blockIdx.y, lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (s >= nseq) return;
+  int lo, hi;
+  pf_rows(off + (int64_t)b * (nseq + 1), s, R, lo, hi);
+  const double v = pf_sum(lp + (int64_t)b * R, lo, hi, lane);
+  if (lane == 0) logps[(int64_t)b * nseq + s] = (float)v;
+}
+
+// ------------------------------------------------------------------ pairs: a wavefront each
+__global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ lp, const int32_t* __restrict__ off, int pairs, const float* __restrict__ ref,
+                                                      const float* __restrict__ beta, const float* __restrict__ smoothing,
+                                                      float* __restrict__ logps, float* __restrict__ term, float* __restrict__ coef,
+                                                      int R) {
+  const int b = blockIdx.y, lane = threadIdx.x & 63, p = blockIdx.x * 4 + (threadIdx.x >> 6), nseq = 2 * pairs;
+  if (p >= pairs) return;
+  off += (int64_t)b * (nseq + 1);
+  lp += (int64_t)b * R;
+  int lo[2], hi[2];
+  double v[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    pf_rows(off, 2 * p + i, R, lo[i], hi[i]);
+    v[i] = pf_sum(lp, lo[i], hi[i], lane);
+  }
+  const int64_t at = (int64_t)b * nseq + 2 * p;
+  const double be = beta[b], eps = smoothing ? smoothing[b] : 0.f;
+  const double t = be * ((v[0] - (double)ref[at]) - (v[1] - (double)ref[at + 1]));
+  const double e = exp(-fabs(t)), tail = log1p(e);                  // softplus(x) = max(x, 0) + log1p(exp(-|x|))
+  const double up = (t >= 0 ? 1.0 : e) / (1.0 + e), down = (t >= 0 ? e : 1.0) / (1.0 + e);      // sigma(t), sigma(-t)
+  const float c = (float)(-be * ((1.0 - eps) * down - eps * up) / pairs);
+  if (lane == 0) {
+    logps[at] = (float)v[0];
+    logps[at + 1] = (float)v[1];
+    term[(int64_t)b * pairs + p] = (float)((1.0 - eps) * (fmax(-t, 0.0) + tail) + eps * (fmax(t, 0.0) + tail));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    for (int r = lo[i] + lane; r < hi[i]; r += 64)
+      coef[(int64_t)b * R + r] = i ? -c : c;
+}
+
+// ------------------------------------------------------------------ gradient: a row per workgroup; the last one of a
+// model adds its pairs' terms (in order)
+template <typename T>
+__global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int32_t* __restrict__ labels,
+                                                      const int32_t* __restrict__ off, int pairs, const float* __restrict__ lse,
+                                                      const float* __restrict__ coef, const float* __restrict__ term,
+                                                      float* __restrict__ loss, T* dlogits, int R, int K) {
+  constexpr int EPP = PfRow<T>::EPP, NV = 4;
+  __shared__ double sh[4];
+  const int r = blockIdx.x, b = blockIdx.y, t = threadIdx.x, nseq = 2 * pairs;
+  if (r == R) {
+    double v = 0;
+    for (int i = t; i < pairs; i += 256) v += (double)term[(int64_t)b * pairs + i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if ((t & 63) == 0) sh[t >> 6] = v;
+    __syncthreads();
+    if (t == 0) loss[b] = (float)(((sh[0] + sh[1]) + (sh[2] + sh[3])) / pairs);
+    return;
+  }
+  const int64_t row = (int64_t)b * R + r;
+  off += (int64_t)b * (nseq + 1);
+  if (r < off[0] || r >= off[nseq]) return;
+  const int y = labels[row];
+  const T* z = logits + row * K;
+  T* dz = dlogits + row * K;
+  const PfRow<T> g(dz, K);
+  uint4* dv = reinterpret_cast<uint4*>(dz + g.head);
+  if (y < 0) {
+    for (int v = t; v < g.nv; v += 256) dv[v] = make_uint4(0, 0, 0, 0);
+    if (t < g.head + g.tail) Elem<T>::store(dz + (t < g.head ? t : K - g.tail + t - g.head), 0.f);
+    return;
+  }
+  const float c = coef[row], ls = lse[row];
+  auto grad = [&](float x, int k) { return c * ((k == y ? 1.f : 0.f) - pf_exp(x, ls)); };
+  if (((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0) {
+    const uint4* zv = reinterpret_cast<const uint4*>(z + g.head);
+    for (int v0 = t; v0 < g.nv; v0 += 256 * NV) {
+      uint4 u[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (v0 + 256 * j < g.nv) u[j] = zv[v0 + 256 * j];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int v = v0 + 256 * j;
+        if (v >= g.nv) continue;
+        float x[EPP];
+        pf_unpack(u[j], x);
+#pragma unroll
+        for (int e = 0; e < EPP; ++e) x[e] = grad(x[e], g.head + v * EPP + e);
+        dv[v] = pf_pack(x);
+      }
+    }
+    if (t < g.head + g.tail) {
+      const int k = t < g.head ? t : K - g.tail + t - g.head;
+      Elem<T>::store(dz + k, grad(Elem<T>::load(z + k), k));
+    }
+  } else {                                           // logits and gradient lie differently against 16 bytes
+    for (int k = t; k < K; k += 256) Elem<T>::store(dz + k, grad(Elem<T>::load(z + k), k));
+  }
+}
+
+int pf_check(int B, int R, int K, int nseq, int dtype) {
+  if (B <= 0 || R <= 0 || K <= 0 || nseq <= 0 || !valid_dtype(dtype)) return HFTA_EINVAL;
+  return B > 65535 || R == 0x7fffffff ? HFTA_EUNSUPPORTED : HFTA_OK;
+}
+
+template <typename T>
+void pf_rows_launch(int B, int R, int K, int nseq, const void* logits, const int32_t* labels, const int32_t* off, float* lse,
+                    float* lp, hipStream_t st) {
+  hipLaunchKernelGGL(pf_rows_kernel<T>, dim3((unsigned)R, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off, nseq, lse,
+                     lp, R, K);
+}
+
+}  // namespace
+}  // namespace hfta
+
+using namespace hfta;
+
+extern "C" {
+
+int hfta_seq_logps(int B, int R, int K, int nseq, int dtype, const void* logits, const int32_t* labels, const int32_t* seq_offsets,
+                   float* token_logps, float* logps, void* stream) {
+  const int rc = pf_check(B, R, K, nseq, dtype);
+  if (rc == HFTA_EINVAL || !logits || !labels || !seq_offsets || !token_logps || !logps) return HFTA_EINVAL;
+  if (rc != HFTA_OK) return rc;
+  hipStream_t st = as_stream(stream);
+  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
+  else pf_rows_launch<float>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
+  if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
+  hipLaunchKernelGGL(pf_seq_kernel, dim3((unsigned)((nseq + 3) / 4), (unsigned)B), dim3(256), 0, st, token_logps, seq_offsets, nseq,
+                     logps, R);
+  return launch_status();
+}
+
+size_t hfta_preference_loss_workspace_bytes(int B, int R, int npairs) {
+  if (B <= 0 || R <= 0 || npairs <= 0 || npairs > 0x3fffffff) return 0;
+  return ((size_t)B * R * 3 + (size_t)B * npairs) * sizeof(float);     // lse, label terms and factors of the rows; pair terms
+}
+
+int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void* logits, const int32_t* labels,
+                         const int32_t* seq_offsets, const float* ref_logps, const float* beta, const float* label_smoothing,
+                         float* loss, float* logps, void* dlogits, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = pf_check(B, R, K, npairs, dtype);
+  if (rc == HFTA_EINVAL || npairs > 0x3fffffff || !logits || !labels || !seq_offsets || !ref_logps || !beta || !loss || !logps || !dlogits)
+    return HFTA_EINVAL;
+  if (rc != HFTA_OK) return rc;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 4 || ws_bytes < hfta_preference_loss_workspace_bytes(B, R, npairs))
+    return HFTA_EWORKSPACE;
+  hipStream_t st = as_stream(stream);
+  const size_t rows = (size_t)B * R;
+  float *lse = (float*)workspace, *lp = lse + rows, *coef = lp + rows, *term = coef + rows;
+  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
+  else pf_rows_launch<float>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
+  if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
+  hipLaunchKernelGGL(pf_pair_kernel, dim3((unsigned)((npairs + 3) / 4), (unsigned)B), dim3(256), 0, st, lp, seq_offsets,
+                     npairs, ref_logps, beta, label_smoothing, logps, term, coef, R);
+  if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
+  const dim3 grid((unsigned)R + 1u, (unsigned)B);
+  if (dtype == HFTA_BF16)
+    hipLaunchKernelGGL(pf_grad_kernel<bf16_raw>, grid, dim3(256), 0, st, (const bf16_raw*)logits, labels, seq_offsets, npairs, lse,
+                       coef, term, loss, (bf16_raw*)dlogits, R, K);
+  else
+    hipLaunchKernelGGL(pf_grad_kernel<float>, grid, dim3(256), 0, st, (const float*)logits, labels, seq_offsets, npairs, lse, coef,
+                       term, loss, (float*)dlogits, R, K);
+  return launch_status();
+}
+
+}  // extern "C"
