@@ -1,0 +1,356 @@
+// Attention over packed sequences of different lengths with grouped heads, forward and backward (fusion rules table row
+// "MultiheadAttention": the projections are fused Linears, this is what stands between them).
+//
+//   x_ij = scale q_i . k_j for j in i's sequence (causal: j <= i),  lse_i = log sum_j exp x_ij,  p_ij = exp(x_ij - lse_i)
+//   ctx_i = sum_j p_ij v_j
+//   D_i = dctx_i . ctx_i,  ds_ij = p_ij (dctx_i . v_j - D_i)
+//   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dctx_i   (i: all heads of the group)
+//
+// Nothing of the size of the scores is stored.  Forward: one pass over the keys with the running maximum and sum of the
+// softmax; lse is all that the backward needs to form p again.  Backward: two kernels, one per side that owns its sums
+// (a query tile its dq, a key tile its dk and dv over all heads of the group), so that there are no atomics and results
+// are the same bit for bit on every run; scores are formed twice for that (14 instead of 10 products of d per pair).
+//
+// A tile is a stretch of the packed rows, whatever sequences it holds: the keys that its rows see are one stretch again,
+// because sequences are contiguous.  Many short sequences share a tile, and nothing is planned on the host.
+//
+// Matrix instruction 32 x 32: with the keys as its first operand a lane holds one query (l%32) and sixteen keys
+// 8(i/4) + 4(l/32) + i%4, so a row's softmax needs one exchange between two lanes, and the result is the second operand
+// of the product over keys if the other side orders its keys the same way (slots 0..3 of a lane half: keys 4g + 0..3,
+// slots 4..7: 8 + 4g + 0..3).  For bf16 that order is what two LDS transpose reads deliver.  fp32 takes the fp32
+// instruction, whose operands are single values per lane.
+//
+// Entries outside a row's sequence are taken out of the scores by a select, so what stands there does not matter, but
+// in the product over keys a zero probability times a NaN or an infinity would be a NaN.  Products are therefore made
+// as if all values were finite; if a result is not, the workgroup does its rows again, with those values zero in the
+// product over keys and NaN put into what they belong to in the rows that do see them.
+//
+// A workgroup is four wavefronts.  With many rows each takes 32 rows of its own and all keys, which the workgroup stages 64
+// at a time, twice buffered with one barrier per tile.  Where that leaves compute units without work (SPLIT), all four take the
+// same 32 rows and a quarter of the key blocks each, from LDS of their own without barriers, and join at the end.
+#pragma once
+#include "packed_rows.h"
+
+#include <math.h>
+
+namespace hfta {
+
+typedef __bf16 pk_bf8 __attribute__((ext_vector_type(8)));
+typedef float pk_f16 __attribute__((ext_vector_type(16)));
+typedef short pk_s4 __attribute__((ext_vector_type(4)));
+
+constexpr int PK_WT = 32;                                        // rows of a wavefront
+constexpr float PK_LOG2E = 1.4426950408889634f, PK_LN2 = 0.6931471805599453f;
+
+struct PkStr { int64_t b, r, h; };
+struct PkArgs {
+  const void *Q, *K, *V, *dCTX;
+  const int32_t* off;
+  void *CTX, *dQ, *dK, *dV;
+  float *LSE, *Dsum;
+  PkStr qs, ks, cs, dqs, dks;
+  int B, R, nseq, Hq, Hkv, d, causal;
+  float scale;
+};
+struct PkForm { bool bf16, vec, split; };                        // storage, rows in 16-byte pieces, keys split over wavefronts
+int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_packed_fwd.hip
+int pk_dq(const PkArgs& a, const PkForm& f, hipStream_t st);     // attention_packed_dq.hip
+int pk_dkv(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_packed_dkv.hip
+
+__device__ __forceinline__ float pk_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <typename T, int D> struct PkTile { static constexpr int PITCH = D * (int)sizeof(T) + 16; };   // 16 rows' 16-byte reads cover all banks
+
+// ------------------------------------------------------------------ operands
+// A lane's row (l%32) of a 32 x D matrix as the second operand of a product over columns.
+template <typename T, int D> struct PkRow;
+template <int D> struct PkRow<bf16_raw, D> {
+  static constexpr int N = D / 16, STEP = 16, EPP = 8;
+  union Piece { uint4 u; pk_bf8 v; bf16_raw e[8]; };
+  Piece p[N];                                                    // columns 16 s + 8 (l/32) + 0..7
+};
+template <int D> struct PkRow<float, D> {
+  static constexpr int N = D / 8, STEP = 8, EPP = 4;
+  union Piece { uint4 u; float e[4]; };
+  Piece p[N];                                                    // columns 8 s + 4 (l/32) + 0..3
+};
+
+template <typename T, int D, bool VEC>
+__device__ __forceinline__ void pk_load_row(PkRow<T, D>& x, const T* row, bool ok, int d, int g) {
+#pragma unroll
+  for (int s = 0; s < PkRow<T, D>::N; ++s) {
+    const int c = s * PkRow<T, D>::STEP + g * PkRow<T, D>::EPP;
+    x.p[s].u = make_uint4(0, 0, 0, 0);
+    if constexpr (VEC) {
+      if (ok && c < d) x.p[s].u = *reinterpret_cast<const uint4*>(row + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < PkRow<T, D>::EPP; ++e)
+        if (ok && c + e < d) x.p[s].e[e] = row[c + e];
+    }
+  }
+}
+
+// acc[tile row][lane row] = sum over columns of tile row row0 + .. and the lane's row x
+template <int D>
+__device__ __forceinline__ void pk_rows(pk_f16& acc, const unsigned char* tile, int row0, const PkRow<bf16_raw, D>& x, int lane) {
+  const unsigned char* a = tile + (row0 + (lane & 31)) * PkTile<bf16_raw, D>::PITCH + (lane >> 5) * 16;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const pk_bf8*>(a + s * 32), x.p[s].v, acc, 0, 0, 0);
+}
+template <int D>
+__device__ __forceinline__ void pk_rows(pk_f16& acc, const unsigned char* tile, int row0, const PkRow<float, D>& x, int lane) {
+  const unsigned char* a = tile + (row0 + (lane & 31)) * PkTile<float, D>::PITCH + (lane >> 5) * 16;
+#pragma unroll
+  for (int s = 0; s < D / 8; ++s) {
+    const float4 v = *reinterpret_cast<const float4*>(a + s * 32);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.x, x.p[s].e[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.y, x.p[s].e[1], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.z, x.p[s].e[2], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.w, x.p[s].e[3], acc, 0, 0, 0);
+  }
+}
+
+// A product over 32 tile rows: acc[c/32][column c of the tile][lane row] += sum of tile[row0 + i][c] w[i], where w holds
+// the weights as a product's result does.
+template <typename T, int D>
+__device__ __forceinline__ void pk_cols(pk_f16 (&acc)[D / 32], const unsigned char* tile, int row0, const pk_f16& w, int lane) {
+  constexpr int PITCH = PkTile<T, D>::PITCH;
+  if constexpr (sizeof(T) == 2) {
+    typedef __attribute__((address_space(3))) pk_s4* lds_s4;
+    union Frag { uint32_t u[4]; pk_s4 h[2]; pk_bf8 v; } f, x;
+    const int g = lane >> 5, r = lane & 15;
+    const unsigned char* a = tile + (row0 + 4 * g + (r >> 2)) * PITCH + (16 * ((lane >> 4) & 1) + 4 * (r & 3)) * 2;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f.u[e] = pack_bf16x2(w[8 * t + 2 * e], w[8 * t + 2 * e + 1]);
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb) {
+        x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + 16 * t * PITCH + cb * 64));
+        x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + (16 * t + 8) * PITCH + cb * 64));
+        acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v, f.v, acc[cb], 0, 0, 0);
+      }
+    }
+  } else {
+    const unsigned char* a = tile + (row0 + 4 * (lane >> 5)) * PITCH + (lane & 31) * 4;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb)
+        acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(a + (8 * (i >> 2) + (i & 3)) * PITCH + cb * 128),
+                                                       w[i], acc[cb], 0, 0, 0);
+  }
+}
+
+// Tile rows j0 + .. (of the tensor) at row0 of the tile: NaN for the entries that a value which is not finite takes part in,
+// in lane rows that see its row, [lo, hi).
+template <typename T, int D>
+__device__ __forceinline__ void pk_mark(pk_f16 (&acc)[D / 32], const unsigned char* tile, int row0, int j0, int lo, int hi, int lane) {
+  const unsigned char* a = tile + row0 * PkTile<T, D>::PITCH + 4 * (lane >> 5) * (int)sizeof(T);
+#pragma unroll 1
+  for (int r = 0; r < 32; ++r, a += PkTile<T, D>::PITCH) {
+    const bool sees = j0 + r >= lo && j0 + r < hi;
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = Elem<T>::load(reinterpret_cast<const T*>(a) + cb * 32 + 8 * (i >> 2) + (i & 3));
+        if (sees && (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) acc[cb][i] = __builtin_nanf("");
+      }
+  }
+}
+
+// ------------------------------------------------------------------ tiles
+// Rows row0 .. of a [row][D] matrix through registers into LDS, a workgroup's 64 or a wavefront's 32; rows from `hi` on and
+// columns from d on: zeros.
+template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage {
+  static constexpr int ROWS = SPLIT ? 32 : TILE, NT = SPLIT ? 64 : 256, BYTES = ROWS * PkTile<T, D>::PITCH;
+  static constexpr int PPR = D * (int)sizeof(T) / 16, RP = NT / PPR, N = ROWS / RP, EPP = 16 / (int)sizeof(T);
+  union Piece { uint4 u; T e[EPP]; uint32_t w[4]; };
+  Piece v[N];
+  static __device__ __forceinline__ int tid() { return SPLIT ? threadIdx.x & 63 : threadIdx.x; }
+  __device__ __forceinline__ void load(const T* src, int64_t ld, int row0, int hi, int d) {
+    const int r = tid() / PPR, c = (tid() % PPR) * EPP;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int row = row0 + r + RP * n;
+      const T* p = src + (int64_t)row * ld + c;
+      v[n].u = make_uint4(0, 0, 0, 0);
+      if constexpr (VEC) {
+        if (row < hi && c < d) v[n].u = *reinterpret_cast<const uint4*>(p);
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPP; ++e)
+          if (row < hi && c + e < d) v[n].e[e] = p[e];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* tile) const {
+    const int r = tid() / PPR, c = tid() % PPR;
+#pragma unroll
+    for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(tile + (r + RP * n) * PkTile<T, D>::PITCH + c * 16) = v[n].u;
+  }
+  __device__ __forceinline__ void clean() {                      // zeros in place of values that are not finite
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t& x = v[n].w[e];
+        if constexpr (sizeof(T) == 2) {
+          if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+          if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        } else {
+          if ((x & 0x7f800000u) == 0x7f800000u) x = 0;
+        }
+      }
+  }
+};
+// between writing a tile and reading it: all wavefronts, or the lanes of one
+template <bool SPLIT> __device__ __forceinline__ void pk_sync() {
+  if constexpr (SPLIT) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  else __syncthreads();
+}
+
+// a lane's row of a result: columns 32 cb + 8 (i/4) + 4 (l/32) + i%4, column blocks from cb0 on
+template <typename T, int NCB, bool VEC>
+__device__ __forceinline__ void pk_store_row(T* row, const pk_f16 (&acc)[NCB], float f, int cb0, int d, int g) {
+#pragma unroll
+  for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = (cb0 + cb) * 32 + q * 8 + 4 * g;
+      const float x[4] = {f * acc[cb][4 * q], f * acc[cb][4 * q + 1], f * acc[cb][4 * q + 2], f * acc[cb][4 * q + 3]};
+      if constexpr (VEC) {
+        if (c >= d) continue;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(row + c) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        else *reinterpret_cast<float4*>(row + c) = make_float4(x[0], x[1], x[2], x[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < d) Elem<T>::store(row + c + e, x[e]);
+      }
+    }
+}
+
+template <int N> __device__ __forceinline__ bool pk_not_finite(const pk_f16 (&acc)[N]) {
+  float z = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = fmaf(0.f, acc[n][i], z);
+  return z != z;
+}
+
+// The four wavefronts' sums of the same rows, added in order: wavefront w gets column block w (w < D / 32) in acc[0].  lds: 512 D bytes.
+template <int D> __device__ __forceinline__ void pk_join(pk_f16 (&acc)[D / 32], float* lds, int wave, int lane) {
+  __syncthreads();                                               // the tiles that lay there have been read
+#pragma unroll
+  for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds[((wave * (D / 32) + cb) * 16 + i) * 64 + lane] = acc[cb][i];
+  __syncthreads();
+  if (wave < D / 32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float* x = lds + (wave * 16 + i) * 64 + lane;
+      constexpr int W = D / 32 * 1024;
+      acc[0][i] = (x[0] + x[W]) + (x[2 * W] + x[3 * W]);
+    }
+  }
+}
+
+template <typename T> __device__ __forceinline__ const T* pk_at(const void* p, const PkStr& s, int b, int h) {
+  return reinterpret_cast<const T*>(p) + b * s.b + h * s.h;
+}
+template <typename T> __device__ __forceinline__ T* pk_at(void* p, const PkStr& s, int b, int h) {
+  return reinterpret_cast<T*>(p) + b * s.b + h * s.h;
+}
+
+// Workgroup -> (tile, key head, head of its group).  Key heads run fastest, so that where their number is a multiple of
+// eight all workgroups that read one head's keys share an XCD's L2.  The last tiles, of which rows see the most keys where
+// attention is causal, come first; the first tiles do, of which keys are seen by the most rows (KEYS).
+template <bool SPLIT> constexpr int pk_bm() { return SPLIT ? PK_WT : 4 * PK_WT; }
+static inline int pk_tiles(int R, int bm) { return R / bm + (R % bm != 0); }
+template <int BM, bool KEYS> struct PkPlace {
+  int b, hk, hq, t0;
+  __device__ __forceinline__ PkPlace(const PkArgs& a) {
+    const int group = KEYS ? 1 : a.Hq / a.Hkv, nk = a.B * a.Hkv, per = nk * group;
+    const int tile = blockIdx.x / per, rest = blockIdx.x % per, kh = rest % nk;
+    b = kh / a.Hkv;
+    hk = kh % a.Hkv;
+    hq = hk * (a.Hq / a.Hkv) + rest / nk;
+    t0 = (KEYS ? tile : (int)(gridDim.x / per) - 1 - tile) * BM;
+  }
+};
+
+// The rows of a workgroup: what each sees of the other side ([lo, hi), empty outside the sequences), what the workgroup
+// and the wavefront see together, and what all rows of the wavefront see.
+template <int BM> struct PkSpan {
+  int row, lo, hi;
+  bool in;
+  int glo, ghi, wlo, whi, alo, ahi;
+  // queries: keys from the sequence's start; keys: queries up to the sequence's end.  row0: the wavefront's first row in the tile
+  template <bool KEYS> __device__ __forceinline__ void init(PackedRows<BM>& pr, int (&lim)[2], const PkArgs& a, int b, int t0, int row0) {
+    if (threadIdx.x == 0) { lim[0] = 0x7fffffff; lim[1] = 0; }
+    pr.template scan<256>(a.off + (int64_t)b * (a.nseq + 1), a.nseq, a.R, t0);
+    const int i = row0 + (threadIdx.x & 31);
+    row = t0 + i;
+    in = pr.range(t0, i, lo, hi);
+    if (a.causal && in) {
+      if (KEYS) lo = row;
+      else hi = row + 1;
+    }
+    wlo = in ? lo : 0x7fffffff;
+    whi = in ? hi : 0;
+    alo = in ? lo : 0;
+    ahi = in ? hi : 0x7fffffff;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+      wlo = min(wlo, __shfl_xor(wlo, s, 64));
+      whi = max(whi, __shfl_xor(whi, s, 64));
+      alo = max(alo, __shfl_xor(alo, s, 64));
+      ahi = min(ahi, __shfl_xor(ahi, s, 64));
+    }
+    glo = wlo = __builtin_amdgcn_readfirstlane(wlo);
+    ghi = whi = __builtin_amdgcn_readfirstlane(whi);
+    alo = __builtin_amdgcn_readfirstlane(alo);
+    ahi = __builtin_amdgcn_readfirstlane(ahi);
+    if constexpr (BM > PK_WT) {
+      if ((threadIdx.x & 63) == 0) { atomicMin(&lim[0], wlo); atomicMax(&lim[1], whi); }
+      __syncthreads();
+      glo = __builtin_amdgcn_readfirstlane(lim[0]);
+      ghi = __builtin_amdgcn_readfirstlane(lim[1]);
+    }
+  }
+  __device__ __forceinline__ bool none(int j0, int n) const { return j0 >= whi || j0 + n <= wlo; }      // of rows j0 .. j0 + n - 1
+  __device__ __forceinline__ bool all(int j0, int n) const { return j0 >= alo && j0 + n <= ahi; }
+  // whether this lane's row sees row j0 + 8(i/4) + 4g + i%4
+  __device__ __forceinline__ bool sees(int j0, int i, int g) const {
+    const int j = j0 + 8 * (i >> 2) + 4 * g + (i & 3);
+    return j >= lo && j < hi;
+  }
+};
+
+#define PK_LAUNCH(KERNEL, WGS)                                                                               \
+  do {                                                                                                       \
+    const dim3 grid_((unsigned)(WGS)), block_(256);                                                          \
+    if (f.bf16) { PK_LAUNCH_T(KERNEL, bf16_raw); }                                                           \
+    else { PK_LAUNCH_T(KERNEL, float); }                                                                     \
+    return launch_status();                                                                                  \
+  } while (0)
+#define PK_LAUNCH_T(KERNEL, T)                                                                               \
+  do {                                                                                                       \
+    if (a.d <= 32) { PK_LAUNCH_D(KERNEL, T, 32); }                                                           \
+    else if (a.d <= 64) { PK_LAUNCH_D(KERNEL, T, 64); }                                                      \
+    else { PK_LAUNCH_D(KERNEL, T, 128); }                                                                    \
+  } while (0)
+#define PK_LAUNCH_D(KERNEL, T, D)                                                                            \
+  do {                                                                                                       \
+    if (f.split) { hipLaunchKernelGGL((KERNEL<T, D, true, true>), grid_, block_, 0, st, a); }                \
+    else if (f.vec) { hipLaunchKernelGGL((KERNEL<T, D, true, false>), grid_, block_, 0, st, a); }            \
+    else { hipLaunchKernelGGL((KERNEL<T, D, false, false>), grid_, block_, 0, st, a); }                      \
+  } while (0)
+
+}  // namespace hfta

@@ -1,0 +1,123 @@
+// Attention over packed sequences: the backward kernel of the queries, which also leaves D for the one of the keys
+// (attention_packed.h).
+#include "attention_packed.h"
+
+namespace hfta {
+namespace {
+
+template <typename T, int D, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_kernel(PkArgs a) {
+  typedef PkStage<T, D, VEC, SPLIT> Stage;
+  constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();
+  __shared__ __attribute__((aligned(16))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
+  __shared__ PackedRows<BM> pr;
+  __shared__ int lim[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const PkPlace<BM, false> at(a);
+  PkSpan<BM> sp;
+  sp.template init<false>(pr, lim, a, at.b, at.t0, SPLIT ? 0 : wave * PK_WT);
+  if (sp.glo >= sp.ghi) return;
+  const T* kp = pk_at<T>(a.K, a.ks, at.b, at.hk);
+  const T* vp = pk_at<T>(a.V, a.ks, at.b, at.hk);
+  const int64_t srow = ((int64_t)at.b * a.Hq + at.hq) * a.R + sp.row;
+  PkRow<T, D> q, dc;
+  pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)sp.row * a.qs.r, sp.in, a.d, g);
+  pk_load_row<T, D, VEC>(dc, pk_at<T>(a.dCTX, a.cs, at.b, at.hq) + (int64_t)sp.row * a.cs.r, sp.in, a.d, g);
+  float dsum = 0.f;
+  {
+    PkRow<T, D> x;
+    pk_load_row<T, D, VEC>(x, pk_at<T>(a.CTX, a.cs, at.b, at.hq) + (int64_t)sp.row * a.cs.r, sp.in, a.d, g);
+#pragma unroll
+    for (int s = 0; s < PkRow<T, D>::N; ++s)
+#pragma unroll
+      for (int e = 0; e < PkRow<T, D>::EPP; ++e) dsum = fmaf(Elem<T>::to_f32(x.p[s].e[e]), Elem<T>::to_f32(dc.p[s].e[e]), dsum);
+    dsum += __shfl_xor(dsum, 32, 64);
+  }
+  const float lse = sp.in ? a.LSE[srow] * PK_LOG2E : 0.f;
+  if (sp.in && g == 0 && (!SPLIT || wave == 0)) a.Dsum[srow] = dsum;
+  const float c = a.scale * PK_LOG2E;
+  const int first = sp.glo + (SPLIT ? wave * 32 : 0);
+  constexpr int STEP = SPLIT ? 128 : 64;
+  pk_f16 o[D / 32];
+  for (bool safe = false;; safe = true) {
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
+    int buf = SPLIT ? wave : 0;
+    Stage nk, nv;
+    auto fetch = [&](int k0) {
+      nk.load(kp, a.ks.r, k0, sp.ghi, a.d);
+      nv.load(vp, a.ks.r, k0, sp.ghi, a.d);
+    };
+    auto put = [&] {
+      nk.store(tiles + buf * 2 * Stage::BYTES);
+      nv.store(tiles + (buf * 2 + 1) * Stage::BYTES);
+    };
+    if (first < sp.ghi) {
+      fetch(first);
+      put();
+    }
+    for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
+      pk_sync<SPLIT>();
+      const bool more = k0 + STEP < sp.ghi;
+      if (more && !safe) fetch(k0 + STEP);
+      unsigned char* tk = tiles + buf * 2 * Stage::BYTES;
+      const unsigned char* tv = tiles + (buf * 2 + 1) * Stage::BYTES;
+      pk_f16 s[NB];
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const int j0 = k0 + kb * 32;
+        if (sp.none(j0, 32)) continue;
+        pk_f16 p{};
+        s[kb] = pk_f16{};
+        pk_rows<D>(s[kb], tk, kb * 32, q, lane);
+        pk_rows<D>(p, tv, kb * 32, dc, lane);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = pk_exp2(fmaf(c, s[kb][i], -lse)) * (p[i] - dsum);
+        if (!sp.all(j0, 32)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!sp.sees(j0, i, g)) s[kb][i] = 0.f;
+        }
+        if (!safe) pk_cols<T, D>(o, tk, kb * 32, s[kb], lane);
+      }
+      if (safe) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+          if (!sp.none(k0 + kb * 32, 32)) pk_mark<T, D>(o, tk, kb * 32, k0 + kb * 32, sp.lo, sp.hi, lane);
+        pk_sync<SPLIT>();
+        nk.clean();
+        nk.store(tk);
+        pk_sync<SPLIT>();
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+          if (!sp.none(k0 + kb * 32, 32)) pk_cols<T, D>(o, tk, kb * 32, s[kb], lane);
+      }
+      if (more) {
+        if (safe) fetch(k0 + STEP);
+        if (!SPLIT) buf ^= 1;
+        pk_sync<true>();
+        put();
+      }
+    }
+    if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
+  }
+  if constexpr (SPLIT) {
+    pk_join<D>(o, reinterpret_cast<float*>(tiles), wave, lane);
+    if (wave >= D / 32) return;
+  }
+  if (sp.in) {
+    T* row = pk_at<T>(a.dQ, a.dqs, at.b, at.hq) + (int64_t)sp.row * a.dqs.r;
+    if constexpr (SPLIT) {
+      const pk_f16 one[1] = {o[0]};
+      pk_store_row<T, 1, VEC>(row, one, a.scale, wave, a.d, g);
+    } else {
+      pk_store_row<T, D / 32, VEC>(row, o, a.scale, 0, a.d, g);
+    }
+  }
+}
+
+}  // namespace
+
+int pk_dq(const PkArgs& a, const PkForm& f, hipStream_t st) { PK_LAUNCH(pk_dq_kernel, pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq); }
+
+}  // namespace hfta

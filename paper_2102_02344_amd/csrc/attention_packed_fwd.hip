@@ -1,0 +1,151 @@
+// Attention over packed sequences: the forward kernel (attention_packed.h).
+#include "attention_packed.h"
+
+namespace hfta {
+namespace {
+
+template <typename T, int D, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_kernel(PkArgs a) {
+  typedef PkStage<T, D, VEC, SPLIT> Stage;
+  constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();        // key blocks per tile; tiles: a wavefront's, or two in turn
+  __shared__ __attribute__((aligned(16))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
+  __shared__ PackedRows<BM> pr;
+  __shared__ int lim[2];
+  __shared__ float jm[4][32], jl[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const PkPlace<BM, false> at(a);
+  PkSpan<BM> sp;
+  sp.template init<false>(pr, lim, a, at.b, at.t0, SPLIT ? 0 : wave * PK_WT);
+  if (sp.glo >= sp.ghi) return;
+  const T* kp = pk_at<T>(a.K, a.ks, at.b, at.hk);
+  const T* vp = pk_at<T>(a.V, a.ks, at.b, at.hk);
+  PkRow<T, D> q;
+  pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)sp.row * a.qs.r, sp.in, a.d, g);
+  const float c = a.scale * PK_LOG2E;
+  const int first = sp.glo + (SPLIT ? wave * 32 : 0);
+  constexpr int STEP = SPLIT ? 128 : 64;
+  pk_f16 o[D / 32];
+  float m, l;
+  for (bool safe = false;; safe = true) {
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
+    m = -INFINITY;
+    l = 0.f;
+    int buf = SPLIT ? wave : 0;
+    Stage nk, nv;
+    auto fetch = [&](int k0) {
+      nk.load(kp, a.ks.r, k0, sp.ghi, a.d);
+      nv.load(vp, a.ks.r, k0, sp.ghi, a.d);
+    };
+    auto put = [&] {
+      nk.store(tiles + buf * 2 * Stage::BYTES);
+      nv.store(tiles + (buf * 2 + 1) * Stage::BYTES);
+    };
+    if (first < sp.ghi) {
+      fetch(first);
+      put();
+    }
+    for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
+      pk_sync<SPLIT>();
+      const bool more = k0 + STEP < sp.ghi;
+      if (more && !safe) fetch(k0 + STEP);
+      const unsigned char* tk = tiles + buf * 2 * Stage::BYTES;
+      unsigned char* tv = tiles + (buf * 2 + 1) * Stage::BYTES;
+      const bool some = !sp.none(k0, NB * 32);
+      pk_f16 s[NB];
+      float mu = 0.f;
+      if (some) {
+        float mt = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+          s[kb] = pk_f16{};
+          pk_rows<D>(s[kb], tk, kb * 32, q, lane);
+        }
+        if (!sp.all(k0, NB * 32)) {
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (!sp.sees(k0 + kb * 32, i, g)) s[kb][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kb][i]);
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float mn = fmaxf(m, c * mt);
+        mu = mn == -INFINITY ? 0.f : mn;
+        if (__any(mn > m)) {
+          const float f = pk_exp2(m - mu);
+          l *= f;
+#pragma unroll
+          for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][i] *= f;
+          m = mn;
+        }
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[kb][i] = pk_exp2(fmaf(c, s[kb][i], -mu));
+            l += s[kb][i];
+          }
+      }
+      if (safe) {
+        if (some) {
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb) pk_mark<T, D>(o, tv, kb * 32, k0 + kb * 32, sp.lo, sp.hi, lane);
+        }
+        pk_sync<SPLIT>();
+        nv.clean();
+        nv.store(tv);
+        pk_sync<SPLIT>();
+      }
+      if (some) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) pk_cols<T, D>(o, tv, kb * 32, s[kb], lane);
+      }
+      if (more) {
+        if (safe) fetch(k0 + STEP);
+        if (!SPLIT) buf ^= 1;
+        pk_sync<true>();
+        put();
+      }
+    }
+    if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
+  }
+  l += __shfl_xor(l, 32, 64);
+  if constexpr (SPLIT) {
+    if (g == 0) { jm[wave][lane] = m; jl[wave][lane] = l; }
+    __syncthreads();
+    const int r = lane & 31;
+    m = fmaxf(fmaxf(jm[0][r], jm[1][r]), fmaxf(jm[2][r], jm[3][r]));
+    const float mu = m == -INFINITY ? 0.f : m, f = pk_exp2(jm[wave][r] - mu);
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) l += jl[w][r] * pk_exp2(jm[w][r] - mu);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[n][i] *= f;
+    pk_join<D>(o, reinterpret_cast<float*>(tiles), wave, lane);
+    if (wave >= D / 32) return;
+  }
+  if (sp.in) {
+    T* row = pk_at<T>(a.CTX, a.cs, at.b, at.hq) + (int64_t)sp.row * a.cs.r;
+    if constexpr (SPLIT) {
+      const pk_f16 one[1] = {o[0]};
+      pk_store_row<T, 1, VEC>(row, one, 1.f / l, wave, a.d, g);
+    } else {
+      pk_store_row<T, D / 32, VEC>(row, o, 1.f / l, 0, a.d, g);
+    }
+    if (g == 0 && (!SPLIT || wave == 0)) a.LSE[((int64_t)at.b * a.Hq + at.hq) * a.R + sp.row] = (m + __builtin_amdgcn_logf(l)) * PK_LN2;
+  }
+}
+
+}  // namespace
+
+int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st) { PK_LAUNCH(pk_fwd_kernel, pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq); }
+
+}  // namespace hfta
