@@ -47,11 +47,12 @@ struct PkArgs {
   const void *Q, *K, *V, *dCTX;
   const int32_t* off;
   void *CTX, *dQ, *dK, *dV;
-  float *LSE, *Dsum;
+  float *LSE, *Dsum, *part;        // Dsum, part: the backward's workspace
   PkStr qs, ks, cs, dqs, dks;
-  int B, R, nseq, Hq, Hkv, d, causal;
+  int B, R, nseq, Hq, Hkv, d, causal, parts;       // parts: workgroups that share the sums of a tile of keys
   float scale;
 };
+constexpr int PK_PARTS_MAX = 8;
 struct PkForm { bool bf16, vec, split; };                        // storage, rows in 16-byte pieces, keys split over wavefronts
 int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_packed_fwd.hip
 int pk_dq(const PkArgs& a, const PkForm& f, hipStream_t st);     // attention_packed_dq.hip
@@ -156,41 +157,50 @@ __device__ __forceinline__ void pk_mark(pk_f16 (&acc)[D / 32], const unsigned ch
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float x = Elem<T>::load(reinterpret_cast<const T*>(a) + cb * 32 + 8 * (i >> 2) + (i & 3));
-        if (sees && (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) acc[cb][i] = __builtin_nanf("");
+        const float x = Elem<T>::load(reinterpret_cast<const T*>(a) + cb * 32 + 8 * (i >> 2) + (i & 3)), y = sees ? x : 0.f;
+        acc[cb][i] += y - y;                                     // NaN, or nothing
       }
   }
 }
 
 // ------------------------------------------------------------------ tiles
 // Rows row0 .. of a [row][D] matrix through registers into LDS, a workgroup's 64 or a wavefront's 32; rows from `hi` on and
-// columns from d on: zeros.
+// columns from d on: zeros.  In whole pieces the loads go through a buffer that ends with the last row, which gives the
+// zeros; it is placed anew for every tile, so that offsets stay small however far the rows lie.
+typedef int pk_i4 __attribute__((ext_vector_type(4)));
+constexpr int64_t PK_LD_MAX = 1 << 22;                           // elements between rows that such a buffer's offsets take
 template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage {
   static constexpr int ROWS = SPLIT ? 32 : TILE, NT = SPLIT ? 64 : 256, BYTES = ROWS * PkTile<T, D>::PITCH;
-  static constexpr int PPR = D * (int)sizeof(T) / 16, RP = NT / PPR, N = ROWS / RP, EPP = 16 / (int)sizeof(T);
-  union Piece { uint4 u; T e[EPP]; uint32_t w[4]; };
+  static constexpr int PPR = D * (int)sizeof(T) / 16, RP = NT / PPR, N = RP < ROWS ? ROWS / RP : 1, EPP = 16 / (int)sizeof(T);
+  union Piece { pk_i4 i; uint4 u; T e[EPP]; uint32_t w[4]; };
   Piece v[N];
   static __device__ __forceinline__ int tid() { return SPLIT ? threadIdx.x & 63 : threadIdx.x; }
-  __device__ __forceinline__ void load(const T* src, int64_t ld, int row0, int hi, int d) {
+  // src: the tile's first row, rows: how many there are; the same for all threads that share the tile
+  __device__ __forceinline__ void load(const T* src, int64_t ld, int rows, int d) {
     const int r = tid() / PPR, c = (tid() % PPR) * EPP;
+    if constexpr (VEC) {
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<T*>(src), 0, rows > 0 ? ((min(rows, ROWS) - 1) * (int)ld + d) * (int)sizeof(T) : 0, 0x00020000);
+      const uint32_t at = c < d && r < ROWS ? (uint32_t)(r * (int)ld + c) * (uint32_t)sizeof(T) : 0x80000000u, step = (uint32_t)(RP * (int)ld) * (uint32_t)sizeof(T);
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int row = row0 + r + RP * n;
-      const T* p = src + (int64_t)row * ld + c;
-      v[n].u = make_uint4(0, 0, 0, 0);
-      if constexpr (VEC) {
-        if (row < hi && c < d) v[n].u = *reinterpret_cast<const uint4*>(p);
-      } else {
+      for (int n = 0; n < N; ++n) v[n].i = __builtin_amdgcn_raw_buffer_load_b128(rs, at + n * step, 0, 0);
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int row = r + RP * n;
+        const T* p = src + (int64_t)row * ld + c;
+        v[n].u = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int e = 0; e < EPP; ++e)
-          if (row < hi && c + e < d) v[n].e[e] = p[e];
+          if (row < min(rows, ROWS) && c + e < d) v[n].e[e] = p[e];
       }
     }
   }
   __device__ __forceinline__ void store(unsigned char* tile) const {
     const int r = tid() / PPR, c = tid() % PPR;
 #pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(tile + (r + RP * n) * PkTile<T, D>::PITCH + c * 16) = v[n].u;
+    for (int n = 0; n < N; ++n)
+      if (RP <= ROWS || r < ROWS) *reinterpret_cast<uint4*>(tile + (r + RP * n) * PkTile<T, D>::PITCH + c * 16) = v[n].u;
   }
   __device__ __forceinline__ void clean() {                      // zeros in place of values that are not finite
 #pragma unroll
@@ -274,13 +284,14 @@ template <typename T> __device__ __forceinline__ T* pk_at(void* p, const PkStr& 
 template <bool SPLIT> constexpr int pk_bm() { return SPLIT ? PK_WT : 4 * PK_WT; }
 static inline int pk_tiles(int R, int bm) { return R / bm + (R % bm != 0); }
 template <int BM, bool KEYS> struct PkPlace {
-  int b, hk, hq, t0;
+  int b, hk, hq, t0, part;         // KEYS: hq the group's first head
   __device__ __forceinline__ PkPlace(const PkArgs& a) {
-    const int group = KEYS ? 1 : a.Hq / a.Hkv, nk = a.B * a.Hkv, per = nk * group;
+    const int group = KEYS ? a.parts : a.Hq / a.Hkv, nk = a.B * a.Hkv, per = nk * group;
     const int tile = blockIdx.x / per, rest = blockIdx.x % per, kh = rest % nk;
     b = kh / a.Hkv;
     hk = kh % a.Hkv;
-    hq = hk * (a.Hq / a.Hkv) + rest / nk;
+    part = rest / nk;
+    hq = hk * (a.Hq / a.Hkv) + (KEYS ? 0 : part);
     t0 = (KEYS ? tile : (int)(gridDim.x / per) - 1 - tile) * BM;
   }
 };
@@ -333,24 +344,9 @@ template <int BM> struct PkSpan {
   }
 };
 
-#define PK_LAUNCH(KERNEL, WGS)                                                                               \
-  do {                                                                                                       \
-    const dim3 grid_((unsigned)(WGS)), block_(256);                                                          \
-    if (f.bf16) { PK_LAUNCH_T(KERNEL, bf16_raw); }                                                           \
-    else { PK_LAUNCH_T(KERNEL, float); }                                                                     \
-    return launch_status();                                                                                  \
-  } while (0)
-#define PK_LAUNCH_T(KERNEL, T)                                                                               \
-  do {                                                                                                       \
-    if (a.d <= 32) { PK_LAUNCH_D(KERNEL, T, 32); }                                                           \
-    else if (a.d <= 64) { PK_LAUNCH_D(KERNEL, T, 64); }                                                      \
-    else { PK_LAUNCH_D(KERNEL, T, 128); }                                                                    \
-  } while (0)
-#define PK_LAUNCH_D(KERNEL, T, D)                                                                            \
-  do {                                                                                                       \
-    if (f.split) { hipLaunchKernelGGL((KERNEL<T, D, true, true>), grid_, block_, 0, st, a); }                \
-    else if (f.vec) { hipLaunchKernelGGL((KERNEL<T, D, true, false>), grid_, block_, 0, st, a); }            \
-    else { hipLaunchKernelGGL((KERNEL<T, D, false, false>), grid_, block_, 0, st, a); }                      \
-  } while (0)
+// launch<T, D>(a, f, st) of the storage type and the tile's columns
+#define PK_BY_SIZE(launch)                                                                                                            \
+  (f.bf16 ? (a.d <= 32 ? launch<bf16_raw, 32>(a, f, st) : a.d <= 64 ? launch<bf16_raw, 64>(a, f, st) : launch<bf16_raw, 128>(a, f, st)) \
+          : (a.d <= 32 ? launch<float, 32>(a, f, st) : a.d <= 64 ? launch<float, 64>(a, f, st) : launch<float, 128>(a, f, st)))
 
 }  // namespace hfta

@@ -5,142 +5,217 @@
 namespace hfta {
 namespace {
 
-template <typename T, int D, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(256, (D * sizeof(T) <= 128 ? 2 : 1)) void pk_dkv_kernel(PkArgs a) {
-  typedef PkStage<T, D, VEC, SPLIT> Stage;
-  constexpr int ROWS = Stage::ROWS, NB = ROWS / 32, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
-  __shared__ __attribute__((aligned(16))) float stats[NBUF][2][ROWS];      // lse and D of the tile's rows
+// The tiles from which a workgroup's keys are seen: the last rows first, all heads of the group each, so that the
+// workgroups of a sequence's keys read the same ones at the same time.  A workgroup takes every a.parts-th.  Places are kept and moved
+// on, not computed anew: products of 64-bit strides were a thousand cycles a tile.
+template <typename T, int ROWS> struct PkWalk {
+  const T *q, *c;                  // the tile's first row
+  int64_t srow;                    // of LSE and D
+  int64_t qd[2], cd[2];            // a step, and what a step past the last head adds
+  int i0, head, group, di, dh;
+  __device__ __forceinline__ void init(const PkArgs& a, int b, int hq, int glo, int nt, int part) {
+    group = a.Hq / a.Hkv;
+    head = part % group;
+    i0 = glo + (nt - 1 - part / group) * ROWS;
+    q = pk_at<T>(a.Q, a.qs, b, hq + head) + i0 * a.qs.r;
+    c = pk_at<T>(a.dCTX, a.cs, b, hq + head) + i0 * a.cs.r;
+    srow = ((int64_t)b * a.Hq + hq) * a.R;
+    di = a.parts / group * ROWS;
+    dh = a.parts % group;
+    qd[0] = dh * a.qs.h - di * a.qs.r;
+    cd[0] = dh * a.cs.h - di * a.cs.r;
+    qd[1] = -group * a.qs.h - ROWS * a.qs.r;
+    cd[1] = -group * a.cs.h - ROWS * a.cs.r;
+  }
+  __device__ __forceinline__ void next() {
+    head += dh;
+    i0 -= di;
+    q += qd[0];
+    c += cd[0];
+    if (head >= group) {
+      head -= group;
+      i0 -= ROWS;
+      q += qd[1];
+      c += cd[1];
+    }
+  }
+};
+
+// The sums of 32 keys, their operands and the scores are more registers than two wavefronts per SIMD can have (heads of 128).  So
+// two wavefronts share 32 keys: one forms p and dv, the other dctx . v, takes p from LDS, and forms ds and dk -- the same products,
+// half the registers each.  Two barriers per 32 rows; a workgroup takes 64 keys.  Where workgroups are few or uneven (the first
+// keys of a long sequence are seen by all its rows) a.parts of them share the tiles of 64 keys; their sums go through the workspace.
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)sizeof(T) <= 256 ? 3 : 2)) void pk_dkv_kernel(PkArgs a) {
+  typedef PkStage<T, D, VEC, false, 32> Stage;
+  constexpr int ROWS = 32, BM = 64;
+  __shared__ __attribute__((aligned(16))) unsigned char tiles[2 * 2 * Stage::BYTES];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][ROWS];         // lse and D of the tile's rows
+  __shared__ __attribute__((aligned(16))) float prob[2][4][64][4];         // p of a pair: as its wavefronts hold it
   __shared__ PackedRows<BM> pr;
   __shared__ int lim[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const int pair = wave >> 1;
+  const bool forms_v = (wave & 1) == 0;
   const PkPlace<BM, true> at(a);
+  const int part = at.part;
   PkSpan<BM> sp;
-  sp.template init<true>(pr, lim, a, at.b, at.t0, SPLIT ? 0 : wave * PK_WT);
+  sp.template init<true>(pr, lim, a, at.b, at.t0, pair * PK_WT);
   if (sp.glo >= sp.ghi) return;
-  PkRow<T, D> k, v;
-  pk_load_row<T, D, VEC>(k, pk_at<T>(a.K, a.ks, at.b, at.hk) + (int64_t)sp.row * a.ks.r, sp.in, a.d, g);
-  pk_load_row<T, D, VEC>(v, pk_at<T>(a.V, a.ks, at.b, at.hk) + (int64_t)sp.row * a.ks.r, sp.in, a.d, g);
+  PkRow<T, D> x;                                                           // the first's keys, the second's values
+  pk_load_row<T, D, VEC>(x, pk_at<T>(forms_v ? a.K : a.V, a.ks, at.b, at.hk) + (int64_t)sp.row * a.ks.r, sp.in, a.d, g);
   const float c = a.scale * PK_LOG2E;
-  const int nt = (sp.ghi - sp.glo + ROWS - 1) / ROWS, total = nt * (a.Hq / a.Hkv);      // tiles of a head, of the group
-  constexpr int STEP = SPLIT ? 4 : 1;
-  pk_f16 dk[D / 32], dv[D / 32];
+  const int group = a.Hq / a.Hkv, nt = (sp.ghi - sp.glo + ROWS - 1) / ROWS, total = nt * group;
+  pk_f16 o[D / 32];
   for (bool safe = false;; safe = true) {
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = pk_f16{};
-    int buf = SPLIT ? wave : 0;
+    for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
+    int buf = 0;
     Stage nq, nc;
     float nl = 0.f;
-    auto fetch = [&](int n) {
-      const int h = at.hq + n / nt, i0 = sp.glo + n % nt * ROWS;
-      nq.load(pk_at<T>(a.Q, a.qs, at.b, h), a.qs.r, i0, sp.ghi, a.d);
-      nc.load(pk_at<T>(a.dCTX, a.cs, at.b, h), a.cs.r, i0, sp.ghi, a.d);
-      if (Stage::tid() < 2 * ROWS) {
-        const int i = i0 + Stage::tid() % ROWS;
-        const int64_t at_ = ((int64_t)at.b * a.Hq + h) * a.R + i;
-        nl = i < sp.ghi ? (Stage::tid() < ROWS ? a.LSE[at_] * PK_LOG2E : a.Dsum[at_]) : 0.f;
-      }
+    PkWalk<T, ROWS> w;
+    w.init(a, at.b, at.hq, sp.glo, nt, part);
+    int j0 = 0;                                                            // first row of the tile that is multiplied
+    auto fetch = [&] {
+      nq.load(w.q, a.qs.r, sp.ghi - w.i0, a.d);
+      nc.load(w.c, a.cs.r, sp.ghi - w.i0, a.d);
+      if (threadIdx.x < 2 * ROWS) nl = (threadIdx.x < ROWS ? a.LSE : a.Dsum)[w.srow + (int64_t)w.head * a.R + min(w.i0 + (int)threadIdx.x % ROWS, sp.ghi - 1)];
     };
     auto put = [&] {
       nq.store(tiles + buf * 2 * Stage::BYTES);
       nc.store(tiles + (buf * 2 + 1) * Stage::BYTES);
-      if (Stage::tid() < 2 * ROWS) (&stats[buf][0][0])[Stage::tid()] = nl;
+      if (threadIdx.x < 2 * ROWS) (&stats[buf][0][0])[threadIdx.x] = nl;
     };
-    const int first = SPLIT ? wave : 0;
-    if (first < total) {
-      fetch(first);
+    if (part < total) {
+      fetch();
       put();
     }
-    for (int n = first; n < total; n += STEP) {
-      pk_sync<SPLIT>();
-      const bool more = n + STEP < total;
-      if (more && !safe) fetch(n + STEP);
+    for (int n = part; n < total; n += a.parts) {
+      __syncthreads();
+      const bool more = n + a.parts < total;
+      j0 = w.i0;
+      w.next();
+      if (more && !safe) fetch();
       unsigned char* tq = tiles + buf * 2 * Stage::BYTES;
       unsigned char* tc = tiles + (buf * 2 + 1) * Stage::BYTES;
-      const int i0 = sp.glo + n % nt * ROWS;
-      pk_f16 s[NB], p[NB];
+      const bool some = !sp.none(j0, 32);
+      pk_f16 s{};
+      if (some) {
+        pk_rows<D>(s, forms_v ? tq : tc, 0, x, lane);
+        if (forms_v) {
 #pragma unroll
-      for (int qb = 0; qb < NB; ++qb) {
-        const int j0 = i0 + qb * 32;
-        if (sp.none(j0, 32)) continue;
-        s[qb] = pk_f16{};
-        p[qb] = pk_f16{};
-        pk_rows<D>(s[qb], tq, qb * 32, k, lane);
-        pk_rows<D>(p[qb], tc, qb * 32, v, lane);
+          for (int y = 0; y < 4; ++y) {
+            const float4 ls = *reinterpret_cast<const float4*>(&stats[buf][0][y * 8 + 4 * g]);
+            const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float4 ls = *reinterpret_cast<const float4*>(&stats[buf][0][qb * 32 + x * 8 + 4 * g]);
-          const float4 ds = *reinterpret_cast<const float4*>(&stats[buf][1][qb * 32 + x * 8 + 4 * g]);
-          const float lv[4] = {ls.x, ls.y, ls.z, ls.w}, dd[4] = {ds.x, ds.y, ds.z, ds.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * x + e;
-            s[qb][i] = pk_exp2(fmaf(c, s[qb][i], -lv[e]));
-            p[qb][i] = s[qb][i] * (p[qb][i] - dd[e]);
+            for (int e = 0; e < 4; ++e) s[4 * y + e] = pk_exp2(fmaf(c, s[4 * y + e], -PK_LOG2E * lv[e]));
           }
+          if (!sp.all(j0, 32)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (!sp.sees(j0, i, g)) s[i] = 0.f;
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            *reinterpret_cast<float4*>(prob[pair][y][lane]) = make_float4(s[4 * y], s[4 * y + 1], s[4 * y + 2], s[4 * y + 3]);
+        }
+      }
+      __syncthreads();
+      if (some && !forms_v) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float4 ds = *reinterpret_cast<const float4*>(&stats[buf][1][y * 8 + 4 * g]);
+          const float4 p = *reinterpret_cast<const float4*>(prob[pair][y][lane]);
+          const float dd[4] = {ds.x, ds.y, ds.z, ds.w}, pv[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * y + e] = pv[e] * (s[4 * y + e] - dd[e]);
         }
         if (!sp.all(j0, 32)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (!sp.sees(j0, i, g)) s[qb][i] = p[qb][i] = 0.f;
-        }
-        if (!safe) {
-          pk_cols<T, D>(dv, tc, qb * 32, s[qb], lane);
-          pk_cols<T, D>(dk, tq, qb * 32, p[qb], lane);
+            if (!sp.sees(j0, i, g)) s[i] = 0.f;
         }
       }
       if (safe) {
-#pragma unroll
-        for (int qb = 0; qb < NB; ++qb)
-          if (!sp.none(i0 + qb * 32, 32)) {
-            pk_mark<T, D>(dv, tc, qb * 32, i0 + qb * 32, sp.lo, sp.hi, lane);
-            pk_mark<T, D>(dk, tq, qb * 32, i0 + qb * 32, sp.lo, sp.hi, lane);
-          }
-        pk_sync<SPLIT>();
+        if (some) pk_mark<T, D>(o, forms_v ? tc : tq, 0, j0, sp.lo, sp.hi, lane);
+        __syncthreads();
         nq.clean();
         nc.clean();
         nq.store(tq);
         nc.store(tc);
-        pk_sync<SPLIT>();
-#pragma unroll
-        for (int qb = 0; qb < NB; ++qb)
-          if (!sp.none(i0 + qb * 32, 32)) {
-            pk_cols<T, D>(dv, tc, qb * 32, s[qb], lane);
-            pk_cols<T, D>(dk, tq, qb * 32, p[qb], lane);
-          }
+        __syncthreads();
       }
+      if (some) pk_cols<T, D>(o, forms_v ? tc : tq, 0, s, lane);
       if (more) {
-        if (safe) fetch(n + STEP);
-        if (!SPLIT) buf ^= 1;
-        pk_sync<true>();
+        if (safe) fetch();
+        buf ^= 1;
         put();
       }
     }
-    if (safe || !__syncthreads_or(sp.in && (pk_not_finite(dk) || pk_not_finite(dv)))) break;
+    if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
   }
-  if constexpr (SPLIT) {
-    pk_join<D>(dk, reinterpret_cast<float*>(tiles), wave, lane);
-    pk_join<D>(dv, reinterpret_cast<float*>(tiles), wave, lane);
-    if (wave >= D / 32) return;
+  if (!sp.in) return;
+  if (a.parts == 1) {
+    T* row = pk_at<T>(forms_v ? a.dV : a.dK, a.dks, at.b, at.hk) + (int64_t)sp.row * a.dks.r;
+    pk_store_row<T, D / 32, VEC>(row, o, forms_v ? 1.f : a.scale, 0, a.d, g);
+  } else {                                                                 // [parts][dk, dv][B][Hkv][R][d]
+    float* row = a.part + ((((int64_t)part * 2 + forms_v) * a.B + at.b) * a.Hkv + at.hk) * a.R * a.d + (int64_t)sp.row * a.d;
+    pk_store_row<float, D / 32, VEC>(row, o, forms_v ? 1.f : a.scale, 0, a.d, g);
   }
-  if (sp.in) {
-    T* rk = pk_at<T>(a.dK, a.dks, at.b, at.hk) + (int64_t)sp.row * a.dks.r;
-    T* rv = pk_at<T>(a.dV, a.dks, at.b, at.hk) + (int64_t)sp.row * a.dks.r;
-    if constexpr (SPLIT) {
-      const pk_f16 one[2][1] = {{dk[0]}, {dv[0]}};
-      pk_store_row<T, 1, VEC>(rk, one[0], a.scale, wave, a.d, g);
-      pk_store_row<T, 1, VEC>(rv, one[1], 1.f, wave, a.d, g);
-    } else {
-      pk_store_row<T, D / 32, VEC>(rk, dk, a.scale, 0, a.d, g);
-      pk_store_row<T, D / 32, VEC>(rv, dv, 1.f, 0, a.d, g);
-    }
+}
+
+// The parts' sums, added in order: a workgroup takes 32 rows of one key head, dk and dv.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void pk_parts_kernel(PkArgs a) {
+  constexpr int ROWS = 32, W = VEC ? 4 : 1;
+  __shared__ PackedRows<ROWS> pr;
+  const int nk = a.B * a.Hkv, kh = blockIdx.x % nk, b = kh / a.Hkv, hk = kh % a.Hkv, t0 = blockIdx.x / nk * ROWS;
+  pr.template scan<256>(a.off + (int64_t)b * (a.nseq + 1), a.nseq, a.R, t0);
+  const int ppr = a.d / W, lo = max(t0, pr.first), hi = min(t0 + ROWS, pr.last);
+  const int64_t all = (int64_t)nk * a.R * a.d;
+  for (int i = threadIdx.x; i < (hi - lo) * 2 * ppr; i += 256) {
+    const int c = i % ppr * W, x = i / ppr & 1, row = lo + i / ppr / 2;
+    const float* src = a.part + x * all + ((int64_t)kh * a.R + row) * a.d + c;
+    float y[PK_PARTS_MAX][W], v[W];
+#pragma unroll
+    for (int p = 0; p < PK_PARTS_MAX; ++p)                         // all in flight
+      if (p < a.parts) {
+        if constexpr (VEC) {
+          const float4 f = *reinterpret_cast<const float4*>(src + 2 * p * all);
+          y[p][0] = f.x; y[p][1] = f.y; y[p][2] = f.z; y[p][3] = f.w;
+        } else {
+          y[p][0] = src[2 * p * all];
+        }
+      }
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = y[0][e];
+#pragma unroll
+    for (int p = 1; p < PK_PARTS_MAX; ++p)
+      if (p < a.parts) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] += y[p][e];
+      }
+    T* dst = pk_at<T>(x ? a.dV : a.dK, a.dks, b, hk) + (int64_t)row * a.dks.r + c;
+    if constexpr (!VEC) Elem<T>::store(dst, v[0]);
+    else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    else *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
   }
+}
+
+template <typename T, int D> int launch(const PkArgs& a, const PkForm& f, hipStream_t st) {
+  const dim3 grid((unsigned)(pk_tiles(a.R, 2 * PK_WT) * a.B * a.Hkv * a.parts)), block(256);
+  if (f.vec) hipLaunchKernelGGL((pk_dkv_kernel<T, D, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((pk_dkv_kernel<T, D, false>), grid, block, 0, st, a);
+  const int rc = launch_status();
+  if (a.parts == 1 || rc != HFTA_OK) return rc;
+  const dim3 gp((unsigned)(pk_tiles(a.R, 32) * a.B * a.Hkv));
+  if (f.vec) hipLaunchKernelGGL((pk_parts_kernel<T, true>), gp, block, 0, st, a);
+  else hipLaunchKernelGGL((pk_parts_kernel<T, false>), gp, block, 0, st, a);
+  return launch_status();
 }
 
 }  // namespace
 
-int pk_dkv(const PkArgs& a, const PkForm& f, hipStream_t st) {
-  PK_LAUNCH(pk_dkv_kernel, pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hkv);
-}
+int pk_dkv(const PkArgs& a, const PkForm& f, hipStream_t st) { return PK_BY_SIZE(launch); }
 
 }  // namespace hfta

@@ -33,9 +33,13 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
     l = 0.f;
     int buf = SPLIT ? wave : 0;
     Stage nk, nv;
+    const T *kt = kp + (int64_t)first * a.ks.r, *vt = vp + (int64_t)first * a.ks.r;
+    const int64_t step = (int64_t)STEP * a.ks.r;
     auto fetch = [&](int k0) {
-      nk.load(kp, a.ks.r, k0, sp.ghi, a.d);
-      nv.load(vp, a.ks.r, k0, sp.ghi, a.d);
+      nk.load(kt, a.ks.r, sp.ghi - k0, a.d);
+      nv.load(vt, a.ks.r, sp.ghi - k0, a.d);
+      kt += step;
+      vt += step;
     };
     auto put = [&] {
       nk.store(tiles + buf * 2 * Stage::BYTES);
@@ -144,8 +148,16 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
   }
 }
 
+template <typename T, int D> int launch(const PkArgs& a, const PkForm& f, hipStream_t st) {
+  const dim3 grid((unsigned)(pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq)), block(256);
+  if (f.split) hipLaunchKernelGGL((pk_fwd_kernel<T, D, true, true>), grid, block, 0, st, a);
+  else if (f.vec) hipLaunchKernelGGL((pk_fwd_kernel<T, D, true, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((pk_fwd_kernel<T, D, false, false>), grid, block, 0, st, a);
+  return launch_status();
+}
+
 }  // namespace
 
-int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st) { PK_LAUNCH(pk_fwd_kernel, pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq); }
+int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st) { return PK_BY_SIZE(launch); }
 
 }  // namespace hfta
