@@ -336,11 +336,21 @@ template <int BM> struct PkSpan {
     }
   }
   __device__ __forceinline__ bool none(int j0, int n) const { return j0 >= whi || j0 + n <= wlo; }      // of rows j0 .. j0 + n - 1
-  __device__ __forceinline__ bool all(int j0, int n) const { return j0 >= alo && j0 + n <= ahi; }
-  // whether this lane's row sees row j0 + 8(i/4) + 4g + i%4
-  __device__ __forceinline__ bool sees(int j0, int i, int g) const {
-    const int j = j0 + 8 * (i >> 2) + 4 * g + (i & 3);
-    return j >= lo && j < hi;
+  // `none` in place of the entries i of s, tile rows j0 + 8(i/4) + 4g + i%4, that this lane's row does not see: a comparison with a
+  // constant each, on the sides where a row of the wavefront has an end
+  __device__ __forceinline__ void mask(pk_f16& s, int j0, int g, float none) const {
+    if (j0 < alo) {
+      const int x = lo - j0 - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i >> 2) + (i & 3) < x) s[i] = none;
+    }
+    if (j0 + 32 > ahi) {
+      const int x = hi - j0 - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i >> 2) + (i & 3) >= x) s[i] = none;
+    }
   }
 };
 

@@ -110,11 +110,7 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[4 * y + e] = pk_exp2(fmaf(c, s[4 * y + e], -PK_LOG2E * lv[e]));
           }
-          if (!sp.all(j0, 32)) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!sp.sees(j0, i, g)) s[i] = 0.f;
-          }
+          sp.mask(s, j0, g, 0.f);
 #pragma unroll
           for (int y = 0; y < 4; ++y)
             *reinterpret_cast<float4*>(prob[pair][y][lane]) = make_float4(s[4 * y], s[4 * y + 1], s[4 * y + 2], s[4 * y + 3]);
@@ -130,11 +126,7 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[4 * y + e] = pv[e] * (s[4 * y + e] - dd[e]);
         }
-        if (!sp.all(j0, 32)) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!sp.sees(j0, i, g)) s[i] = 0.f;
-        }
+        sp.mask(s, j0, g, 0.f);
       }
       if (safe) {
         if (some) pk_mark<T, D>(o, forms_v ? tc : tq, 0, j0, sp.lo, sp.hi, lane);

@@ -77,11 +77,7 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_ker
         pk_rows<D>(p, tv, kb * 32, dc, lane);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[kb][i] = pk_exp2(fmaf(c, s[kb][i], -lse)) * (p[i] - dsum);
-        if (!sp.all(j0, 32)) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!sp.sees(j0, i, g)) s[kb][i] = 0.f;
-        }
+        sp.mask(s[kb], j0, g, 0.f);
         if (!safe) pk_cols<T, D>(o, tk, kb * 32, s[kb], lane);
       }
       if (safe) {

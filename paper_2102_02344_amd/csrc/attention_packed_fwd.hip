@@ -65,13 +65,8 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
           s[kb] = pk_f16{};
           pk_rows<D>(s[kb], tk, kb * 32, q, lane);
         }
-        if (!sp.all(k0, NB * 32)) {
 #pragma unroll
-          for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!sp.sees(k0 + kb * 32, i, g)) s[kb][i] = -INFINITY;
-        }
+        for (int kb = 0; kb < NB; ++kb) sp.mask(s[kb], k0 + kb * 32, g, -INFINITY);
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
