@@ -29,9 +29,11 @@
 // at a time, twice buffered with one barrier per tile.  Where that leaves compute units without work (SPLIT), all four take the
 // same 32 rows and a quarter of the key blocks each, from LDS of their own without barriers, and join at the end.
 #pragma once
+#include "gemm_dma.h"
 #include "packed_rows.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace hfta {
 
@@ -60,7 +62,15 @@ int pk_dkv(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_pa
 
 __device__ __forceinline__ float pk_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <typename T, int D> struct PkTile { static constexpr int PITCH = D * (int)sizeof(T) + 16; };   // 16 rows' 16-byte reads cover all banks
+// A staged tile: rows of D columns without padding, as the loads into LDS leave them; piece p (16 bytes) of row r lies at place p ^ key(r).
+// Sixteen rows' reads of one piece then cover all 64 banks once, and so do a transpose read's four rows of four pieces.
+template <typename T, int D> struct PkTile {
+  static constexpr int ROW = D * (int)sizeof(T), PPR = ROW / 16;
+  static __device__ __forceinline__ constexpr int key(int r) {
+    return PPR >= 16 ? (r & 3) << 2 | (r >> 2 & 3) : PPR == 8 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : r >> 2 & 3;
+  }
+  static __device__ __forceinline__ int at(int r, int byte) { return r * ROW + (((byte >> 4) ^ key(r)) << 4) + (byte & 15); }
+};
 
 // ------------------------------------------------------------------ operands
 // A lane's row (l%32) of a 32 x D matrix as the second operand of a product over columns.
@@ -92,56 +102,75 @@ __device__ __forceinline__ void pk_load_row(PkRow<T, D>& x, const T* row, bool o
   }
 }
 
-// acc[tile row][lane row] = sum over columns of tile row row0 + .. and the lane's row x
-template <int D>
-__device__ __forceinline__ void pk_rows(pk_f16& acc, const unsigned char* tile, int row0, const PkRow<bf16_raw, D>& x, int lane) {
-  const unsigned char* a = tile + (row0 + (lane & 31)) * PkTile<bf16_raw, D>::PITCH + (lane >> 5) * 16;
+// What follows in the code up to the next branch: AHEAD reads of LDS first, then MFMAS times one matrix instruction and PER reads.  Left to
+// itself the compiler keeps two reads in flight, and each pair's latency shows.
+template <int AHEAD, int MFMAS, int PER> __device__ __forceinline__ void pk_order() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const pk_bf8*>(a + s * 32), x.p[s].v, acc, 0, 0, 0);
-}
-template <int D>
-__device__ __forceinline__ void pk_rows(pk_f16& acc, const unsigned char* tile, int row0, const PkRow<float, D>& x, int lane) {
-  const unsigned char* a = tile + (row0 + (lane & 31)) * PkTile<float, D>::PITCH + (lane >> 5) * 16;
-#pragma unroll
-  for (int s = 0; s < D / 8; ++s) {
-    const float4 v = *reinterpret_cast<const float4*>(a + s * 32);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.x, x.p[s].e[0], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.y, x.p[s].e[1], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.z, x.p[s].e[2], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.w, x.p[s].e[3], acc, 0, 0, 0);
+  for (int i = 0; i < MFMAS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
   }
+}
+
+// acc[n][tile row][lane row] = sum over columns of tile row row0 + 32 n + .. (row0: a multiple of 32) and the lane's row x
+template <typename T, int D, int NB>
+__device__ __forceinline__ void pk_rows(pk_f16 (&acc)[NB], const unsigned char* tile, int row0, const PkRow<T, D>& x, int lane) {
+  typedef PkTile<T, D> Tile;
+  const uint32_t a = (uint32_t)((lane & 31) * Tile::ROW + (((lane >> 5) ^ Tile::key(lane & 31)) << 4));
+  const unsigned char* t = tile + row0 * Tile::ROW;
+#pragma unroll
+  for (int s = 0; s < PkRow<T, D>::N; ++s)                       // two pieces of the tile's row, one for each half of the lanes
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const unsigned char* p = t + (a ^ (uint32_t)(s << 5)) + n * 32 * Tile::ROW;
+      if constexpr (sizeof(T) == 2) {
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const pk_bf8*>(p), x.p[s].v, acc[n], 0, 0, 0);
+      } else {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.x, x.p[s].e[0], acc[n], 0, 0, 0);
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.y, x.p[s].e[1], acc[n], 0, 0, 0);
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.z, x.p[s].e[2], acc[n], 0, 0, 0);
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.w, x.p[s].e[3], acc[n], 0, 0, 0);
+      }
+    }
 }
 
 // A product over 32 tile rows: acc[c/32][column c of the tile][lane row] += sum of tile[row0 + i][c] w[i], where w holds
 // the weights as a product's result does.
 template <typename T, int D>
 __device__ __forceinline__ void pk_cols(pk_f16 (&acc)[D / 32], const unsigned char* tile, int row0, const pk_f16& w, int lane) {
-  constexpr int PITCH = PkTile<T, D>::PITCH;
+  typedef PkTile<T, D> Tile;
+  const int g = lane >> 5;
+  const unsigned char* t0 = tile + row0 * Tile::ROW;
   if constexpr (sizeof(T) == 2) {
     typedef __attribute__((address_space(3))) pk_s4* lds_s4;
     union Frag { uint32_t u[4]; pk_s4 h[2]; pk_bf8 v; } f, x;
-    const int g = lane >> 5, r = lane & 15;
-    const unsigned char* a = tile + (row0 + 4 * g + (r >> 2)) * PITCH + (16 * ((lane >> 4) & 1) + 4 * (r & 3)) * 2;
+    const int r = lane & 15, row = 4 * g + (r >> 2);
+    const uint32_t a = (uint32_t)Tile::at(row, (16 * ((lane >> 4) & 1) + 4 * (r & 3)) * 2);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) f.u[e] = pack_bf16x2(w[8 * t + 2 * e], w[8 * t + 2 * e + 1]);
 #pragma unroll
       for (int cb = 0; cb < D / 32; ++cb) {
-        x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + 16 * t * PITCH + cb * 64));
-        x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + (16 * t + 8) * PITCH + cb * 64));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)                              // eight rows on: another bit of the key
+          x.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(t0 + (a ^ (uint32_t)(cb << 6 | h << 5)) + (16 * t + 8 * h) * Tile::ROW));
         acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v, f.v, acc[cb], 0, 0, 0);
       }
     }
   } else {
-    const unsigned char* a = tile + (row0 + 4 * (lane >> 5)) * PITCH + (lane & 31) * 4;
+    const uint32_t a = (uint32_t)Tile::at(4 * g, (lane & 31) * 4);
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 16; ++i) {
+      constexpr int ROW = Tile::ROW;
+      const int row = 8 * (i >> 2) + (i & 3);                    // (past 4 g: the other bits of the key)
 #pragma unroll
       for (int cb = 0; cb < D / 32; ++cb)
-        acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(a + (8 * (i >> 2) + (i & 3)) * PITCH + cb * 128),
+        acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(t0 + (a ^ (uint32_t)(Tile::key(row) << 4 ^ cb << 7)) + row * ROW),
                                                        w[i], acc[cb], 0, 0, 0);
+    }
   }
 }
 
@@ -149,45 +178,74 @@ __device__ __forceinline__ void pk_cols(pk_f16 (&acc)[D / 32], const unsigned ch
 // in lane rows that see its row, [lo, hi).
 template <typename T, int D>
 __device__ __forceinline__ void pk_mark(pk_f16 (&acc)[D / 32], const unsigned char* tile, int row0, int j0, int lo, int hi, int lane) {
-  const unsigned char* a = tile + row0 * PkTile<T, D>::PITCH + 4 * (lane >> 5) * (int)sizeof(T);
+  typedef PkTile<T, D> Tile;
 #pragma unroll 1
-  for (int r = 0; r < 32; ++r, a += PkTile<T, D>::PITCH) {
+  for (int r = 0; r < 32; ++r) {
     const bool sees = j0 + r >= lo && j0 + r < hi;
 #pragma unroll
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float x = Elem<T>::load(reinterpret_cast<const T*>(a) + cb * 32 + 8 * (i >> 2) + (i & 3)), y = sees ? x : 0.f;
+        const int c = cb * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+        const float x = Elem<T>::load(reinterpret_cast<const T*>(tile + Tile::at(row0 + r, c * (int)sizeof(T)))), y = sees ? x : 0.f;
         acc[cb][i] += y - y;                                     // NaN, or nothing
       }
   }
 }
 
 // ------------------------------------------------------------------ tiles
-// Rows row0 .. of a [row][D] matrix through registers into LDS, a workgroup's 64 or a wavefront's 32; rows from `hi` on and
-// columns from d on: zeros.  In whole pieces the loads go through a buffer that ends with the last row, which gives the
-// zeros; it is placed anew for every tile, so that offsets stay small however far the rows lie.
+// Rows of a [row][D] matrix into LDS, a workgroup's 64 or 32 or (SPLIT) a wavefront's 32; rows that are not there and columns
+// from d on: zeros.  fetch() starts the loads of a tile and land() ends them; the tile's place must not be read in between.
+// In whole pieces the loads go through a buffer that ends with the last row, which gives the zeros; it is placed anew for
+// every tile, so that offsets stay small however far the rows lie.  A workgroup's tile is loaded into LDS itself, without
+// registers (32 of 256 at d = 128); the others pass through them.
 typedef int pk_i4 __attribute__((ext_vector_type(4)));
 constexpr int64_t PK_LD_MAX = 1 << 22;                           // elements between rows that such a buffer's offsets take
+constexpr uint32_t PK_OUT = 0x80000000u;                         // an offset past every such buffer
 template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage {
-  static constexpr int ROWS = SPLIT ? 32 : TILE, NT = SPLIT ? 64 : 256, BYTES = ROWS * PkTile<T, D>::PITCH;
-  static constexpr int PPR = D * (int)sizeof(T) / 16, RP = NT / PPR, N = RP < ROWS ? ROWS / RP : 1, EPP = 16 / (int)sizeof(T);
+  static constexpr int ROWS = SPLIT ? 32 : TILE, NT = SPLIT ? 64 : 256, BYTES = ROWS * PkTile<T, D>::ROW, PIECES = BYTES / 16;
+  static constexpr int PPR = PkTile<T, D>::PPR, N = (PIECES + NT - 1) / NT, EPP = 16 / (int)sizeof(T);
+  static constexpr bool DIRECT = VEC && !SPLIT;
   union Piece { pk_i4 i; uint4 u; T e[EPP]; uint32_t w[4]; };
-  Piece v[N];
+  typename std::conditional<DIRECT, uint32_t, Piece>::type v[N]; // offsets of a lane's pieces, or the pieces
   static __device__ __forceinline__ int tid() { return SPLIT ? threadIdx.x & 63 : threadIdx.x; }
-  // src: the tile's first row, rows: how many there are; the same for all threads that share the tile
-  __device__ __forceinline__ void load(const T* src, int64_t ld, int rows, int d) {
-    const int r = tid() / PPR, c = (tid() % PPR) * EPP;
-    if constexpr (VEC) {
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<T*>(src), 0, rows > 0 ? ((min(rows, ROWS) - 1) * (int)ld + d) * (int)sizeof(T) : 0, 0x00020000);
-      const uint32_t at = c < d && r < ROWS ? (uint32_t)(r * (int)ld + c) * (uint32_t)sizeof(T) : 0x80000000u, step = (uint32_t)(RP * (int)ld) * (uint32_t)sizeof(T);
+  // row and source byte of a thread's n-th place
+  static __device__ __forceinline__ void place(int n, int& row, int& byte) {
+    const int q = n * NT + tid();
+    row = q / PPR;
+    byte = ((q % PPR) ^ PkTile<T, D>::key(row)) * 16;
+  }
+  static __device__ __forceinline__ uint32_t offset(int n, int64_t ld, int d) {
+    int row, byte;
+    place(n, row, byte);
+    return row < ROWS && byte < d * (int)sizeof(T) ? (uint32_t)(row * (int)ld) * (uint32_t)sizeof(T) + (uint32_t)byte : PK_OUT;
+  }
+  __device__ __forceinline__ void init(int64_t ld, int d) {
+    if constexpr (DIRECT) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) v[n].i = __builtin_amdgcn_raw_buffer_load_b128(rs, at + n * step, 0, 0);
+      for (int n = 0; n < N; ++n) v[n] = offset(n, ld, d);
+    }
+  }
+  // src: the tile's first row, rows: how many there are; the same for all threads that share the tile
+  __device__ __forceinline__ void fetch(unsigned char* tile, const T* src, int64_t ld, int rows, int d) {
+    const uint32_t bytes = rows > 0 ? (uint32_t)((min(rows, ROWS) - 1) * (int)ld + d) * (uint32_t)sizeof(T) : 0u;
+    if constexpr (DIRECT) {
+      const dma_i32x4 rs = dma_rsrc(src, bytes);
+      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile;
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if ((n * NT + wave * 64) < PIECES) dma_load(lds + (uint32_t)(n * NT + wave * 64) * 16u, v[n], rs);
+    } else if constexpr (VEC) {
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(src), 0, (int)bytes, 0x00020000);
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n].i = __builtin_amdgcn_raw_buffer_load_b128(rs, offset(n, ld, d), 0, 0);
     } else {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const int row = r + RP * n;
+        int row, byte;
+        place(n, row, byte);
+        const int c = byte / (int)sizeof(T);
         const T* p = src + (int64_t)row * ld + c;
         v[n].u = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -196,25 +254,30 @@ template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage
       }
     }
   }
-  __device__ __forceinline__ void store(unsigned char* tile) const {
-    const int r = tid() / PPR, c = tid() % PPR;
+  __device__ __forceinline__ void land(unsigned char* tile) const {
+    if constexpr (DIRECT) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-      if (RP <= ROWS || r < ROWS) *reinterpret_cast<uint4*>(tile + (r + RP * n) * PkTile<T, D>::PITCH + c * 16) = v[n].u;
+      for (int n = 0; n < N; ++n)
+        if (n * NT + tid() < PIECES) *reinterpret_cast<uint4*>(tile + (n * NT + tid()) * 16) = v[n].u;
+    }
   }
-  __device__ __forceinline__ void clean() {                      // zeros in place of values that are not finite
-#pragma unroll
-    for (int n = 0; n < N; ++n)
+  static __device__ __forceinline__ void clean(unsigned char* tile, int rows) {      // zeros in place of values that are not finite
+    for (int q = tid(); q < rows * PPR; q += NT) {
+      Piece x;
+      x.u = *reinterpret_cast<const uint4*>(tile + q * 16);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        uint32_t& x = v[n].w[e];
         if constexpr (sizeof(T) == 2) {
-          if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-          if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+          if ((x.w[e] & 0x7f80u) == 0x7f80u) x.w[e] &= 0xffff0000u;
+          if ((x.w[e] & 0x7f800000u) == 0x7f800000u) x.w[e] &= 0xffffu;
         } else {
-          if ((x & 0x7f800000u) == 0x7f800000u) x = 0;
+          if ((x.w[e] & 0x7f800000u) == 0x7f800000u) x.w[e] = 0;
         }
       }
+      *reinterpret_cast<uint4*>(tile + q * 16) = x.u;
+    }
   }
 };
 // between writing a tile and reading it: all wavefronts, or the lanes of one

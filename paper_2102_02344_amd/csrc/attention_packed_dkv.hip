@@ -49,7 +49,7 @@ template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)sizeof(T) <= 256 ? 3 : 2)) void pk_dkv_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, false, 32> Stage;
   constexpr int ROWS = 32, BM = 64;
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[2 * 2 * Stage::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * 2 * Stage::BYTES];
   __shared__ __attribute__((aligned(16))) float stats[2][2][ROWS];         // lse and D of the tile's rows
   __shared__ __attribute__((aligned(16))) float prob[2][4][64][4];         // p of a pair: as its wavefronts hold it
   __shared__ PackedRows<BM> pr;
@@ -72,36 +72,41 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
     for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
     int buf = 0;
     Stage nq, nc;
+    nq.init(a.qs.r, a.d);
+    nc.init(a.cs.r, a.d);
     float nl = 0.f;
     PkWalk<T, ROWS> w;
     w.init(a, at.b, at.hq, sp.glo, nt, part);
     int j0 = 0;                                                            // first row of the tile that is multiplied
-    auto fetch = [&] {
-      nq.load(w.q, a.qs.r, sp.ghi - w.i0, a.d);
-      nc.load(w.c, a.cs.r, sp.ghi - w.i0, a.d);
+    auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
+    auto fetch = [&](int b) {
       if (threadIdx.x < 2 * ROWS) nl = (threadIdx.x < ROWS ? a.LSE : a.Dsum)[w.srow + (int64_t)w.head * a.R + min(w.i0 + (int)threadIdx.x % ROWS, sp.ghi - 1)];
+      nq.fetch(place(b, 0), w.q, a.qs.r, sp.ghi - w.i0, a.d);
+      nc.fetch(place(b, 1), w.c, a.cs.r, sp.ghi - w.i0, a.d);
     };
-    auto put = [&] {
-      nq.store(tiles + buf * 2 * Stage::BYTES);
-      nc.store(tiles + (buf * 2 + 1) * Stage::BYTES);
-      if (threadIdx.x < 2 * ROWS) (&stats[buf][0][0])[threadIdx.x] = nl;
+    auto land = [&](int b) {
+      if (threadIdx.x < 2 * ROWS) (&stats[b][0][0])[threadIdx.x] = nl;
+      nq.land(place(b, 0));
+      nc.land(place(b, 1));
     };
     if (part < total) {
-      fetch();
-      put();
+      fetch(0);
+      land(0);
     }
     for (int n = part; n < total; n += a.parts) {
       __syncthreads();
       const bool more = n + a.parts < total;
       j0 = w.i0;
       w.next();
-      if (more && !safe) fetch();
-      unsigned char* tq = tiles + buf * 2 * Stage::BYTES;
-      unsigned char* tc = tiles + (buf * 2 + 1) * Stage::BYTES;
+      if (more && !safe) fetch(buf ^ 1);
+      unsigned char* tq = place(buf, 0);
+      unsigned char* tc = place(buf, 1);
       const bool some = !sp.none(j0, 32);
-      pk_f16 s{};
+      pk_f16 sn[1] = {pk_f16{}};
+      pk_f16& s = sn[0];
       if (some) {
-        pk_rows<D>(s, forms_v ? tq : tc, 0, x, lane);
+        pk_rows<T, D, 1>(sn, forms_v ? tq : tc, 0, x, lane);
+        if constexpr (sizeof(T) == 2) pk_order<4, D / 16, 1>();
         if (forms_v) {
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
@@ -131,17 +136,18 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
       if (safe) {
         if (some) pk_mark<T, D>(o, forms_v ? tc : tq, 0, j0, sp.lo, sp.hi, lane);
         __syncthreads();
-        nq.clean();
-        nc.clean();
-        nq.store(tq);
-        nc.store(tc);
+        Stage::clean(tq, ROWS);
+        Stage::clean(tc, ROWS);
         __syncthreads();
       }
-      if (some) pk_cols<T, D>(o, forms_v ? tc : tq, 0, s, lane);
+      if (some) {
+        pk_cols<T, D>(o, forms_v ? tc : tq, 0, s, lane);
+        if constexpr (sizeof(T) == 2) pk_order<4, D / 16, 2>();
+      }
       if (more) {
-        if (safe) fetch();
+        if (safe) fetch(buf ^ 1);
+        land(buf ^ 1);
         buf ^= 1;
-        put();
       }
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;

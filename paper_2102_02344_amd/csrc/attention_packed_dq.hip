@@ -9,7 +9,7 @@ template <typename T, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, SPLIT> Stage;
   constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
   __shared__ PackedRows<BM> pr;
   __shared__ int lim[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
@@ -44,59 +44,58 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_ker
     for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
     int buf = SPLIT ? wave : 0;
     Stage nk, nv;
+    nk.init(a.ks.r, a.d);
+    nv.init(a.ks.r, a.d);
     const T *kt = kp + (int64_t)first * a.ks.r, *vt = vp + (int64_t)first * a.ks.r;
     const int64_t step = (int64_t)STEP * a.ks.r;
-    auto fetch = [&](int k0) {
-      nk.load(kt, a.ks.r, sp.ghi - k0, a.d);
-      nv.load(vt, a.ks.r, sp.ghi - k0, a.d);
+    auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
+    auto fetch = [&](int b, int k0) {
+      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - k0, a.d);
+      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - k0, a.d);
       kt += step;
       vt += step;
     };
-    auto put = [&] {
-      nk.store(tiles + buf * 2 * Stage::BYTES);
-      nv.store(tiles + (buf * 2 + 1) * Stage::BYTES);
+    auto land = [&](int b) {
+      nk.land(place(b, 0));
+      nv.land(place(b, 1));
     };
     if (first < sp.ghi) {
-      fetch(first);
-      put();
+      fetch(buf, first);
+      land(buf);
     }
     for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
       pk_sync<SPLIT>();
       const bool more = k0 + STEP < sp.ghi;
-      if (more && !safe) fetch(k0 + STEP);
-      unsigned char* tk = tiles + buf * 2 * Stage::BYTES;
-      const unsigned char* tv = tiles + (buf * 2 + 1) * Stage::BYTES;
-      pk_f16 s[NB];
+      const int other = SPLIT ? buf : buf ^ 1;
+      if (more && !safe) fetch(other, k0 + STEP);
+      unsigned char* tk = place(buf, 0);
+      const unsigned char* tv = place(buf, 1);
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb) {
         const int j0 = k0 + kb * 32;
-        if (sp.none(j0, 32)) continue;
-        pk_f16 p{};
-        s[kb] = pk_f16{};
-        pk_rows<D>(s[kb], tk, kb * 32, q, lane);
-        pk_rows<D>(p, tv, kb * 32, dc, lane);
+        const bool some = !sp.none(j0, 32);
+        pk_f16 s[1] = {pk_f16{}};
+        if (some) {
+          pk_f16 p[1] = {pk_f16{}};
+          pk_rows<T, D, 1>(s, tk, kb * 32, q, lane);
+          pk_rows<T, D, 1>(p, tv, kb * 32, dc, lane);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = pk_exp2(fmaf(c, s[kb][i], -lse)) * (p[i] - dsum);
-        sp.mask(s[kb], j0, g, 0.f);
-        if (!safe) pk_cols<T, D>(o, tk, kb * 32, s[kb], lane);
-      }
-      if (safe) {
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-          if (!sp.none(k0 + kb * 32, 32)) pk_mark<T, D>(o, tk, kb * 32, k0 + kb * 32, sp.lo, sp.hi, lane);
-        pk_sync<SPLIT>();
-        nk.clean();
-        nk.store(tk);
-        pk_sync<SPLIT>();
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-          if (!sp.none(k0 + kb * 32, 32)) pk_cols<T, D>(o, tk, kb * 32, s[kb], lane);
+          for (int i = 0; i < 16; ++i) s[0][i] = pk_exp2(fmaf(c, s[0][i], -lse)) * (p[0][i] - dsum);
+          sp.mask(s[0], j0, g, 0.f);
+        }
+        if (safe) {
+          if (some) pk_mark<T, D>(o, tk, kb * 32, j0, sp.lo, sp.hi, lane);
+          pk_sync<SPLIT>();
+          Stage::clean(tk + kb * 32 * PkTile<T, D>::ROW, 32);
+          pk_sync<SPLIT>();
+        }
+        if (some) pk_cols<T, D>(o, tk, kb * 32, s[0], lane);
       }
       if (more) {
-        if (safe) fetch(k0 + STEP);
-        if (!SPLIT) buf ^= 1;
+        if (safe) fetch(other, k0 + STEP);
         pk_sync<true>();
-        put();
+        land(other);
+        buf = other;
       }
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;

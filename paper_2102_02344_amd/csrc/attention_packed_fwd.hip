@@ -8,7 +8,7 @@ template <typename T, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, SPLIT> Stage;
   constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();        // key blocks per tile; tiles: a wavefront's, or two in turn
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
   __shared__ PackedRows<BM> pr;
   __shared__ int lim[2];
   __shared__ float jm[4][32], jl[4][32];
@@ -33,38 +33,41 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
     l = 0.f;
     int buf = SPLIT ? wave : 0;
     Stage nk, nv;
+    nk.init(a.ks.r, a.d);
+    nv.init(a.ks.r, a.d);
     const T *kt = kp + (int64_t)first * a.ks.r, *vt = vp + (int64_t)first * a.ks.r;
     const int64_t step = (int64_t)STEP * a.ks.r;
-    auto fetch = [&](int k0) {
-      nk.load(kt, a.ks.r, sp.ghi - k0, a.d);
-      nv.load(vt, a.ks.r, sp.ghi - k0, a.d);
+    auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
+    auto fetch = [&](int b, int k0) {
+      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - k0, a.d);
+      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - k0, a.d);
       kt += step;
       vt += step;
     };
-    auto put = [&] {
-      nk.store(tiles + buf * 2 * Stage::BYTES);
-      nv.store(tiles + (buf * 2 + 1) * Stage::BYTES);
+    auto land = [&](int b) {
+      nk.land(place(b, 0));
+      nv.land(place(b, 1));
     };
     if (first < sp.ghi) {
-      fetch(first);
-      put();
+      fetch(buf, first);
+      land(buf);
     }
     for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
       pk_sync<SPLIT>();
       const bool more = k0 + STEP < sp.ghi;
-      if (more && !safe) fetch(k0 + STEP);
-      const unsigned char* tk = tiles + buf * 2 * Stage::BYTES;
-      unsigned char* tv = tiles + (buf * 2 + 1) * Stage::BYTES;
+      const int other = SPLIT ? buf : buf ^ 1;
+      if (more && !safe) fetch(other, k0 + STEP);
+      const unsigned char* tk = place(buf, 0);
+      unsigned char* tv = place(buf, 1);
       const bool some = !sp.none(k0, NB * 32);
       pk_f16 s[NB];
       float mu = 0.f;
       if (some) {
         float mt = -INFINITY;
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
-          s[kb] = pk_f16{};
-          pk_rows<D>(s[kb], tk, kb * 32, q, lane);
-        }
+        for (int kb = 0; kb < NB; ++kb) s[kb] = pk_f16{};
+        pk_rows<T, D, NB>(s, tk, 0, q, lane);
+        if constexpr (sizeof(T) == 2) pk_order<4, NB * D / 16, 1>();
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) sp.mask(s[kb], k0 + kb * 32, g, -INFINITY);
 #pragma unroll
@@ -97,19 +100,19 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
           for (int kb = 0; kb < NB; ++kb) pk_mark<T, D>(o, tv, kb * 32, k0 + kb * 32, sp.lo, sp.hi, lane);
         }
         pk_sync<SPLIT>();
-        nv.clean();
-        nv.store(tv);
+        Stage::clean(tv, Stage::ROWS);
         pk_sync<SPLIT>();
       }
       if (some) {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) pk_cols<T, D>(o, tv, kb * 32, s[kb], lane);
+        if constexpr (sizeof(T) == 2) pk_order<4, NB * D / 16, 2>();
       }
       if (more) {
-        if (safe) fetch(k0 + STEP);
-        if (!SPLIT) buf ^= 1;
+        if (safe) fetch(other, k0 + STEP);
         pk_sync<true>();
-        put();
+        land(other);
+        buf = other;
       }
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
