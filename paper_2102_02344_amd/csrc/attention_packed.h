@@ -45,6 +45,16 @@ constexpr int PK_WT = 32;                                        // rows of a wa
 constexpr float PK_LOG2E = 1.4426950408889634f, PK_LN2 = 0.6931471805599453f;
 
 struct PkStr { int64_t b, r, h; };
+// x / d for x < 2^31 by a product (d >= 1): m = floor(2^(31 + l) / d) + 1 with l = ceil(log2 d) is off by at most 1 / 2^(31 + l) d per unit of x
+struct PkDiv {
+  uint32_t d, m, s;
+  PkDiv() = default;
+  explicit PkDiv(uint32_t x) : d(x), m(0), s(0) {
+    while ((1ull << s) < x) ++s;
+    m = (uint32_t)((1ull << (31 + s)) / x + 1);
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> 31 >> s); }
+};
 struct PkArgs {
   const void *Q, *K, *V, *dCTX;
   const int32_t* off;
@@ -52,6 +62,7 @@ struct PkArgs {
   float *LSE, *Dsum, *part;        // Dsum, part: the backward's workspace
   PkStr qs, ks, cs, dqs, dks;
   int B, R, nseq, Hq, Hkv, d, causal, parts;       // parts: workgroups that share the sums of a tile of keys
+  PkDiv by_heads, by_hkv, by_group, by_parts;      // B Hkv, Hkv, Hq / Hkv, parts
   float scale;
 };
 constexpr int PK_PARTS_MAX = 8;
@@ -60,6 +71,12 @@ int pk_fwd(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_pa
 int pk_dq(const PkArgs& a, const PkForm& f, hipStream_t st);     // attention_packed_dq.hip
 int pk_dkv(const PkArgs& a, const PkForm& f, hipStream_t st);    // attention_packed_dkv.hip
 
+constexpr float PK_SLACK = 8.f;
+// of a lane and the one 32 on
+__device__ __forceinline__ float pk_both_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 __device__ __forceinline__ float pk_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A staged tile: rows of D columns without padding, as the loads into LDS leave them; piece p (16 bytes) of row r lies at place p ^ key(r).
@@ -194,6 +211,8 @@ __device__ __forceinline__ void pk_mark(pk_f16 (&acc)[D / 32], const unsigned ch
 }
 
 // ------------------------------------------------------------------ tiles
+// until none of this wavefront's loads is in flight
+__device__ __forceinline__ void pk_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Rows of a [row][D] matrix into LDS, a workgroup's 64 or 32 or (SPLIT) a wavefront's 32; rows that are not there and columns
 // from d on: zeros.  fetch() starts the loads of a tile and land() ends them; the tile's place must not be read in between.
 // In whole pieces the loads go through a buffer that ends with the last row, which gives the zeros; it is placed anew for
@@ -231,7 +250,7 @@ template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage
     const uint32_t bytes = rows > 0 ? (uint32_t)((min(rows, ROWS) - 1) * (int)ld + d) * (uint32_t)sizeof(T) : 0u;
     if constexpr (DIRECT) {
       const dma_i32x4 rs = dma_rsrc(src, bytes);
-      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile;
+      const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile);
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -256,7 +275,7 @@ template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage
   }
   __device__ __forceinline__ void land(unsigned char* tile) const {
     if constexpr (DIRECT) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      pk_landed();
     } else {
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -280,6 +299,13 @@ template <typename T, int D, bool VEC, bool SPLIT, int TILE = 64> struct PkStage
     }
   }
 };
+// 32 values from src, of which `rows` are there, to LDS, by lanes 0..31
+__device__ __forceinline__ void pk_fetch32(float* lds, const float* src, int rows, int lane) {
+  const dma_i32x4 rs = dma_rsrc(src, rows > 0 ? (uint32_t)min(rows, 32) * 4u : 0u);
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)lds);
+  if (lane < 32)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(at), "v"((uint32_t)lane * 4u), "s"(rs) : "memory", "m0");
+}
 // between writing a tile and reading it: all wavefronts, or the lanes of one
 template <bool SPLIT> __device__ __forceinline__ void pk_sync() {
   if constexpr (SPLIT) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -349,53 +375,58 @@ static inline int pk_tiles(int R, int bm) { return R / bm + (R % bm != 0); }
 template <int BM, bool KEYS> struct PkPlace {
   int b, hk, hq, t0, part;         // KEYS: hq the group's first head
   __device__ __forceinline__ PkPlace(const PkArgs& a) {
-    const int group = KEYS ? a.parts : a.Hq / a.Hkv, nk = a.B * a.Hkv, per = nk * group;
-    const int tile = blockIdx.x / per, rest = blockIdx.x % per, kh = rest % nk;
-    b = kh / a.Hkv;
-    hk = kh % a.Hkv;
-    part = rest / nk;
-    hq = hk * (a.Hq / a.Hkv) + (KEYS ? 0 : part);
-    t0 = (KEYS ? tile : (int)(gridDim.x / per) - 1 - tile) * BM;
+    const uint32_t outer = a.by_heads(blockIdx.x), kh = blockIdx.x - outer * a.by_heads.d;       // of all key heads
+    const PkDiv& by = KEYS ? a.by_parts : a.by_group;
+    const uint32_t tile = by(outer), tiles = by(a.by_heads(gridDim.x));
+    part = (int)(outer - tile * by.d);
+    b = (int)a.by_hkv(kh);
+    hk = (int)kh - b * a.Hkv;
+    hq = hk * (int)a.by_group.d + (KEYS ? 0 : part);
+    t0 = (int)(KEYS ? tile : tiles - 1 - tile) * BM;
   }
 };
 
 // The rows of a workgroup: what each sees of the other side ([lo, hi), empty outside the sequences), what the workgroup
-// and the wavefront see together, and what all rows of the wavefront see.
+// and the wavefront see together, and what all rows of the wavefront see.  Both ends grow with the row, so the first and the last
+// row tell.
 template <int BM> struct PkSpan {
   int row, lo, hi;
   bool in;
   int glo, ghi, wlo, whi, alo, ahi;
-  // queries: keys from the sequence's start; keys: queries up to the sequence's end.  row0: the wavefront's first row in the tile
-  template <bool KEYS> __device__ __forceinline__ void init(PackedRows<BM>& pr, int (&lim)[2], const PkArgs& a, int b, int t0, int row0) {
-    if (threadIdx.x == 0) { lim[0] = 0x7fffffff; lim[1] = 0; }
+  // queries: keys from the sequence's start; keys: queries up to the sequence's end
+  template <bool KEYS> static __device__ __forceinline__ bool ends(const PackedRows<BM>& pr, int causal, int t0, int i, int& lo, int& hi) {
+    const bool in = pr.range(t0, i, lo, hi);
+    if (causal && in) {
+      if (KEYS) lo = t0 + i;
+      else hi = t0 + i + 1;
+    }
+    return in;
+  }
+  // row0: the wavefront's first row in the tile
+  template <bool KEYS> __device__ __forceinline__ void init(PackedRows<BM>& pr, const PkArgs& a, int b, int t0, int row0) {
     pr.template scan<256>(a.off + (int64_t)b * (a.nseq + 1), a.nseq, a.R, t0);
-    const int i = row0 + (threadIdx.x & 31);
+    const int i = row0 + (threadIdx.x & 31), f = max(pr.first - t0, 0), l = min(pr.last - t0, BM) - 1;
     row = t0 + i;
-    in = pr.range(t0, i, lo, hi);
-    if (a.causal && in) {
-      if (KEYS) lo = row;
-      else hi = row + 1;
+    in = ends<KEYS>(pr, a.causal, t0, i, lo, hi);
+    glo = 0x7fffffff;
+    ghi = 0;
+    int x;
+    if (f <= l) {
+      ends<KEYS>(pr, a.causal, t0, f, glo, x);
+      ends<KEYS>(pr, a.causal, t0, l, x, ghi);
     }
-    wlo = in ? lo : 0x7fffffff;
-    whi = in ? hi : 0;
-    alo = in ? lo : 0;
-    ahi = in ? hi : 0x7fffffff;
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) {
-      wlo = min(wlo, __shfl_xor(wlo, s, 64));
-      whi = max(whi, __shfl_xor(whi, s, 64));
-      alo = max(alo, __shfl_xor(alo, s, 64));
-      ahi = min(ahi, __shfl_xor(ahi, s, 64));
-    }
-    glo = wlo = __builtin_amdgcn_readfirstlane(wlo);
-    ghi = whi = __builtin_amdgcn_readfirstlane(whi);
-    alo = __builtin_amdgcn_readfirstlane(alo);
-    ahi = __builtin_amdgcn_readfirstlane(ahi);
-    if constexpr (BM > PK_WT) {
-      if ((threadIdx.x & 63) == 0) { atomicMin(&lim[0], wlo); atomicMax(&lim[1], whi); }
-      __syncthreads();
-      glo = __builtin_amdgcn_readfirstlane(lim[0]);
-      ghi = __builtin_amdgcn_readfirstlane(lim[1]);
+    glo = __builtin_amdgcn_readfirstlane(glo);
+    ghi = __builtin_amdgcn_readfirstlane(ghi);
+    const uint32_t m = (uint32_t)__ballot(in);
+    wlo = 0x7fffffff;
+    whi = alo = 0;
+    ahi = 0x7fffffff;
+    if (m) {
+      const int fl = __builtin_ctz(m), ll = 31 - __builtin_clz(m);
+      wlo = __builtin_amdgcn_readlane(lo, fl);
+      ahi = __builtin_amdgcn_readlane(hi, fl);
+      alo = __builtin_amdgcn_readlane(lo, ll);
+      whi = __builtin_amdgcn_readlane(hi, ll);
     }
   }
   __device__ __forceinline__ bool none(int j0, int n) const { return j0 >= whi || j0 + n <= wlo; }      // of rows j0 .. j0 + n - 1

@@ -24,6 +24,12 @@ int pk_parts(int B, int R, int nseq, int Hq, int Hkv) {
   return p < 1 ? 1 : (int)p;
 }
 size_t pk_sums(int B, int R, int Hq) { return ((size_t)B * Hq * R * sizeof(float) + 255) / 256 * 256; }     // bytes of D
+void pk_places(PkArgs& a) {
+  a.by_heads = PkDiv((uint32_t)(a.B * a.Hkv));
+  a.by_hkv = PkDiv((uint32_t)a.Hkv);
+  a.by_group = PkDiv((uint32_t)(a.Hq / a.Hkv));
+  a.by_parts = PkDiv((uint32_t)a.parts);
+}
 PkStr pk_str(const int64_t* s) { return s ? PkStr{s[0], s[1], s[2]} : PkStr{0, 0, 0}; }
 
 // vec: rows in whole 16-byte pieces -- pointers, strides and head widths.  split: tiles of 128 rows would be fewer than two
@@ -56,6 +62,8 @@ int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.Q = Q; a.K = K; a.V = V; a.off = seq_offsets; a.CTX = CTX; a.LSE = LSE;
   a.qs = pk_str(qs); a.ks = pk_str(kvs); a.cs = pk_str(cs);
   a.B = B; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.causal = causal != 0; a.scale = scale;
+  a.parts = 1;
+  pk_places(a);
   const void* p[] = {Q, K, V, CTX};
   return pk_fwd(a, pk_form(a, dtype, p, 4, Hq), as_stream(stream));
 }
@@ -86,6 +94,7 @@ int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.parts = pk_parts(B, R, nseq, Hq, Hkv);
   a.qs = pk_str(qs); a.ks = pk_str(kvs); a.cs = pk_str(cs); a.dqs = pk_str(dqs); a.dks = pk_str(dkvs);
   a.B = B; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.causal = causal != 0; a.scale = scale;
+  pk_places(a);
   const void* p[] = {Q, K, V, CTX, dCTX, dQ, dK, dV};
   hipStream_t st = as_stream(stream);
   const int rq = pk_dq(a, pk_form(a, dtype, p, 8, Hq), st);

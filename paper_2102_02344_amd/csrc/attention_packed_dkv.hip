@@ -8,33 +8,41 @@ namespace {
 // The tiles from which a workgroup's keys are seen: the last rows first, all heads of the group each, so that the
 // workgroups of a sequence's keys read the same ones at the same time.  A workgroup takes every a.parts-th.  Places are kept and moved
 // on, not computed anew: products of 64-bit strides were a thousand cycles a tile.
-template <typename T, int ROWS> struct PkWalk {
-  const T *q, *c;                  // the tile's first row
-  int64_t srow;                    // of LSE and D
-  int64_t qd[2], cd[2];            // a step, and what a step past the last head adds
+template <int ROWS> struct PkPlaceOf {
   int i0, head, group, di, dh;
-  __device__ __forceinline__ void init(const PkArgs& a, int b, int hq, int glo, int nt, int part) {
+  __device__ __forceinline__ PkPlaceOf(const PkArgs& a, int glo, int nt, int part) {
     group = a.Hq / a.Hkv;
     head = part % group;
     i0 = glo + (nt - 1 - part / group) * ROWS;
-    q = pk_at<T>(a.Q, a.qs, b, hq + head) + i0 * a.qs.r;
-    c = pk_at<T>(a.dCTX, a.cs, b, hq + head) + i0 * a.cs.r;
-    srow = ((int64_t)b * a.Hq + hq) * a.R;
     di = a.parts / group * ROWS;
     dh = a.parts % group;
-    qd[0] = dh * a.qs.h - di * a.qs.r;
-    cd[0] = dh * a.cs.h - di * a.cs.r;
-    qd[1] = -group * a.qs.h - ROWS * a.qs.r;
-    cd[1] = -group * a.cs.h - ROWS * a.cs.r;
   }
-  __device__ __forceinline__ void next() {
+  __device__ __forceinline__ bool next() {                       // whether past the last head
     head += dh;
     i0 -= di;
+    const bool past = head >= group;
+    if (past) { head -= group; i0 -= ROWS; }
+    return past;
+  }
+};
+template <typename T, int ROWS> struct PkWalk : PkPlaceOf<ROWS> {
+  const T *q, *c;                  // the tile's first row
+  int64_t srow;                    // of LSE and D
+  int64_t qd[2], cd[2];            // a step, and what a step past the last head adds
+  __device__ __forceinline__ PkWalk(const PkArgs& a, int b, int hq, int glo, int nt, int part) : PkPlaceOf<ROWS>(a, glo, nt, part) {
+    const int64_t gr = this->group, di = this->di, dh = this->dh, i0 = this->i0;
+    q = pk_at<T>(a.Q, a.qs, b, hq + this->head) + i0 * a.qs.r;
+    c = pk_at<T>(a.dCTX, a.cs, b, hq + this->head) + i0 * a.cs.r;
+    srow = ((int64_t)b * a.Hq + hq) * a.R;
+    qd[0] = dh * a.qs.h - di * a.qs.r;
+    cd[0] = dh * a.cs.h - di * a.cs.r;
+    qd[1] = -gr * a.qs.h - ROWS * a.qs.r;
+    cd[1] = -gr * a.cs.h - ROWS * a.cs.r;
+  }
+  __device__ __forceinline__ void next() {
     q += qd[0];
     c += cd[0];
-    if (head >= group) {
-      head -= group;
-      i0 -= ROWS;
+    if (PkPlaceOf<ROWS>::next()) {
       q += qd[1];
       c += cd[1];
     }
@@ -48,22 +56,22 @@ template <typename T, int ROWS> struct PkWalk {
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)sizeof(T) <= 256 ? 3 : 2)) void pk_dkv_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, false, 32> Stage;
-  constexpr int ROWS = 32, BM = 64;
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * 2 * Stage::BYTES];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][ROWS];         // lse and D of the tile's rows
+  constexpr int ROWS = 32, BM = 64, NBUF = 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
+  __shared__ __attribute__((aligned(16))) float stats[NBUF][2][ROWS];      // lse and D of the tile's rows
   __shared__ __attribute__((aligned(16))) float prob[2][4][64][4];         // p of a pair: as its wavefronts hold it
   __shared__ PackedRows<BM> pr;
-  __shared__ int lim[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   const int pair = wave >> 1;
   const bool forms_v = (wave & 1) == 0;
   const PkPlace<BM, true> at(a);
   const int part = at.part;
   PkSpan<BM> sp;
-  sp.template init<true>(pr, lim, a, at.b, at.t0, pair * PK_WT);
-  if (sp.glo >= sp.ghi) return;
+  const int own = at.t0 + pair * PK_WT + (lane & 31);
   PkRow<T, D> x;                                                           // the first's keys, the second's values
-  pk_load_row<T, D, VEC>(x, pk_at<T>(forms_v ? a.K : a.V, a.ks, at.b, at.hk) + (int64_t)sp.row * a.ks.r, sp.in, a.d, g);
+  pk_load_row<T, D, VEC>(x, pk_at<T>(forms_v ? a.K : a.V, a.ks, at.b, at.hk) + (int64_t)own * a.ks.r, own < a.R, a.d, g);
+  sp.template init<true>(pr, a, at.b, at.t0, pair * PK_WT);
+  if (sp.glo >= sp.ghi) return;
   const float c = a.scale * PK_LOG2E;
   const int group = a.Hq / a.Hkv, nt = (sp.ghi - sp.glo + ROWS - 1) / ROWS, total = nt * group;
   pk_f16 o[D / 32];
@@ -74,31 +82,31 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
     Stage nq, nc;
     nq.init(a.qs.r, a.d);
     nc.init(a.cs.r, a.d);
-    float nl = 0.f;
-    PkWalk<T, ROWS> w;
-    w.init(a, at.b, at.hq, sp.glo, nt, part);
-    int j0 = 0;                                                            // first row of the tile that is multiplied
+    PkWalk<T, ROWS> w(a, at.b, at.hq, sp.glo, nt, part);
     auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
+    int nf = part;                                                         // the next tile that is loaded
     auto fetch = [&](int b) {
-      if (threadIdx.x < 2 * ROWS) nl = (threadIdx.x < ROWS ? a.LSE : a.Dsum)[w.srow + (int64_t)w.head * a.R + min(w.i0 + (int)threadIdx.x % ROWS, sp.ghi - 1)];
-      nq.fetch(place(b, 0), w.q, a.qs.r, sp.ghi - w.i0, a.d);
-      nc.fetch(place(b, 1), w.c, a.cs.r, sp.ghi - w.i0, a.d);
-    };
-    auto land = [&](int b) {
-      if (threadIdx.x < 2 * ROWS) (&stats[b][0][0])[threadIdx.x] = nl;
-      nq.land(place(b, 0));
-      nc.land(place(b, 1));
-    };
-    if (part < total) {
-      fetch(0);
-      land(0);
-    }
-    for (int n = part; n < total; n += a.parts) {
-      __syncthreads();
-      const bool more = n + a.parts < total;
-      j0 = w.i0;
+      const int rows = sp.ghi - w.i0;
+      if (wave < 2) pk_fetch32(stats[b][wave], (wave ? a.Dsum : a.LSE) + w.srow + (int64_t)w.head * a.R + w.i0, rows, lane);
+      nq.fetch(place(b, 0), w.q, a.qs.r, rows, a.d);
+      nc.fetch(place(b, 1), w.c, a.cs.r, rows, a.d);
       w.next();
-      if (more && !safe) fetch(buf ^ 1);
+      nf += a.parts;
+    };
+    if (!safe && nf < total) fetch(buf);
+    PkPlaceOf<ROWS> at_(a, sp.glo, nt, part);                              // first row of the tile that is multiplied
+    for (int n = part; n < total; n += a.parts) {
+      if (__builtin_expect(safe, 0)) {                                                          // one at a time
+        __syncthreads();
+        fetch(buf);
+      }
+      pk_landed();                                                         // lse and D
+      nq.land(place(buf, 0));
+      nc.land(place(buf, 1));
+      __syncthreads();
+      const int j0 = at_.i0;
+      at_.next();
+      if (!safe && nf < total) fetch(buf ^ 1);
       unsigned char* tq = place(buf, 0);
       unsigned char* tc = place(buf, 1);
       const bool some = !sp.none(j0, 32);
@@ -133,7 +141,7 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
         }
         sp.mask(s, j0, g, 0.f);
       }
-      if (safe) {
+      if (__builtin_expect(safe, 0)) {
         if (some) pk_mark<T, D>(o, forms_v ? tc : tq, 0, j0, sp.lo, sp.hi, lane);
         __syncthreads();
         Stage::clean(tq, ROWS);
@@ -144,11 +152,7 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
         pk_cols<T, D>(o, forms_v ? tc : tq, 0, s, lane);
         if constexpr (sizeof(T) == 2) pk_order<4, D / 16, 2>();
       }
-      if (more) {
-        if (safe) fetch(buf ^ 1);
-        land(buf ^ 1);
-        buf ^= 1;
-      }
+      if (!safe) buf ^= 1;
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
   }

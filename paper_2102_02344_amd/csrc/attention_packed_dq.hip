@@ -8,33 +8,36 @@ namespace {
 template <typename T, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, SPLIT> Stage;
-  constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();
+  constexpr int NB = SPLIT ? 1 : 2, BM = pk_bm<SPLIT>();         // key blocks per tile, rows of the workgroup
+  constexpr int NBUF = SPLIT ? 4 : 2;                            // tiles: a wavefront's, or in turn
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
   __shared__ PackedRows<BM> pr;
-  __shared__ int lim[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   const PkPlace<BM, false> at(a);
   PkSpan<BM> sp;
-  sp.template init<false>(pr, lim, a, at.b, at.t0, SPLIT ? 0 : wave * PK_WT);
-  if (sp.glo >= sp.ghi) return;
-  const T* kp = pk_at<T>(a.K, a.ks, at.b, at.hk);
-  const T* vp = pk_at<T>(a.V, a.ks, at.b, at.hk);
-  const int64_t srow = ((int64_t)at.b * a.Hq + at.hq) * a.R + sp.row;
+  const int row0 = SPLIT ? 0 : wave * PK_WT, own = at.t0 + row0 + (lane & 31);
+  const bool there = own < a.R;                                  // (what stands in rows of no sequence does not matter)
+  const int64_t srow = ((int64_t)at.b * a.Hq + at.hq) * a.R + own;
   PkRow<T, D> q, dc;
-  pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)sp.row * a.qs.r, sp.in, a.d, g);
-  pk_load_row<T, D, VEC>(dc, pk_at<T>(a.dCTX, a.cs, at.b, at.hq) + (int64_t)sp.row * a.cs.r, sp.in, a.d, g);
-  float dsum = 0.f;
+  float lse, dsum = 0.f;
   {
     PkRow<T, D> x;
-    pk_load_row<T, D, VEC>(x, pk_at<T>(a.CTX, a.cs, at.b, at.hq) + (int64_t)sp.row * a.cs.r, sp.in, a.d, g);
+    pk_load_row<T, D, VEC>(dc, pk_at<T>(a.dCTX, a.cs, at.b, at.hq) + (int64_t)own * a.cs.r, there, a.d, g);
+    pk_load_row<T, D, VEC>(x, pk_at<T>(a.CTX, a.cs, at.b, at.hq) + (int64_t)own * a.cs.r, there, a.d, g);
+    pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)own * a.qs.r, there, a.d, g);
+    lse = there ? a.LSE[srow] : 0.f;
+    sp.template init<false>(pr, a, at.b, at.t0, row0);
+    if (sp.glo >= sp.ghi) return;
 #pragma unroll
     for (int s = 0; s < PkRow<T, D>::N; ++s)
 #pragma unroll
       for (int e = 0; e < PkRow<T, D>::EPP; ++e) dsum = fmaf(Elem<T>::to_f32(x.p[s].e[e]), Elem<T>::to_f32(dc.p[s].e[e]), dsum);
     dsum += __shfl_xor(dsum, 32, 64);
   }
-  const float lse = sp.in ? a.LSE[srow] * PK_LOG2E : 0.f;
+  lse *= PK_LOG2E;
   if (sp.in && g == 0 && (!SPLIT || wave == 0)) a.Dsum[srow] = dsum;
+  const T* kp = pk_at<T>(a.K, a.ks, at.b, at.hk);
+  const T* vp = pk_at<T>(a.V, a.ks, at.b, at.hk);
   const float c = a.scale * PK_LOG2E;
   const int first = sp.glo + (SPLIT ? wave * 32 : 0);
   constexpr int STEP = SPLIT ? 128 : 64;
@@ -48,26 +51,25 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_ker
     nv.init(a.ks.r, a.d);
     const T *kt = kp + (int64_t)first * a.ks.r, *vt = vp + (int64_t)first * a.ks.r;
     const int64_t step = (int64_t)STEP * a.ks.r;
+    int kf = first;                                              // the next tile that is loaded
     auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
-    auto fetch = [&](int b, int k0) {
-      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - k0, a.d);
-      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - k0, a.d);
+    auto fetch = [&](int b) {
+      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - kf, a.d);
+      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - kf, a.d);
       kt += step;
       vt += step;
+      kf += STEP;
     };
-    auto land = [&](int b) {
-      nk.land(place(b, 0));
-      nv.land(place(b, 1));
-    };
-    if (first < sp.ghi) {
-      fetch(buf, first);
-      land(buf);
-    }
+    if (!safe && kf < sp.ghi) fetch(buf);
     for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
+      if (__builtin_expect(safe, 0)) {                                                // one at a time
+        pk_sync<SPLIT>();
+        fetch(buf);
+      }
+      nk.land(place(buf, 0));
+      nv.land(place(buf, 1));
       pk_sync<SPLIT>();
-      const bool more = k0 + STEP < sp.ghi;
-      const int other = SPLIT ? buf : buf ^ 1;
-      if (more && !safe) fetch(other, k0 + STEP);
+      if (!safe && kf < sp.ghi) fetch(SPLIT ? buf : buf ^ 1);
       unsigned char* tk = place(buf, 0);
       const unsigned char* tv = place(buf, 1);
 #pragma unroll
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_ker
           for (int i = 0; i < 16; ++i) s[0][i] = pk_exp2(fmaf(c, s[0][i], -lse)) * (p[0][i] - dsum);
           sp.mask(s[0], j0, g, 0.f);
         }
-        if (safe) {
+        if (__builtin_expect(safe, 0)) {
           if (some) pk_mark<T, D>(o, tk, kb * 32, j0, sp.lo, sp.hi, lane);
           pk_sync<SPLIT>();
           Stage::clean(tk + kb * 32 * PkTile<T, D>::ROW, 32);
@@ -91,12 +93,7 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_ker
         }
         if (some) pk_cols<T, D>(o, tk, kb * 32, s[0], lane);
       }
-      if (more) {
-        if (safe) fetch(other, k0 + STEP);
-        pk_sync<true>();
-        land(other);
-        buf = other;
-      }
+      if (!SPLIT && !safe) buf ^= 1;
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
   }

@@ -7,20 +7,21 @@ namespace {
 template <typename T, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_kernel(PkArgs a) {
   typedef PkStage<T, D, VEC, SPLIT> Stage;
-  constexpr int NB = SPLIT ? 1 : 2, NBUF = SPLIT ? 4 : 2, BM = pk_bm<SPLIT>();        // key blocks per tile; tiles: a wavefront's, or two in turn
+  constexpr int NB = SPLIT ? 1 : 2, BM = pk_bm<SPLIT>();         // key blocks per tile, rows of the workgroup
+  constexpr int NBUF = SPLIT ? 4 : 2;                            // tiles: a wavefront's, or in turn
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[NBUF * 2 * Stage::BYTES];
   __shared__ PackedRows<BM> pr;
-  __shared__ int lim[2];
   __shared__ float jm[4][32], jl[4][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   const PkPlace<BM, false> at(a);
   PkSpan<BM> sp;
-  sp.template init<false>(pr, lim, a, at.b, at.t0, SPLIT ? 0 : wave * PK_WT);
+  const int row0 = SPLIT ? 0 : wave * PK_WT, own = at.t0 + row0 + (lane & 31);
+  PkRow<T, D> q;                                                 // (what stands in rows of no sequence does not matter)
+  pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)own * a.qs.r, own < a.R, a.d, g);
+  sp.template init<false>(pr, a, at.b, at.t0, row0);
   if (sp.glo >= sp.ghi) return;
   const T* kp = pk_at<T>(a.K, a.ks, at.b, at.hk);
   const T* vp = pk_at<T>(a.V, a.ks, at.b, at.hk);
-  PkRow<T, D> q;
-  pk_load_row<T, D, VEC>(q, pk_at<T>(a.Q, a.qs, at.b, at.hq) + (int64_t)sp.row * a.qs.r, sp.in, a.d, g);
   const float c = a.scale * PK_LOG2E;
   const int first = sp.glo + (SPLIT ? wave * 32 : 0);
   constexpr int STEP = SPLIT ? 128 : 64;
@@ -37,26 +38,25 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
     nv.init(a.ks.r, a.d);
     const T *kt = kp + (int64_t)first * a.ks.r, *vt = vp + (int64_t)first * a.ks.r;
     const int64_t step = (int64_t)STEP * a.ks.r;
+    int kf = first;                                              // the next tile that is loaded
     auto place = [&](int b, int i) { return tiles + (b * 2 + i) * Stage::BYTES; };
-    auto fetch = [&](int b, int k0) {
-      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - k0, a.d);
-      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - k0, a.d);
+    auto fetch = [&](int b) {
+      nk.fetch(place(b, 0), kt, a.ks.r, sp.ghi - kf, a.d);
+      nv.fetch(place(b, 1), vt, a.ks.r, sp.ghi - kf, a.d);
       kt += step;
       vt += step;
+      kf += STEP;
     };
-    auto land = [&](int b) {
-      nk.land(place(b, 0));
-      nv.land(place(b, 1));
-    };
-    if (first < sp.ghi) {
-      fetch(buf, first);
-      land(buf);
-    }
+    if (!safe && kf < sp.ghi) fetch(buf);
     for (int k0 = first; k0 < sp.ghi; k0 += STEP) {
+      if (__builtin_expect(safe, 0)) {                                                // one at a time
+        pk_sync<SPLIT>();
+        fetch(buf);
+      }
+      nk.land(place(buf, 0));
+      nv.land(place(buf, 1));
       pk_sync<SPLIT>();
-      const bool more = k0 + STEP < sp.ghi;
-      const int other = SPLIT ? buf : buf ^ 1;
-      if (more && !safe) fetch(other, k0 + STEP);
+      if (!safe && kf < sp.ghi) fetch(SPLIT ? buf : buf ^ 1);
       const unsigned char* tk = place(buf, 0);
       unsigned char* tv = place(buf, 1);
       const bool some = !sp.none(k0, NB * 32);
@@ -74,18 +74,20 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kb][i]);
-        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-        const float mn = fmaxf(m, c * mt);
-        mu = mn == -INFINITY ? 0.f : mn;
-        if (__any(mn > m)) {
-          const float f = pk_exp2(m - mu);
+        mt = pk_both_max(mt);
+        // The maximum that p is taken against moves only where it would let p grow past 2^PK_SLACK: sums and products are
+        // consistent with any, and are divided by each other at the end.
+        const float mn = c * mt;
+        if (__any(mn > m + PK_SLACK)) {
+          const float to = fmaxf(m, mn), f = pk_exp2(m - (to == -INFINITY ? 0.f : to));
           l *= f;
 #pragma unroll
           for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[n][i] *= f;
-          m = mn;
+          m = to;
         }
+        mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
             l += s[kb][i];
           }
       }
-      if (safe) {
+      if (__builtin_expect(safe, 0)) {
         if (some) {
 #pragma unroll
           for (int kb = 0; kb < NB; ++kb) pk_mark<T, D>(o, tv, kb * 32, k0 + kb * 32, sp.lo, sp.hi, lane);
@@ -108,12 +110,7 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
         for (int kb = 0; kb < NB; ++kb) pk_cols<T, D>(o, tv, kb * 32, s[kb], lane);
         if constexpr (sizeof(T) == 2) pk_order<4, NB * D / 16, 2>();
       }
-      if (more) {
-        if (safe) fetch(other, k0 + STEP);
-        pk_sync<true>();
-        land(other);
-        buf = other;
-      }
+      if (!SPLIT && !safe) buf ^= 1;
     }
     if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
   }

@@ -17,12 +17,14 @@ template <int ROWS> struct PackedRows {
   // called by all NT threads; ends with a barrier
   template <int NT> __device__ __forceinline__ void scan(const int32_t* __restrict__ off, int nseq, int R, int t0) {
     const int t = threadIdx.x, end = t0 + ROWS - 1;
+    int next = t <= nseq ? off[t] : 0;
     for (int i = t; i < ROWS / 32; i += NT) mark[i] = 0;
     if (t == 0) { lo = -1; hi = 0x7fffffff; first = 0x7fffffff; last = -1; }
     __syncthreads();
     int vlo = -1, vhi = 0x7fffffff, vfirst = 0x7fffffff, vlast = -1;
     for (int i = t; i <= nseq; i += NT) {
-      const int o = min(max(off[i], 0), R);
+      const int o = min(max(next, 0), R);
+      if (i + NT <= nseq) next = off[i + NT];
       vfirst = min(vfirst, o);
       vlast = max(vlast, o);
       if (o <= t0) vlo = max(vlo, o);
