@@ -659,8 +659,8 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
  * Language models on packed sequences (fusion rules table rows "Embedding" and "MultiheadAttention"; appendix "Fused Loss").
  * Each model's R rows hold nseq sequences of any lengths back to back: sequence s is rows [seq_offsets[b][s],
  * seq_offsets[b][s + 1]) of model b, seq_offsets: device int32 [B][nseq + 1], non-decreasing, in [0, R].  Sequences may be
- * empty, and every model has its own.  Rows in front of the first and behind the last sequence belong to none: nothing of them is
- * read, and what the calls return per row is left as it was there (clear it once where a later call reads it).  Offsets are
+ * empty, and every model has its own.  Rows in front of the first and behind the last sequence belong to none: what stands in
+ * them does not matter, and what the calls return per row is left as it was there (clear it once where a later call reads it).  Offsets are
  * taken into [0, R]; if they are not in order the results are not defined, but nothing outside the tensors is touched.
  * Results are the same bit for bit on every run.
  *
@@ -687,7 +687,8 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
  *   label_smoothing[b];   beta, label_smoothing: fp32 [B] (label_smoothing NULL: 0).  dlogits: the gradient, storage dtype, 0 in rows with a negative
  *   label; it may be logits itself.  A label >= K makes its model's loss and its pair's gradient NaN.  Workspace
  *   hfta_preference_loss_workspace_bytes, 4-byte aligned (EWORKSPACE).
- * EUNSUPPORTED above 65535 models (attention: above 2^31 - 1 workgroups).
+ * EUNSUPPORTED above 65535 models, 2^28 rows or 2^30 tokens of an embedding, 2^24 - 2 rows of logits (each of a model), and, attention, above
+ * 2^24 - 1 tiles of 64 rows of one head in all.
  * ---------------------------------------------------------------------- */
 int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
                               const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, float scale,

@@ -8,8 +8,8 @@ int pk_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, float sc
   if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || !(scale > 0.f) ||
       isinf(scale) || R > 0x7fffffff - 128)
     return HFTA_EINVAL;
-  const int64_t tiles = pk_tiles(R, PK_WT);
-  return d > 128 || (int64_t)B * Hq > 0x7fffffff / tiles ? HFTA_EUNSUPPORTED : HFTA_OK;
+  // (a launch has fewer than 2^32 threads; tiles are of at least 64 rows where there are many)
+  return d > 128 || (int64_t)B * Hq > 0xffffff / pk_tiles(R, 2 * PK_WT) ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 // Workgroups that share the sums of 64 keys, so that there are about 2048 of them: eight per compute unit, enough to even out the
 // keys that many rows see with those that few do.  A part is at least 16 tiles of 32 rows on average, or two where the

@@ -76,16 +76,16 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
           for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kb][i]);
         mt = pk_both_max(mt);
         // The maximum that p is taken against moves only where it would let p grow past 2^PK_SLACK: sums and products are
-        // consistent with any, and are divided by each other at the end.
-        const float mn = c * mt;
-        if (__any(mn > m + PK_SLACK)) {
-          const float to = fmaxf(m, mn), f = pk_exp2(m - (to == -INFINITY ? 0.f : to));
+        // consistent with any, and are divided by each other at the end.  (Each row by itself: its bits do not depend on the others.)
+        const bool grows = c * mt > m + PK_SLACK;
+        if (__any(grows)) {
+          const float f = grows ? pk_exp2(m - c * mt) : 1.f;
           l *= f;
 #pragma unroll
           for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[n][i] *= f;
-          m = to;
+          m = grows ? c * mt : m;
         }
         mu = m == -INFINITY ? 0.f : m;
 #pragma unroll

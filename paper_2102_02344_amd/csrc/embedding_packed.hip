@@ -449,7 +449,7 @@ __global__ __launch_bounds__(256) void ep_join_kernel(const uint2* __restrict__ 
 
 int ep_check(int B, int R, int V, int E, int dtype) {
   if (B <= 0 || R <= 0 || V <= 0 || E <= 0 || !valid_dtype(dtype)) return HFTA_EINVAL;
-  return B > 65535 || E > 65535 * SORT_SLICE || R > 0x7fffffff - SORT_BLK ? HFTA_EUNSUPPORTED : HFTA_OK;
+  return B > 65535 || E > 65535 * SORT_SLICE || R > 1 << 28 || V > 1 << 30 ? HFTA_EUNSUPPORTED : HFTA_OK;     // (a launch has fewer than 2^32 threads)
 }
 
 struct SortPlan {

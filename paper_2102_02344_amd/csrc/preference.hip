@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
 
 int pf_check(int B, int R, int K, int nseq, int dtype) {
   if (B <= 0 || R <= 0 || K <= 0 || nseq <= 0 || !valid_dtype(dtype)) return HFTA_EINVAL;
-  return B > 65535 || R == 0x7fffffff ? HFTA_EUNSUPPORTED : HFTA_OK;
+  return B > 65535 || R > 0xfffffe ? HFTA_EUNSUPPORTED : HFTA_OK;      // (a launch has fewer than 2^32 threads)
 }
 
 template <typename T>

@@ -118,6 +118,70 @@ def test_heads_and_layouts(hb, dtype, layout, Hq, Hkv, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [24, 64, 120])
+@pytest.mark.parametrize("causal", [1, 0])
+def test_many_heads(hb, dtype, d, causal):
+    """Enough tiles of 128 rows to fill the chip: a wavefront has 32 rows of its own and all keys."""
+    c = Case(dtype, 2, [[150, 0, 61, 90], [3, 299, 1, 0]], 96, 48, d, first=1, behind=4, seed=d)
+    c.fwd(hb, causal)
+    c.bwd(hb, causal)
+    torch.cuda.synchronize()
+    c.check(causal)
+
+
+@pytest.mark.parametrize("Hq", [2, 300])
+def test_more_sequences_than_threads(hb, Hq):
+    g = torch.Generator().manual_seed(6)
+    c = Case("bf16", 1, [torch.randint(0, 4, (700,), generator=g).tolist()], Hq, 2, 16, first=2, behind=3, seed=6)
+    c.fwd(hb, 1)
+    c.bwd(hb, 1)
+    torch.cuda.synchronize()
+    c.check(1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq", [4, 256])
+def test_inputs_of_stride_zero(hb, dtype, Hq):
+    """Keys and values shared by all heads, queries by all rows (expanded tensors): gradients come per head and row."""
+    c = Case(dtype, 2, [[90, 120], [200, 10]], Hq, Hq, 64, seed=8)
+    for n in ("k", "v"):
+        t = getattr(c, n)[:, :, :1].contiguous().expand(-1, -1, Hq, -1)
+        setattr(c, n, t)
+        setattr(c, n + "s", t.stride()[:3])
+    c.q = c.q[:, :1].contiguous().expand(-1, c.R, -1, -1)
+    c.qs = c.q.stride()[:3]
+    c.fwd(hb, 1)
+    c.bwd(hb, 1)
+    torch.cuda.synchronize()
+    c.check(1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_in_reverse(hb, dtype):
+    """Negative row strides."""
+    c = Case(dtype, 1, [[60, 75]], 2, 2, 32, seed=10)
+    for n in ("q", "k", "v", "dctx", "ctx", "dq", "dk", "dv"):
+        t = getattr(c, n)
+        flat = t.flip(1).contiguous()
+        s = flat.stride()
+
+        class Last:                                      # the last row in memory is the first
+            def __init__(self, x):
+                self.x = x
+
+            def data_ptr(self):
+                return self.x[:, -1].data_ptr()
+        setattr(c, n, Last(flat))
+        setattr(c, n + "s", (s[0], -s[1], s[2]))
+    c.fwd(hb, 1)
+    c.bwd(hb, 1)
+    torch.cuda.synchronize()
+    for n in ("q", "k", "v", "dctx", "ctx", "dq", "dk", "dv"):
+        setattr(c, n, getattr(c, n).x.flip(1))
+    c.check(1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_packed_projection_and_long_rows(hb, dtype):
     """Q, K, V and their gradients as blocks of one [R][q | k | v] tensor, sequences past several tiles of keys."""
     B, Hq, Hkv, d = 2, 4, 2, 64
@@ -153,10 +217,11 @@ def test_large_and_equal_scores(hb, dtype):
 @pytest.mark.parametrize("causal", [1, 0])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("what", ["v", "k", "dctx", "q"])
-def test_values_that_are_not_finite(hb, dtype, causal, value, what):
+@pytest.mark.parametrize("many", [0, 1])
+def test_values_that_are_not_finite(hb, many, dtype, causal, value, what):
     """One such value in one row: rows that do not see it keep their bits, outputs it takes part in are not finite."""
     lengths, at = [[20, 150, 40]], 20 + 101
-    a, b = (Case(dtype, 1, lengths, 2, 1, 64, first=4, behind=6, seed=21) for _ in range(2))
+    a, b = (Case(dtype, 1, lengths, *((300, 150) if many else (2, 1)), 64, first=4, behind=6, seed=21) for _ in range(2))
     at += 4
     getattr(b, what)[0, at, 0, 9] = value
     for c in (a, b):
@@ -177,9 +242,9 @@ def test_values_that_are_not_finite(hb, dtype, causal, value, what):
     ca, cb = a.ctx[0].float().cpu(), b.ctx[0].float().cpu()
     if what != "dctx":
         heads = slice(0, 2) if what in ("v", "k") else slice(0, 1)
-        assert torch.equal(ca[clean], cb[clean])
+        assert torch.equal(ca[clean], cb[clean]) and torch.equal(ca[:, 2:], cb[:, 2:])
         if what == "v":
-            assert not bool(torch.isfinite(cb[sees][:, :, 9]).any())
+            assert not bool(torch.isfinite(cb[sees][:, :2, 9]).any())
             other = [i for i in range(64) if i != 9]
             assert torch.equal(ca[:, :, other], cb[:, :, other])
         elif what == "q" or math.isnan(value):
@@ -190,17 +255,18 @@ def test_values_that_are_not_finite(hb, dtype, causal, value, what):
     seen = seq & ((row <= at) if causal else seq)              # keys that row `at` sees
     for n in ("dk", "dv"):
         x, y = getattr(a, n)[0].float().cpu(), getattr(b, n)[0].float().cpu()
-        assert torch.equal(x[~seen], y[~seen]), n
-        assert not bool(torch.isfinite(y[seen]).all(dim=(1, 2)).any()), n
+        assert torch.equal(x[~seen], y[~seen]) and torch.equal(x[:, 1:], y[:, 1:]), n
+        assert not bool(torch.isfinite(y[seen][:, 0]).all(dim=1).any()), n
     x, y = a.dq[0].float().cpu(), b.dq[0].float().cpu()
-    assert torch.equal(x[clean], y[clean]) and torch.equal(x[:, 1], y[:, 1])
+    assert torch.equal(x[clean], y[clean]) and torch.equal(x[:, 1:], y[:, 1:])
     assert not bool(torch.isfinite(y[at, 0]).any())
 
 
 @pytest.mark.parametrize("what", ["q", "k"])
-def test_gradients_of_rows_that_do_not_see_it(hb, what):
+@pytest.mark.parametrize("Hq", [2, 600])
+def test_gradients_of_rows_that_do_not_see_it(hb, what, Hq):
     """A NaN in a query or key: gradients of the sequences beside it, in the same tiles, keep their bits."""
-    a, b = (Case("bf16", 1, [[30, 50, 40]], 2, 2, 64, seed=23) for _ in range(2))
+    a, b = (Case("bf16", 1, [[30, 50, 40]], Hq, Hq, 64, seed=23) for _ in range(2))
     getattr(b, what)[0, 55, 1, 3] = math.nan
     for c in (a, b):
         c.fwd(hb, 1)

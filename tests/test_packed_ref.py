@@ -89,6 +89,7 @@ def test_attention_refusals(lib):
         assert fwd(**bad) == lib.EINVAL, bad
     assert fwd(d=129) == lib.EUNSUPPORTED
     assert fwd(B=2 ** 20, Hq=4096, R=2 ** 20) == lib.EUNSUPPORTED
+    assert fwd(B=1, Hq=1, Hkv=1, R=2 ** 31 - 200) == lib.EUNSUPPORTED
     assert fwd(d=129, Q=None) == lib.EINVAL
 
     need = raw.hfta_attention_packed_bwd_workspace_bytes(2, 64, 3, 4, 2, 16, 1)
@@ -116,7 +117,7 @@ def test_embedding_refusals(lib):
     for bad in (dict(B=0), dict(R=0), dict(V=0), dict(E=0), dict(nseq=0), dict(dt=3), dict(table=None), dict(idx=None), dict(off=None),
                 dict(out=None), dict(S=0)):
         assert fwd(**bad) == lib.EINVAL, bad
-    assert fwd(B=65536) == lib.EUNSUPPORTED
+    assert fwd(B=65536) == lib.EUNSUPPORTED and fwd(R=2 ** 28 + 1) == lib.EUNSUPPORTED and fwd(V=2 ** 30 + 1) == lib.EUNSUPPORTED
 
     need = raw.hfta_embedding_bwd_sorted_workspace_bytes(2, 64, 100, 24)
     assert need > 0 and raw.hfta_embedding_bwd_sorted_workspace_bytes(0, 64, 100, 24) == 0
@@ -137,7 +138,7 @@ def test_preference_refusals(lib):
     for bad in (dict(B=0), dict(R=0), dict(K=0), dict(nseq=0), dict(dt=2), dict(z=None), dict(y=None), dict(off=None), dict(tok=None),
                 dict(out=None)):
         assert lps(**bad) == lib.EINVAL, bad
-    assert lps(B=65536) == lib.EUNSUPPORTED
+    assert lps(B=65536) == lib.EUNSUPPORTED and lps(R=2 ** 24 - 1) == lib.EUNSUPPORTED
 
     need = raw.hfta_preference_loss_workspace_bytes(2, 64, 2)
     assert need > 0 and raw.hfta_preference_loss_workspace_bytes(2, 0, 2) == 0
