@@ -113,8 +113,10 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
       pk_f16 sn[1] = {pk_f16{}};
       pk_f16& s = sn[0];
       if (some) {
+        __builtin_amdgcn_s_setprio(1);
         pk_rows<T, D, 1>(sn, forms_v ? tq : tc, 0, x, lane);
         if constexpr (sizeof(T) == 2) pk_order<4, D / 16, 1>();
+        __builtin_amdgcn_s_setprio(0);
         if (forms_v) {
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
@@ -149,8 +151,10 @@ __global__ __launch_bounds__(256, (D * (int)sizeof(T) <= 128 ? 4 : D * (int)size
         __syncthreads();
       }
       if (some) {
+        __builtin_amdgcn_s_setprio(1);
         pk_cols<T, D>(o, forms_v ? tc : tq, 0, s, lane);
         if constexpr (sizeof(T) == 2) pk_order<4, D / 16, 2>();
+        __builtin_amdgcn_s_setprio(0);
       }
       if (!safe) buf ^= 1;
     }

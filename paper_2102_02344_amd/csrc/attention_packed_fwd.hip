@@ -66,8 +66,10 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
         float mt = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) s[kb] = pk_f16{};
+        __builtin_amdgcn_s_setprio(1);
         pk_rows<T, D, NB>(s, tk, 0, q, lane);
         if constexpr (sizeof(T) == 2) pk_order<4, NB * D / 16, 1>();
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) sp.mask(s[kb], k0 + kb * 32, g, -INFINITY);
 #pragma unroll
@@ -106,9 +108,11 @@ __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_fwd_ke
         pk_sync<SPLIT>();
       }
       if (some) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) pk_cols<T, D>(o, tv, kb * 32, s[kb], lane);
         if constexpr (sizeof(T) == 2) pk_order<4, NB * D / 16, 2>();
+        __builtin_amdgcn_s_setprio(0);
       }
       if (!SPLIT && !safe) buf ^= 1;
     }
