@@ -176,7 +176,8 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
                                                       float* __restrict__ loss, T* dlogits, int R, int K) {
   constexpr int EPP = PfRow<T>::EPP, NV = 4;
   __shared__ double sh[4];
-  const int r = blockIdx.x, b = blockIdx.y, t = threadIdx.x, nseq = 2 * pairs;
+  // the last rows first: what the pass before read last may still be in the last-level cache
+  const int r = R - (int)blockIdx.x, b = (int)(gridDim.y - 1 - blockIdx.y), t = threadIdx.x, nseq = 2 * pairs;
   if (r == R) {
     double v = 0;
     for (int i = t; i < pairs; i += 256) v += (double)term[(int64_t)b * pairs + i];
