@@ -370,3 +370,40 @@ def test_past_two_to_the_31_elements(hb):
     for n, x in (("ctx", ctx), ("dq", dq), ("dk", dk), ("dv", dv)):
         got = x[:, R - 90:].double().cpu()[:, :, None]
         assert bool(((got - ref[n]).abs() <= ref[n + "_b"]).all()), n
+
+
+@pytest.mark.parametrize("Hq", [2, 20])
+def test_thousands_of_sequences(hb, Hq):
+    """So many that their offsets are searched: short ones, long runs of empty ones around longer ones, and none at all."""
+    g = torch.Generator().manual_seed(40)
+    short = torch.randint(0, 2, (2400,), generator=g).tolist()
+    around = [0] * 1100 + [70] + [0] * 1298 + [200]
+    c = Case("bf16", 3, [short, around, [0] * 2400], Hq, 2, 16, first=1, behind=5, seed=40)
+    for causal in (1, 0):
+        c.fwd(hb, causal)
+        c.bwd(hb, causal)
+        torch.cuda.synchronize()
+        c.check(causal)
+    order = torch.randperm(2401, generator=g)                  # in any order: finite and inside
+    c.offd = c.off[:, order].contiguous().cuda()
+    c.fwd(hb, 1)
+    c.bwd(hb, 1)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("d", [40, 128])
+@pytest.mark.parametrize("lengths", [[[12] * 60], [[20] * 40], [[130, 150]], [[700]]], ids=["12", "20", "140", "700"])
+def test_bf16_errors_are_those_of_two_roundings(hb, lengths, d):
+    """An output in bf16 has one rounding; p or ds have one before the product, of the same size and independent, so that the mean error is
+    sqrt(2) of the rounded result's.  6 % more are for the rest: D, whose error stays in dq where sequences are long, and the sums."""
+    c = Case("bf16", 1, lengths, 4, 2, d, seed=d)
+    c.fwd(hb, 1)
+    c.bwd(hb, 1)
+    torch.cuda.synchronize()
+    ref, got = c.ref(1), c.outputs()
+    far, near = 0.0, 0.0
+    for n in ("dq", "dk", "dv"):
+        far += float((got[n].double().cpu() - ref[n]).square().sum())
+        near += float((ref[n].bfloat16().double() - ref[n]).square().sum())
+    print(f"  {math.sqrt(far / near):.3f} roundings", flush=True)
+    assert far <= 1.5 ** 2 * near
