@@ -9,7 +9,7 @@ int pk_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, float sc
       isinf(scale) || R > 0x7fffffff - 128)
     return HFTA_EINVAL;
   // (a launch has fewer than 2^32 threads; tiles are of at least 64 rows where there are many)
-  return d > 128 || (int64_t)B * Hq > 0xffffff / pk_tiles(R, 2 * PK_WT) ? HFTA_EUNSUPPORTED : HFTA_OK;
+  return d > 128 || nseq > PACKED_MAX || (int64_t)B * Hq > 0xffffff / pk_tiles(R, 2 * PK_WT) ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 // Workgroups that share the sums of 64 keys, so that there are about 2048 of them: eight per compute unit, enough to even out the
 // keys that many rows see with those that few do.  A part is at least 16 tiles of 32 rows on average, or two where the

@@ -484,7 +484,7 @@ int hfta_embedding_packed_fwd(int B, int R, int V, int E, int nseq, int dtype, c
                               const int32_t* seq_offsets, float scale, const float* pos, int S, void* out, void* stream) {
   const int rc = ep_check(B, R, V, E, dtype);
   if (rc == HFTA_EINVAL || nseq <= 0 || !table || !idx || !seq_offsets || !out || (pos && S <= 0)) return HFTA_EINVAL;
-  if (rc != HFTA_OK) return rc;
+  if (rc != HFTA_OK || nseq > PACKED_MAX) return HFTA_EUNSUPPORTED;
   const int epp = dtype == HFTA_BF16 ? 8 : 4;
   const bool vec = E % epp == 0 && ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
   const dim3 grid((unsigned)((R + EP_ROWS - 1) / EP_ROWS), (unsigned)B);
@@ -507,7 +507,7 @@ int hfta_embedding_bwd_sorted(int B, int R, int V, int E, int nseq, int dtype, c
                               void* stream) {
   const int rc = ep_check(B, R, V, E, dtype);
   if (rc == HFTA_EINVAL || (seq_offsets && nseq <= 0) || !dY || !idx || !dtable) return HFTA_EINVAL;
-  if (rc != HFTA_OK) return rc;
+  if (rc != HFTA_OK || (seq_offsets && nseq > PACKED_MAX)) return HFTA_EUNSUPPORTED;
   const SortPlan pl(B, R, V, E);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 || ws_bytes < pl.total) return HFTA_EWORKSPACE;
   unsigned char* w = (unsigned char*)workspace;

@@ -47,7 +47,8 @@ def tokens(kind, B, R, V, seed):
 @pytest.mark.parametrize("kind,B,R,V,E,nseq,first,behind", [
     ("uniform", 1, 1, 1, 1, 1, 0, 0), ("uniform", 2, 70, 9, 8, 3, 2, 5), ("outside", 2, 300, 256, 72, 7, 0, 1), ("runs", 2, 2485, 255, 40, 30, 1, 0),
     ("one", 1, 33, 5, 65, 2, 0, 0), ("one", 2, 5000, 70, 264, 3, 3, 9), ("padded", 2, 9000, 300, 256, 50, 0, 40), ("uniform", 1, 64, 65536, 12, 64, 0, 0),
-    ("uniform", 3, 4097, 70000, 4, 200, 0, 3), ("padded", 1, 20000, 1000, 1028, 90, 0, 0), ("uniform", 1, 100, 17, 2050, 100, 0, 0)])
+    ("uniform", 3, 4097, 70000, 4, 200, 0, 3), ("padded", 1, 20000, 1000, 1028, 90, 0, 0), ("uniform", 1, 100, 17, 2050, 100, 0, 0),
+    ("uniform", 2, 3000, 90, 16, 2500, 1, 2)])
 def test_rows_and_gradients(hb, dtype, kind, B, R, V, E, nseq, first, behind):
     print(kind, dtype, B, R, V, E, nseq, flush=True)
     g = torch.Generator().manual_seed(R + E)
