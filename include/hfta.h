@@ -684,11 +684,11 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
  * preference_loss: pairs of sequences (2p: preferred, 2p + 1: not), npairs per model, seq_offsets [B][2 npairs + 1].  With L_s as logps
  *   above, returned in logps [B][2 npairs], ref_logps [B][2 npairs] the same of a reference model, and t_p = beta[b] ((L_2p -
  *   ref_2p) - (L_2p+1 - ref_2p+1)):   loss[b] = mean over p of -(1 - eps) log sigma(t_p) - eps log sigma(-t_p),  eps =
- *   label_smoothing[b];   beta, label_smoothing: fp32 [B] (label_smoothing NULL: 0).  dlogits: the gradient, storage dtype, 0 in rows with a negative
+ *   label_smoothing[b] (a weight of zero takes no part);   beta, label_smoothing: fp32 [B] (label_smoothing NULL: 0).  dlogits: the gradient, storage dtype, 0 in rows with a negative
  *   label; it may be logits itself.  A label >= K makes its model's loss and its pair's gradient NaN.  Workspace
  *   hfta_preference_loss_workspace_bytes, 4-byte aligned (EWORKSPACE).
- * EUNSUPPORTED above 65535 models, 2^28 rows or 2^30 tokens of an embedding, 2^24 - 2 rows of logits (each of a model), and, attention, above
- * 2^24 - 1 tiles of 64 rows of one head in all.
+ * EUNSUPPORTED above 2^24 - 2 sequences, 2^28 rows or 2^30 tokens of an embedding, 2^24 - 2 rows of logits (each of a model), 65535 models
+ * (attention: 2^24 - 1 tiles of 64 rows of one head in all).
  * ---------------------------------------------------------------------- */
 int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
                               const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, float scale,

@@ -115,32 +115,46 @@ __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logi
   }
 }
 
-// a wavefront's sum over rows [lo, hi), in 64 bits
-__device__ __forceinline__ double pf_sum(const float* lp, int lo, int hi, int lane) {
+// a workgroup's sum over rows [lo, hi), in 64 bits: each thread eight rows at once, so that a sequence of many rows is no chain of
+// loads; sh: four words of LDS, one per wavefront
+__device__ __forceinline__ double pf_sum(const float* lp, int lo, int hi, double* sh) {
+  constexpr int NV = 8;
+  const int t = threadIdx.x;
   double v = 0;
-  for (int i = lo + lane; i < hi; i += 64) v += (double)lp[i];
+  for (int i = lo + t; i < hi; i += 256 * NV) {
+    float x[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) x[j] = i + 256 * j < hi ? lp[i + 256 * j] : 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v += (double)x[j];
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  if ((t & 63) == 0) sh[t >> 6] = v;
+  __syncthreads();
+  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
 __global__ __launch_bounds__(256) void pf_seq_kernel(const float* __restrict__ lp, const int32_t* __restrict__ off, int nseq,
                                                      float* __restrict__ logps, int R) {
-  const int b = blockIdx.y, lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (s >= nseq) return;
+  __shared__ double sh[4];
+  const int b = blockIdx.y, s = blockIdx.x;
   int lo, hi;
   pf_rows(off + (int64_t)b * (nseq + 1), s, R, lo, hi);
-  const double v = pf_sum(lp + (int64_t)b * R, lo, hi, lane);
-  if (lane == 0) logps[(int64_t)b * nseq + s] = (float)v;
+  const double v = pf_sum(lp + (int64_t)b * R, lo, hi, sh);
+  if (threadIdx.x == 0) logps[(int64_t)b * nseq + s] = (float)v;
 }
 
-// ------------------------------------------------------------------ pairs: a wavefront each
+// ------------------------------------------------------------------ pairs: a workgroup each
+// w x: a weight of zero takes no part, however large x is (a rejected text that the model rules out)
+__device__ __forceinline__ double pf_part(double w, double x) { return w == 0.0 ? 0.0 : w * x; }
+
 __global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ lp, const int32_t* __restrict__ off, int pairs, const float* __restrict__ ref,
                                                       const float* __restrict__ beta, const float* __restrict__ smoothing,
                                                       float* __restrict__ logps, float* __restrict__ term, float* __restrict__ coef,
                                                       int R) {
-  const int b = blockIdx.y, lane = threadIdx.x & 63, p = blockIdx.x * 4 + (threadIdx.x >> 6), nseq = 2 * pairs;
-  if (p >= pairs) return;
+  __shared__ double sh[2][4];
+  const int b = blockIdx.y, p = blockIdx.x, nseq = 2 * pairs;
   off += (int64_t)b * (nseq + 1);
   lp += (int64_t)b * R;
   int lo[2], hi[2];
@@ -148,7 +162,7 @@ __global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ 
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     pf_rows(off, 2 * p + i, R, lo[i], hi[i]);
-    v[i] = pf_sum(lp, lo[i], hi[i], lane);
+    v[i] = pf_sum(lp, lo[i], hi[i], sh[i]);
   }
   const int64_t at = (int64_t)b * nseq + 2 * p;
   const double be = beta[b], eps = smoothing ? smoothing[b] : 0.f;
@@ -156,14 +170,14 @@ __global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ 
   const double e = exp(-fabs(t)), tail = log1p(e);                  // softplus(x) = max(x, 0) + log1p(exp(-|x|))
   const double up = (t >= 0 ? 1.0 : e) / (1.0 + e), down = (t >= 0 ? e : 1.0) / (1.0 + e);      // sigma(t), sigma(-t)
   const float c = (float)(-be * ((1.0 - eps) * down - eps * up) / pairs);
-  if (lane == 0) {
+  if (threadIdx.x == 0) {
     logps[at] = (float)v[0];
     logps[at + 1] = (float)v[1];
-    term[(int64_t)b * pairs + p] = (float)((1.0 - eps) * (fmax(-t, 0.0) + tail) + eps * (fmax(t, 0.0) + tail));
+    term[(int64_t)b * pairs + p] = (float)(pf_part(1.0 - eps, fmax(-t, 0.0) + tail) + pf_part(eps, fmax(t, 0.0) + tail));
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    for (int r = lo[i] + lane; r < hi[i]; r += 64)
+    for (int r = lo[i] + (int)threadIdx.x; r < hi[i]; r += 256)
       coef[(int64_t)b * R + r] = i ? -c : c;
 }
 
@@ -232,7 +246,7 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
 
 int pf_check(int B, int R, int K, int nseq, int dtype) {
   if (B <= 0 || R <= 0 || K <= 0 || nseq <= 0 || !valid_dtype(dtype)) return HFTA_EINVAL;
-  return B > 65535 || R > 0xfffffe ? HFTA_EUNSUPPORTED : HFTA_OK;      // (a launch has fewer than 2^32 threads)
+  return B > 65535 || R > 0xfffffe || nseq > PACKED_MAX ? HFTA_EUNSUPPORTED : HFTA_OK;      // (a launch has fewer than 2^32 threads)
 }
 
 template <typename T>
@@ -258,21 +272,21 @@ int hfta_seq_logps(int B, int R, int K, int nseq, int dtype, const void* logits,
   if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
   else pf_rows_launch<float>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
-  hipLaunchKernelGGL(pf_seq_kernel, dim3((unsigned)((nseq + 3) / 4), (unsigned)B), dim3(256), 0, st, token_logps, seq_offsets, nseq,
+  hipLaunchKernelGGL(pf_seq_kernel, dim3((unsigned)nseq, (unsigned)B), dim3(256), 0, st, token_logps, seq_offsets, nseq,
                      logps, R);
   return launch_status();
 }
 
 size_t hfta_preference_loss_workspace_bytes(int B, int R, int npairs) {
-  if (B <= 0 || R <= 0 || npairs <= 0 || npairs > 0x3fffffff) return 0;
+  if (B <= 0 || R <= 0 || npairs <= 0 || npairs > PACKED_MAX / 2) return 0;
   return ((size_t)B * R * 3 + (size_t)B * npairs) * sizeof(float);     // lse, label terms and factors of the rows; pair terms
 }
 
 int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void* logits, const int32_t* labels,
                          const int32_t* seq_offsets, const float* ref_logps, const float* beta, const float* label_smoothing,
                          float* loss, float* logps, void* dlogits, void* workspace, size_t ws_bytes, void* stream) {
-  const int rc = pf_check(B, R, K, npairs, dtype);
-  if (rc == HFTA_EINVAL || npairs > 0x3fffffff || !logits || !labels || !seq_offsets || !ref_logps || !beta || !loss || !logps || !dlogits)
+  const int rc = pf_check(B, R, K, npairs > PACKED_MAX / 2 ? 0x7fffffff : npairs, dtype);
+  if (rc == HFTA_EINVAL || !logits || !labels || !seq_offsets || !ref_logps || !beta || !loss || !logps || !dlogits)
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 4 || ws_bytes < hfta_preference_loss_workspace_bytes(B, R, npairs))
@@ -283,7 +297,7 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
   if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
   else pf_rows_launch<float>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
-  hipLaunchKernelGGL(pf_pair_kernel, dim3((unsigned)((npairs + 3) / 4), (unsigned)B), dim3(256), 0, st, lp, seq_offsets,
+  hipLaunchKernelGGL(pf_pair_kernel, dim3((unsigned)npairs, (unsigned)B), dim3(256), 0, st, lp, seq_offsets,
                      npairs, ref_logps, beta, label_smoothing, logps, term, coef, R);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
   const dim3 grid((unsigned)R + 1u, (unsigned)B);

@@ -206,3 +206,36 @@ def test_past_two_to_the_31_elements(hb):
     got = z[0, R - 20:].double().cpu()[None]
     assert bool(((got - g).abs() <= (2.0 ** -8 + 30 * rb) * g.abs() + 1e-30).all())
     assert not bool(z[0, R - 22:R - 20].any())                  # rows in front of the first sequence: as they were
+
+
+def test_texts_that_cannot_be(hb):
+    """A label whose logit is -inf: as a rejected text it costs nothing and leaves no gradient, smoothed or preferred it costs an infinity,
+    with the factor of the gradient at its limit."""
+    for side, eps, want in ((1, 0.0, 0.0), (1, 0.25, math.inf), (0, 0.0, math.inf), (0, 1.0, 0.0)):
+        c = Case("f32", [[3, 4]], 40, seed=11, prompts=False)
+        c.ref = torch.zeros(1, 2)
+        c.eps[:] = eps
+        row = 3 * side + 1
+        rb = float(c.row_bound().max()) * 2 + 4 * U                  # of a probability, relative
+        c.z[0, row, int(c.y[0, row])] = -math.inf
+        loss, logps, d = c.loss(hb)
+        assert float(loss[0]) == want and float(logps[0, side]) == -math.inf and math.isfinite(logps[0, 1 - side])
+        f = float(c.beta[0]) * (eps if side else eps - 1)            # sigma(t) is 1 where the rejected text cannot be, or else 0
+        p = torch.softmax(c.z.double(), -1)
+        one = torch.zeros_like(p).scatter_(2, c.y.long()[..., None], 1.0)
+        g = f * (one - p) * torch.tensor([1.0] * 3 + [-1.0] * 4)[:, None]
+        assert float((d.double() - g).abs().max()) <= rb * abs(f) and (f != 0 or bool((d == 0).all()))
+
+
+@pytest.mark.parametrize("lengths", [[[9000, 20011], [20011, 9000]], [[2047, 2049], [1, 2048]]], ids=["long", "steps"])
+def test_sums_of_long_sequences(hb, lengths):
+    c = Case("f32", lengths, 7, behind=2, seed=12)
+    loss, logps, _ = c.loss(hb)
+    want, L = pr.preference(c.z.double(), c.y, c.off, c.ref.double(), c.beta.double(), c.eps.double())
+    Lb = pr.seq_sums(torch.where(c.y >= 0, c.row_bound(), 0.0), c.off)
+    assert bool(((logps.double() - L).abs() <= Lb + U * L.abs()).all())
+    assert bool(((loss.double() - want).abs() <= (c.beta.double()[:, None] * Lb).sum(1) + 4 * U * want.abs()).all())
+    tok, out = torch.empty(c.B, c.R, device="cuda"), torch.empty(c.B, c.nseq, device="cuda")
+    hb.seq_logps(c.B, c.R, c.K, c.nseq, DT["f32"], c.z.cuda(), c.y.cuda(), c.off.cuda(), tok, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), logps)

@@ -153,3 +153,15 @@ def test_preference_refusals(lib):
         assert loss(**bad) == lib.EINVAL, bad
     assert loss(B=65536) == lib.EUNSUPPORTED
     assert loss(ws=None) == lib.EWORKSPACE and loss(nws=need - 1) == lib.EWORKSPACE and loss(ws=C.c_void_p(257)) == lib.EWORKSPACE
+
+
+def test_too_many_sequences(lib):
+    raw, many = lib.raw(), 2 ** 24 - 1
+    assert raw.hfta_attention_packed_fwd(2, 64, many, 4, 2, 16, 1, ONE, S3, ONE, ONE, S3, ONE, 0.25, 1, ONE, S3, ONE, None) == lib.EUNSUPPORTED
+    assert raw.hfta_attention_packed_bwd_workspace_bytes(2, 64, many, 4, 2, 16, 1) == 0
+    assert raw.hfta_embedding_packed_fwd(2, 64, 100, 24, many, 1, ONE, ONE, ONE, 1.0, None, 0, ONE, None) == lib.EUNSUPPORTED
+    assert raw.hfta_embedding_bwd_sorted(2, 64, 100, 24, many, 1, ONE, ONE, ONE, 1.0, ONE, ONE, 1 << 30, None) == lib.EUNSUPPORTED
+    assert raw.hfta_seq_logps(2, 64, 100, many, 1, ONE, ONE, ONE, ONE, ONE, None) == lib.EUNSUPPORTED
+    for pairs in (2 ** 23, 2 ** 31 - 1):
+        assert raw.hfta_preference_loss(2, 64, 100, pairs, 1, ONE, ONE, ONE, ONE, ONE, ONE, ONE, ONE, ONE, ONE, 1 << 40, None) == lib.EUNSUPPORTED
+        assert raw.hfta_preference_loss_workspace_bytes(2, 64, pairs) == 0
