@@ -62,6 +62,7 @@ struct PkArgs {
   float *LSE, *Dsum, *part;        // Dsum, part: the backward's workspace
   PkStr qs, ks, cs, dqs, dks;
   int B, R, nseq, Hq, Hkv, d, causal, parts;       // parts: workgroups that share the sums of a tile of keys
+  int twice;                       // sequences are short: the queries' backward sums D's rest first
   PkDiv by_heads, by_hkv, by_group, by_parts;      // B Hkv, Hkv, Hq / Hkv, parts
   float scale;
 };

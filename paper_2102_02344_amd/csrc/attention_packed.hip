@@ -30,6 +30,7 @@ void pk_places(PkArgs& a) {
   a.by_group = PkDiv((uint32_t)(a.Hq / a.Hkv));
   a.by_parts = PkDiv((uint32_t)a.parts);
 }
+constexpr int PK_SHORT = 128;      // rows of a sequence on average up to which D is made exact for dq too: more of D's error than of others
 PkStr pk_str(const int64_t* s) { return s ? PkStr{s[0], s[1], s[2]} : PkStr{0, 0, 0}; }
 
 // vec: rows in whole 16-byte pieces -- pointers, strides and head widths.  split: tiles of 128 rows would be fewer than two
@@ -92,6 +93,7 @@ int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.dQ = dQ; a.dK = dK; a.dV = dV; a.Dsum = reinterpret_cast<float*>(workspace);
   a.part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + pk_sums(B, R, Hq));
   a.parts = pk_parts(B, R, nseq, Hq, Hkv);
+  a.twice = R / nseq <= PK_SHORT;
   a.qs = pk_str(qs); a.ks = pk_str(kvs); a.cs = pk_str(cs); a.dqs = pk_str(dqs); a.dks = pk_str(dkvs);
   a.B = B; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.causal = causal != 0; a.scale = scale;
   pk_places(a);

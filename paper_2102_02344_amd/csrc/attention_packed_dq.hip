@@ -5,16 +5,15 @@
 namespace hfta {
 namespace {
 
-constexpr int PK_SHORT = 128;                                    // rows of a sequence on average, MEAN up to here
-
 // p and ds are rounded to bf16 before their products, which leaves the gradients sqrt(2) of the error that rounding the results has by
 // itself.  D from the stored ctx would add as much again as ctx's rounding is large against D, most where sequences are short.  What it
-// lacks is in the sums anyway: with ds formed from D0, delta_i = sum_j ds_ij = D_i - D0_i.  The kernel of the keys gets D0 + delta; here
-// dq_i lacks -delta_i sum_j p_ij k_j, whose sum is one product more (MEAN).  Mean error of the three gradients in roundings of the results, 12
-// to 48 rows a sequence: 1.44 to 1.56 with neither, 1.40 to 1.51 without MEAN, 1.34 to 1.44 with it; 140 to 1000 rows: 1.41 to 1.46 without it.
-template <typename T, int D, bool VEC, bool SPLIT, bool MEAN>
-__global__ __launch_bounds__(256, (D * sizeof(T) * (MEAN ? 2 : 1) <= 256 ? 2 : 1)) void pk_dq_kernel(PkArgs a) {
-  constexpr bool FIX = sizeof(T) == 2;
+// lacks is in the sums anyway: with ds formed from D0, delta_i = sum_j ds_ij = D_i - D0_i.  The kernel of the keys gets D0 + delta.  Here
+// dq_i lacks -delta_i sum_j p_ij k_j; where sequences are short (a.twice) delta is summed first, in a pass of its own that leaves
+// out the product over keys.  Mean error of the three gradients in roundings of the results, 12 to 48 rows a sequence: 1.44 to 1.56 with
+// neither, 1.40 to 1.51 with delta for the keys alone, 1.34 to 1.44 with both; 140 to 1000 rows: 1.41 to 1.46 with the first.
+template <typename T, int D, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void pk_dq_kernel(PkArgs a) {
+  constexpr bool FIX = sizeof(T) == 2;                           // (fp32 needs none of it)
   typedef PkStage<T, D, VEC, SPLIT> Stage;
   constexpr int NB = SPLIT ? 1 : 2, BM = pk_bm<SPLIT>();         // key blocks per tile, rows of the workgroup
   constexpr int NBUF = SPLIT ? 4 : 2;                            // tiles: a wavefront's, or in turn
@@ -49,14 +48,12 @@ __global__ __launch_bounds__(256, (D * sizeof(T) * (MEAN ? 2 : 1) <= 256 ? 2 : 1
   const float c = a.scale * PK_LOG2E;
   const int first = sp.glo + (SPLIT ? wave * 32 : 0);
   constexpr int STEP = SPLIT ? 128 : 64;
-  pk_f16 o[D / 32], mean[MEAN ? D / 32 : 1];
+  pk_f16 o[D / 32];
   float delta;
-  for (bool safe = false;; safe = true) {
+  for (int pass = FIX && a.twice ? 0 : 1;; ++pass) {
+    const bool sums = FIX && pass == 0, safe = pass == 2;        // delta alone; values that are not finite
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) o[n] = pk_f16{};
-    if constexpr (MEAN)
-#pragma unroll
-      for (int n = 0; n < D / 32; ++n) mean[n] = pk_f16{};
     delta = 0.f;
     int buf = SPLIT ? wave : 0;
     Stage nk, nv;
@@ -89,19 +86,14 @@ __global__ __launch_bounds__(256, (D * sizeof(T) * (MEAN ? 2 : 1) <= 256 ? 2 : 1
       for (int kb = 0; kb < NB; ++kb) {
         const int j0 = k0 + kb * 32;
         const bool some = !sp.none(j0, 32);
-        pk_f16 s[1] = {pk_f16{}}, w = {};
+        pk_f16 s[1] = {pk_f16{}};
         if (some) {
           pk_f16 p[1] = {pk_f16{}};
           pk_rows<T, D, 1>(s, tk, kb * 32, q, lane);
           pk_rows<T, D, 1>(p, tv, kb * 32, dc, lane);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float e = pk_exp2(fmaf(c, s[0][i], -lse));
-            if constexpr (MEAN) w[i] = e;
-            s[0][i] = e * (p[0][i] - dsum);
-          }
+          for (int i = 0; i < 16; ++i) s[0][i] = pk_exp2(fmaf(c, s[0][i], -lse)) * (p[0][i] - dsum);
           sp.mask(s[0], j0, g, 0.f);
-          if constexpr (MEAN) sp.mask(w, j0, g, 0.f);
           if constexpr (FIX)
 #pragma unroll
             for (int i = 0; i < 16; ++i) delta += s[0][i];
@@ -112,28 +104,26 @@ __global__ __launch_bounds__(256, (D * sizeof(T) * (MEAN ? 2 : 1) <= 256 ? 2 : 1
           Stage::clean(tk + kb * 32 * PkTile<T, D>::ROW, 32);
           pk_sync<SPLIT>();
         }
-        if (some) pk_cols<T, D>(o, tk, kb * 32, s[0], lane);
-        if constexpr (MEAN)
-          if (some) pk_cols<T, D>(mean, tk, kb * 32, w, lane);
+        if (some && !sums) pk_cols<T, D>(o, tk, kb * 32, s[0], lane);
       }
       if (!SPLIT && !safe) buf ^= 1;
     }
-    if (safe || !__syncthreads_or(sp.in && (pk_not_finite(o) || (MEAN && pk_not_finite(mean))))) break;
-  }
-  if constexpr (FIX) {
-    delta += __shfl_xor(delta, 32, 64);
-    if constexpr (SPLIT) {
-      if (g == 0) jd[wave][lane] = delta;
-      __syncthreads();
-      delta = (jd[0][lane & 31] + jd[1][lane & 31]) + (jd[2][lane & 31] + jd[3][lane & 31]);
+    if constexpr (FIX) {                                         // (a second time: what the sums still lack)
+      delta += __shfl_xor(delta, 32, 64);
+      if constexpr (SPLIT) {
+        if (g == 0) jd[wave][lane] = delta;
+        __syncthreads();
+        delta = (jd[0][lane & 31] + jd[1][lane & 31]) + (jd[2][lane & 31] + jd[3][lane & 31]);
+      }
+      if (sums) {
+        dsum += delta;
+        __syncthreads();
+        continue;
+      }
     }
-    dsum += delta;
-    if constexpr (MEAN)
-#pragma unroll
-      for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[n][i] = fmaf(-delta, mean[n][i], o[n][i]);
+    if (safe || !__syncthreads_or(sp.in && pk_not_finite(o))) break;
   }
+  if constexpr (FIX) dsum += delta;
   if (sp.in && g == 0 && (!SPLIT || wave == 0)) a.Dsum[srow] = dsum;
   if constexpr (SPLIT) {
     pk_join<D>(o, reinterpret_cast<float*>(tiles), wave, lane);
@@ -150,17 +140,12 @@ __global__ __launch_bounds__(256, (D * sizeof(T) * (MEAN ? 2 : 1) <= 256 ? 2 : 1
   }
 }
 
-template <typename T, int D, bool MEAN> int launch_as(const PkArgs& a, const PkForm& f, hipStream_t st) {
-  const dim3 grid((unsigned)(pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq)), block(256);
-  if (f.split) hipLaunchKernelGGL((pk_dq_kernel<T, D, true, true, MEAN>), grid, block, 0, st, a);
-  else if (f.vec) hipLaunchKernelGGL((pk_dq_kernel<T, D, true, false, MEAN>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((pk_dq_kernel<T, D, false, false, MEAN>), grid, block, 0, st, a);
-  return launch_status();
-}
 template <typename T, int D> int launch(const PkArgs& a, const PkForm& f, hipStream_t st) {
-  if constexpr (sizeof(T) == 2)
-    if (a.R / a.nseq <= PK_SHORT) return launch_as<T, D, true>(a, f, st);
-  return launch_as<T, D, false>(a, f, st);
+  const dim3 grid((unsigned)(pk_tiles(a.R, f.split ? PK_WT : 4 * PK_WT) * a.B * a.Hq)), block(256);
+  if (f.split) hipLaunchKernelGGL((pk_dq_kernel<T, D, true, true>), grid, block, 0, st, a);
+  else if (f.vec) hipLaunchKernelGGL((pk_dq_kernel<T, D, true, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((pk_dq_kernel<T, D, false, false>), grid, block, 0, st, a);
+  return launch_status();
 }
 
 }  // namespace
