@@ -12,15 +12,20 @@ int pk_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, float sc
   return d > 128 || nseq > PACKED_MAX || (int64_t)B * Hq > 0xffffff / pk_tiles(R, 2 * PK_WT) ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 // Workgroups that share the sums of 64 keys, so that there are about 2048 of them: eight per compute unit, enough to even out the
-// keys that many rows see with those that few do.  A part is at least 16 tiles of 32 rows on average, or two where the
-// tiles of keys alone are fewer than two workgroups per compute unit.  2 x 8192 rows, 3 sequences, 8 heads of 128 over 2: 886 us, with
-// 4 parts 381 and 25 for adding them; 3 x 777 rows, 5 sequences, 6 fp32 heads of 48 over 2: 141, with 7 parts 39 in all; 8 x 2048 rows, 12
-// sequences, 4 heads of 64: 27 us, with 2 parts 31 and 13.
-int pk_parts(int B, int R, int nseq, int Hq, int Hkv) {
-  const int64_t base = (int64_t)pk_tiles(R, 2 * PK_WT) * B * Hkv, tiles = (int64_t)(R / nseq) * (Hq / Hkv) / 32;
+// keys that many rows see with those that few do.  A part is at least eight tiles of 32 rows on average, since adding the parts is a launch
+// that reads and writes them: 2 x 8192 rows, 3 sequences, 8 heads of 128 over 2: 886 us, with 4 parts 366 and 28 for adding them; 2 x 6442
+// rows, 15 sequences, 6 heads of 64 over 3: 70, with 3 parts 45 and 11; 8 x 2048 rows, 12 sequences, 4 heads of 64: 26, with 2 parts 31 and
+// 13; 4 x 3591 rows, 133 sequences, 8 heads of 128 over 2: 42, with 4 parts 50 and 22.  Where tiles of keys are fewer than compute units
+// a part is two tiles, or one in fp32, whose products take four times as long: 3 x 777 rows, 5 sequences, 6 fp32 heads of 48 over
+// 2: 141, with 8 parts 27 and 6; 3 x 201 rows, 8 sequences, 2 fp32 heads of 96 over 1: 48, with 5 parts 18 and 7; 2883 rows, 55 sequences, 4
+// heads of 40 over 2: 25, with 4 parts 14 and 5.
+int pk_parts(int B, int R, int nseq, int Hq, int Hkv, int dtype) {
+  const int64_t base = (int64_t)pk_tiles(R, 2 * PK_WT) * B * Hkv;
+  const int64_t rows = R / nseq + 2 * PK_WT < R ? R / nseq + 2 * PK_WT : R, tiles = rows * (Hq / Hkv) / PK_WT;
+  const int64_t least = base >= 256 ? 8 : dtype == HFTA_BF16 ? 2 : 1;
   int64_t p = 2048 / base;
   if (p > PK_PARTS_MAX) p = PK_PARTS_MAX;
-  if (p > tiles / (base < 512 ? 2 : 16)) p = tiles / (base < 512 ? 2 : 16);
+  if (p > tiles / least) p = tiles / least;
   return p < 1 ? 1 : (int)p;
 }
 size_t pk_sums(int B, int R, int Hq) { return ((size_t)B * Hq * R * sizeof(float) + 255) / 256 * 256; }     // bytes of D
@@ -71,7 +76,7 @@ int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
 
 size_t hfta_attention_packed_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   if (pk_check(B, R, nseq, Hq, Hkv, d, dtype, 1.f) != HFTA_OK) return 0;
-  const int parts = pk_parts(B, R, nseq, Hq, Hkv);
+  const int parts = pk_parts(B, R, nseq, Hq, Hkv, dtype);
   return pk_sums(B, R, Hq) + (parts > 1 ? (size_t)parts * 2 * B * R * Hkv * d * sizeof(float) : 0);
 }
 
@@ -92,7 +97,7 @@ int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.Q = Q; a.K = K; a.V = V; a.dCTX = dCTX; a.off = seq_offsets; a.CTX = const_cast<void*>(CTX); a.LSE = const_cast<float*>(LSE);
   a.dQ = dQ; a.dK = dK; a.dV = dV; a.Dsum = reinterpret_cast<float*>(workspace);
   a.part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + pk_sums(B, R, Hq));
-  a.parts = pk_parts(B, R, nseq, Hq, Hkv);
+  a.parts = pk_parts(B, R, nseq, Hq, Hkv, dtype);
   a.twice = R / nseq <= PK_SHORT;
   a.qs = pk_str(qs); a.ks = pk_str(kvs); a.cs = pk_str(cs); a.dqs = pk_str(dqs); a.dks = pk_str(dkvs);
   a.B = B; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.causal = causal != 0; a.scale = scale;
