@@ -15,11 +15,11 @@ namespace {
 
 // ------------------------------------------------------------------ lookup
 constexpr int EP_ROWS = 32;
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool POS>
 __global__ __launch_bounds__(256) void ep_fwd_kernel(const T* __restrict__ table, const int32_t* __restrict__ idx,
                                                      const int32_t* __restrict__ off, int nseq, const float* __restrict__ pos,
                                                      T* __restrict__ out, int R, int V, int E, int S, float scale) {
-  constexpr int EPP = VEC ? 16 / (int)sizeof(T) : 1;
+  constexpr int EPP = VEC ? 16 / (int)sizeof(T) : 1, EP_FLY = VEC ? 2 : 8;      // pieces of a thread in flight
   __shared__ PackedRows<EP_ROWS> pr;
   __shared__ int tok[EP_ROWS], place[EP_ROWS];
   const int b = blockIdx.y, t = threadIdx.x, t0 = blockIdx.x * EP_ROWS;
@@ -28,35 +28,47 @@ __global__ __launch_bounds__(256) void ep_fwd_kernel(const T* __restrict__ table
     int lo, hi;
     const bool in = pr.range(t0, t, lo, hi);
     tok[t] = in ? min(max(idx[(int64_t)b * R + t0 + t], 0), V - 1) : -1;
-    place[t] = min(t0 + t - lo, S - 1);
+    place[t] = in ? min(t0 + t - lo, S - 1) : 0;
   }
   __syncthreads();
   const int ppr = E / EPP, rows = min(EP_ROWS, R - t0), dr = 256 / ppr, dc = 256 - dr * ppr;
   int r = t / ppr, c = t - r * ppr;
+  union Piece { uint4 u; T e[VEC ? EPP : 16 / (int)sizeof(T)]; };
   while (r < rows) {
-    if (tok[r] >= 0) {
-      const T* src = table + ((int64_t)b * V + tok[r]) * E + c * EPP;
-      T* dst = out + ((int64_t)b * R + t0 + r) * E + c * EPP;
-      const float* pp = pos ? pos + (int64_t)place[r] * E + c * EPP : nullptr;
+    Piece x[EP_FLY];
+    float p[EP_FLY][EPP];
+    int at[EP_FLY], col[EP_FLY];
+#pragma unroll
+    for (int j = 0; j < EP_FLY; ++j) {
+      const int rj = min(r, rows - 1), v = tok[rj];
+      at[j] = r < rows && v >= 0 ? r : -1;
+      col[j] = c * EPP;
+      const T* src = table + ((int64_t)b * V + max(v, 0)) * E + col[j];      // (loads without a branch: all in flight)
+      const float* pp = pos + (int64_t)place[rj] * E + col[j];
       if constexpr (VEC) {
-        union { uint4 u; T e[EPP]; } x;
-        x.u = *reinterpret_cast<const uint4*>(src);
-        float p[EPP];
+        x[j].u = *reinterpret_cast<const uint4*>(src);
 #pragma unroll
         for (int q = 0; q < EPP / 4; ++q) {
-          const float4 v = pp ? *reinterpret_cast<const float4*>(pp + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
-          p[4 * q] = v.x; p[4 * q + 1] = v.y; p[4 * q + 2] = v.z; p[4 * q + 3] = v.w;
+          const float4 v = POS ? *reinterpret_cast<const float4*>(pp + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
+          p[j][4 * q] = v.x; p[j][4 * q + 1] = v.y; p[j][4 * q + 2] = v.z; p[j][4 * q + 3] = v.w;
         }
-#pragma unroll
-        for (int e = 0; e < EPP; ++e) x.e[e] = Elem<T>::from_f32(fmaf(scale, Elem<T>::to_f32(x.e[e]), p[e]));
-        *reinterpret_cast<uint4*>(dst) = x.u;
       } else {
-        Elem<T>::store(dst, fmaf(scale, Elem<T>::load(src), pp ? *pp : 0.f));
+        x[j].e[0] = *src;
+        p[j][0] = POS ? *pp : 0.f;
       }
+      r += dr;
+      c += dc;
+      if (c >= ppr) { c -= ppr; ++r; }
     }
-    r += dr;
-    c += dc;
-    if (c >= ppr) { c -= ppr; ++r; }
+#pragma unroll
+    for (int j = 0; j < EP_FLY; ++j) {
+      if (at[j] < 0) continue;
+#pragma unroll
+      for (int e = 0; e < EPP; ++e) x[j].e[e] = Elem<T>::from_f32(fmaf(scale, Elem<T>::to_f32(x[j].e[e]), p[j][e]));
+      T* dst = out + ((int64_t)b * R + t0 + at[j]) * E + col[j];
+      if constexpr (VEC) *reinterpret_cast<uint4*>(dst) = x[j].u;
+      else *dst = x[j].e[0];
+    }
   }
 }
 
@@ -283,7 +295,9 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(SortIn in, uint2* __rest
 }
 
 // ------------------------------------------------------------------ sums of the sorted rows
-// four columns of a row
+// four columns of a row from c on: in pieces c .. c + 3, else c, c + 64, .., so that a wavefront's lanes read next to each other
+// (sums of 5 x 2888 rows of 665 bf16 columns: 23 us, with four side by side 34)
+template <bool VEC> __device__ __forceinline__ int ep_col(int slice, int lane) { return slice * SORT_SLICE + (VEC ? 4 * lane : lane); }
 template <typename T, bool VEC> struct EpCols {
   union { T e[4]; uint2 h; uint4 w; };
   __device__ __forceinline__ void load(const T* row, int c, int E) {
@@ -292,7 +306,7 @@ template <typename T, bool VEC> struct EpCols {
       else w = *reinterpret_cast<const uint4*>(row + c);
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) e[k] = row[min(c + k, E - 1)];
+      for (int k = 0; k < 4; ++k) e[k] = row[min(c + 64 * k, E - 1)];
     }
   }
 };
@@ -302,7 +316,7 @@ template <bool VEC> __device__ __forceinline__ void ep_store(float* dst, int c, 
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (c + k < E) dst[c + k] = f * x[k];
+      if (c + 64 * k < E) dst[c + 64 * k] = f * x[k];
   }
 }
 
@@ -329,11 +343,11 @@ __global__ __launch_bounds__(256) void ep_sum_kernel(const T* __restrict__ dY, c
     const float zero[4] = {};
     for (; none; none &= none - 1) {
       float* row = dtable + ((int64_t)b * V + v0 + __builtin_ctzll(none)) * E;
-      for (int c = 4 * lane; c < E; c += SORT_SLICE) ep_store<VEC>(row, c, E, zero, 1.f);
+      for (int c = ep_col<VEC>(0, lane); c < E; c += SORT_SLICE) ep_store<VEC>(row, c, E, zero, 1.f);
     }
     return;
   }
-  const int ch = blockIdx.x * (4 / beside) + wave / beside, c = (blockIdx.z * beside + wave % beside) * SORT_SLICE + 4 * lane;
+  const int ch = blockIdx.x * (4 / beside) + wave / beside, c = ep_col<VEC>(blockIdx.z * beside + wave % beside, lane);
   if (ch >= chunks) return;
   const int lo = ch * SORT_CH, n = min(SORT_CH, R - lo);
   const uint2* s = sorted + (int64_t)b * R;
@@ -397,7 +411,7 @@ __global__ __launch_bounds__(256) void ep_join_kernel(const uint2* __restrict__ 
                                                       float* __restrict__ dtable, int R, int V, int E, int chunks, float scale) {
   constexpr int FLY = 8;
   __shared__ float sh[4][SORT_SLICE];
-  const int b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.z * SORT_SLICE + 4 * lane;
+  const int b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = ep_col<VEC>(blockIdx.z, lane);
   const uint2* s = sorted + (int64_t)b * R;
   const bool mine = c < E;
   const float* pt = part + (int64_t)b * chunks * 2 * E;
@@ -490,10 +504,16 @@ int hfta_embedding_packed_fwd(int B, int R, int V, int E, int nseq, int dtype, c
   const dim3 grid((unsigned)((R + EP_ROWS - 1) / EP_ROWS), (unsigned)B);
   hipStream_t st = as_stream(stream);
   if (!pos) S = 1;
-#define EP_FWD(T, VEC) hipLaunchKernelGGL((ep_fwd_kernel<T, VEC>), grid, dim3(256), 0, st, (const T*)table, idx, seq_offsets, nseq, pos, \
-                                          (T*)out, R, V, E, S, scale)
-  if (dtype == HFTA_BF16) { if (vec) EP_FWD(bf16_raw, true); else EP_FWD(bf16_raw, false); }
-  else { if (vec) EP_FWD(float, true); else EP_FWD(float, false); }
+#define EP_FWD(T, VEC, POS) hipLaunchKernelGGL((ep_fwd_kernel<T, VEC, POS>), grid, dim3(256), 0, st, (const T*)table, idx, seq_offsets, nseq, pos, \
+                                               (T*)out, R, V, E, S, scale)
+#define EP_FWD_AS(T)                                                                                \
+  do {                                                                                              \
+    if (vec) { if (pos) EP_FWD(T, true, true); else EP_FWD(T, true, false); }                       \
+    else { if (pos) EP_FWD(T, false, true); else EP_FWD(T, false, false); }                         \
+  } while (0)
+  if (dtype == HFTA_BF16) EP_FWD_AS(bf16_raw);
+  else EP_FWD_AS(float);
+#undef EP_FWD_AS
 #undef EP_FWD
   return launch_status();
 }
