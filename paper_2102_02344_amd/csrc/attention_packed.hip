@@ -38,17 +38,29 @@ void pk_places(PkArgs& a) {
 constexpr int PK_SHORT = 128;      // rows of a sequence on average up to which D is made exact for dq too: more of D's error than of others
 PkStr pk_str(const int64_t* s) { return s ? PkStr{s[0], s[1], s[2]} : PkStr{0, 0, 0}; }
 
-// vec: rows in whole 16-byte pieces -- pointers, strides and head widths.  split: tiles of 128 rows would be fewer than two
-// workgroups per compute unit.  3 x 777 rows, 6 fp32 heads of 48 (126 tiles), forward and queries' backward: 40 and 55 us, 19 and 23 split;
-// 8 x 2048 rows, 4 heads of 64 (512 tiles): 18 and 21, 24 and 36 split.
-PkForm pk_form(const PkArgs& a, int dtype, const void* const* p, int n, int heads) {
+// vec: rows in whole 16-byte pieces -- pointers, strides and head widths.
+// split: where tiles of 128 rows are too few for the compute units, most of all where sequences are long and a tile has many keys.
+// Then four times the workgroups each walk a quarter of the keys, at the price of loading keys for 32 rows at a time.  us as one tile and split,
+// forward and backward: 3 x 777 rows, 5 sequences, 6 heads of 48 over 2 (126 tiles): bf16 10.5 / 7.6 and 33 / 30, fp32 25 / 16 and 63 / 53;
+// 8 x 1452, 2 heads of 96 over 1 (192): bf16 33 / 26 and 102 / 105, fp32 192 / 122 and 475 / 351; 3 x 7290, 13 sequences, 2 heads
+// of 40 (348): bf16 forward 28 / 21; 4096, 8 heads of 128 (256): bf16 85 / 66 and 259 /
+// 260, fp32 538 / 363 and 1403 / 1101; the same in 30 sequences: bf16 15 / 19 and 42 / 65, fp32 48 / 72 and 135 / 168; 8 x 2048, 4 heads of 64 (512), 2
+// sequences: bf16 29 / 31 and 95 / 104, fp32 135 / 103 and 384 / 327, in 12: fp32 44 / 50 and 127 / 140; 4 x 2048, 16 heads of 128 (1024): bf16
+// 92 / 150 and 318 / 499, fp32 604 / 799 and 2023 / 2216.
+bool pk_split(const PkArgs& a, int dtype, bool bwd) {
+  const int64_t tiles = (int64_t)pk_tiles(a.R, 4 * PK_WT) * a.B * a.Hq;
+  const bool longer = a.R / a.nseq >= 384;
+  if (dtype == HFTA_BF16) return tiles < (longer && !bwd ? 400 : 192);
+  return tiles < 256 || (longer && tiles * (a.d > 64 ? 2 : 1) < 1024);
+}
+PkForm pk_form(const PkArgs& a, int dtype, const void* const* p, int n, bool bwd) {
   const int64_t m = dtype == HFTA_BF16 ? 8 : 4;
   uintptr_t bits = 0;
   for (int i = 0; i < n; ++i) bits |= reinterpret_cast<uintptr_t>(p[i]);
   const PkStr* s[] = {&a.qs, &a.ks, &a.cs, &a.dqs, &a.dks};
   bool vec = a.d % m == 0 && bits % 16 == 0;
   for (const PkStr* x : s) vec = vec && x->b % m == 0 && x->r % m == 0 && x->h % m == 0 && x->r >= 0 && x->r <= PK_LD_MAX;
-  return PkForm{dtype == HFTA_BF16, vec, vec && (int64_t)pk_tiles(a.R, 4 * PK_WT) * a.B * heads < 512};
+  return PkForm{dtype == HFTA_BF16, vec, vec && pk_split(a, dtype, bwd)};
 }
 
 }  // namespace
@@ -71,7 +83,7 @@ int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.parts = 1;
   pk_places(a);
   const void* p[] = {Q, K, V, CTX};
-  return pk_fwd(a, pk_form(a, dtype, p, 4, Hq), as_stream(stream));
+  return pk_fwd(a, pk_form(a, dtype, p, 4, false), as_stream(stream));
 }
 
 size_t hfta_attention_packed_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
@@ -104,8 +116,9 @@ int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   pk_places(a);
   const void* p[] = {Q, K, V, CTX, dCTX, dQ, dK, dV};
   hipStream_t st = as_stream(stream);
-  const int rq = pk_dq(a, pk_form(a, dtype, p, 8, Hq), st);
-  return rq != HFTA_OK ? rq : pk_dkv(a, pk_form(a, dtype, p, 8, Hq), st);
+  const PkForm f = pk_form(a, dtype, p, 8, true);
+  const int rq = pk_dq(a, f, st);
+  return rq != HFTA_OK ? rq : pk_dkv(a, f, st);
 }
 
 }  // extern "C"
