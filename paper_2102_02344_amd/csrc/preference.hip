@@ -6,8 +6,8 @@
 //   dz_r[k] = c_s (1[k = y_r] - softmax(z_r)_k),  c_2p = -c_2p+1 = -beta ((1 - eps) sigma(-t_p) - eps sigma(t_p)) / pairs
 //
 // Bound by memory: the gradient's factor needs the whole sequence, so rows with a label are read twice and every row of
-// a sequence is written once; rows without one are not read.  A workgroup takes a row, with 16-byte pieces from its first
-// aligned element on.  Sums over a sequence are taken in 64 bits: the loss is a difference of long sums.
+// a sequence is written once; rows without one are not read.  A workgroup takes a row, or a wavefront one where rows are
+// narrow, with 16-byte pieces from its first aligned element on.  Sums over a sequence are taken in 64 bits: the loss is a difference of long sums.
 #include "packed_rows.h"
 
 namespace hfta {
@@ -42,6 +42,9 @@ __device__ __forceinline__ uint4 pf_pack(const float (&x)[4]) {
 }
 __device__ __forceinline__ float pf_exp(float x, float top) { return __builtin_amdgcn_exp2f(fmaf(x, PF_LOG2E, -top * PF_LOG2E)); }
 
+// which of its workgroup's rows NT threads take
+template <int NT> __device__ __forceinline__ int pf_row_of() { return NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0; }
+
 // rows [lo, hi) of sequence s
 __device__ __forceinline__ void pf_rows(const int32_t* off, int s, int R, int& lo, int& hi) {
   lo = min(max(off[s], 0), R);
@@ -49,16 +52,16 @@ __device__ __forceinline__ void pf_rows(const int32_t* off, int s, int R, int& l
 }
 
 // ------------------------------------------------------------------ rows: log-sum-exp and the label's log-probability
-template <typename T>
+template <typename T, int NT>
 __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logits, const int32_t* __restrict__ labels,
                                                       const int32_t* __restrict__ off, int nseq, float* __restrict__ lse,
                                                       float* __restrict__ lp, int R, int K) {
   constexpr int EPP = PfRow<T>::EPP, NV = 4;
   __shared__ float sm[4], ss[4];
-  const int r = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
+  const int r = blockIdx.x * (256 / NT) + pf_row_of<NT>(), b = blockIdx.y, t = threadIdx.x % NT;
   const int64_t row = (int64_t)b * R + r;
   off += (int64_t)b * (nseq + 1);
-  if (r < off[0] || r >= off[nseq]) return;
+  if (r >= R || r < off[0] || r >= off[nseq]) return;
   const int y = labels[row];
   if (y < 0) {
     if (t == 0) lp[row] = 0.f;
@@ -74,12 +77,12 @@ __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logi
     m = mn;
     each(mu);
   };
-  for (int v0 = t; v0 < g.nv; v0 += 256 * NV) {
+  for (int v0 = t; v0 < g.nv; v0 += NT * NV) {
     float x[NV][EPP];
     float mt = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-      if (v0 + 256 * j < g.nv) pf_unpack(zv[v0 + 256 * j], x[j]);
+      if (v0 + NT * j < g.nv) pf_unpack(zv[v0 + NT * j], x[j]);
       else
 #pragma unroll
         for (int e = 0; e < EPP; ++e) x[j][e] = -INFINITY;
@@ -101,15 +104,20 @@ __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logi
   float M = m;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-  if ((t & 63) == 0) sm[t >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  if constexpr (NT > 64) {
+    if ((t & 63) == 0) sm[t >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  }
   const float Mu = M == -INFINITY ? 0.f : M;
   s = wave_sum(s * pf_exp(m, Mu));
-  if ((t & 63) == 0) ss[t >> 6] = s;
-  __syncthreads();
+  if constexpr (NT > 64) {
+    if ((t & 63) == 0) ss[t >> 6] = s;
+    __syncthreads();
+    s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+  }
   if (t == 0) {
-    const float rest = logf((ss[0] + ss[1]) + (ss[2] + ss[3]));
+    const float rest = logf(s);
     if (lse) lse[row] = M + rest;
     lp[row] = (label_score(z, y, K) - M) - rest;     // the two large terms first: what is left is rounded once
   }
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ 
 
 // ------------------------------------------------------------------ gradient: a row per workgroup; the last one of a
 // model adds its pairs' terms (in order)
-template <typename T>
+template <typename T, int NT>
 __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int32_t* __restrict__ labels,
                                                       const int32_t* __restrict__ off, int pairs, const float* __restrict__ lse,
                                                       const float* __restrict__ coef, const float* __restrict__ term,
@@ -191,8 +199,9 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
   constexpr int EPP = PfRow<T>::EPP, NV = 4;
   __shared__ double sh[4];
   // the last rows first: what the pass before read last may still be in the last-level cache
-  const int r = R - (int)blockIdx.x, b = (int)(gridDim.y - 1 - blockIdx.y), t = threadIdx.x, nseq = 2 * pairs;
-  if (r == R) {
+  const int b = (int)(gridDim.y - 1 - blockIdx.y), nseq = 2 * pairs, t = threadIdx.x % NT;
+  if (blockIdx.x == 0) {
+    const int t = threadIdx.x;
     double v = 0;
     for (int i = t; i < pairs; i += 256) v += (double)term[(int64_t)b * pairs + i];
 #pragma unroll
@@ -202,6 +211,8 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
     if (t == 0) loss[b] = (float)(((sh[0] + sh[1]) + (sh[2] + sh[3])) / pairs);
     return;
   }
+  const int r = R - (int)((blockIdx.x - 1) * (256 / NT) + pf_row_of<NT>()) - 1;
+  if (r < 0) return;
   const int64_t row = (int64_t)b * R + r;
   off += (int64_t)b * (nseq + 1);
   if (r < off[0] || r >= off[nseq]) return;
@@ -211,7 +222,7 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
   const PfRow<T> g(dz, K);
   uint4* dv = reinterpret_cast<uint4*>(dz + g.head);
   if (y < 0) {
-    for (int v = t; v < g.nv; v += 256) dv[v] = make_uint4(0, 0, 0, 0);
+    for (int v = t; v < g.nv; v += NT) dv[v] = make_uint4(0, 0, 0, 0);
     if (t < g.head + g.tail) Elem<T>::store(dz + (t < g.head ? t : K - g.tail + t - g.head), 0.f);
     return;
   }
@@ -219,14 +230,14 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
   auto grad = [&](float x, int k) { return c * ((k == y ? 1.f : 0.f) - pf_exp(x, ls)); };
   if (((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0) {
     const uint4* zv = reinterpret_cast<const uint4*>(z + g.head);
-    for (int v0 = t; v0 < g.nv; v0 += 256 * NV) {
+    for (int v0 = t; v0 < g.nv; v0 += NT * NV) {
       uint4 u[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (v0 + 256 * j < g.nv) u[j] = zv[v0 + 256 * j];
+        if (v0 + NT * j < g.nv) u[j] = zv[v0 + NT * j];
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int v = v0 + 256 * j;
+        const int v = v0 + NT * j;
         if (v >= g.nv) continue;
         float x[EPP];
         pf_unpack(u[j], x);
@@ -240,7 +251,7 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
       Elem<T>::store(dz + k, grad(Elem<T>::load(z + k), k));
     }
   } else {                                           // logits and gradient lie differently against 16 bytes
-    for (int k = t; k < K; k += 256) Elem<T>::store(dz + k, grad(Elem<T>::load(z + k), k));
+    for (int k = t; k < K; k += NT) Elem<T>::store(dz + k, grad(Elem<T>::load(z + k), k));
   }
 }
 
@@ -249,11 +260,30 @@ int pf_check(int B, int R, int K, int nseq, int dtype) {
   return B > 65535 || R > 0xfffffe || nseq > PACKED_MAX ? HFTA_EUNSUPPORTED : HFTA_OK;      // (a launch has fewer than 2^32 threads)
 }
 
+// A wavefront takes a row of up to 4 KB at once, four pieces a lane.  A workgroup each and a wavefront each, log-probabilities and loss of
+// bf16 rows: 131072 of 512 classes 137 / 61 and 220 / 107 us, 32768 of 2048 49 / 28 and 91 / 70, 16384 of 8192 43 / 46 and 146 / 154.
+bool pf_narrow(int K, size_t es) { return (size_t)K * es <= 4096; }
+
 template <typename T>
 void pf_rows_launch(int B, int R, int K, int nseq, const void* logits, const int32_t* labels, const int32_t* off, float* lse,
                     float* lp, hipStream_t st) {
-  hipLaunchKernelGGL(pf_rows_kernel<T>, dim3((unsigned)R, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off, nseq, lse,
-                     lp, R, K);
+  if (pf_narrow(K, sizeof(T)))
+    hipLaunchKernelGGL((pf_rows_kernel<T, 64>), dim3((unsigned)(R + 3) / 4, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off,
+                       nseq, lse, lp, R, K);
+  else
+    hipLaunchKernelGGL((pf_rows_kernel<T, 256>), dim3((unsigned)R, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off, nseq,
+                       lse, lp, R, K);
+}
+
+template <typename T>
+void pf_grad_launch(int B, int R, int K, int pairs, const void* logits, const int32_t* labels, const int32_t* off, const float* lse,
+                    const float* coef, const float* term, float* loss, void* dlogits, hipStream_t st) {
+  if (pf_narrow(K, sizeof(T)))
+    hipLaunchKernelGGL((pf_grad_kernel<T, 64>), dim3((unsigned)(R + 3) / 4 + 1u, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels,
+                       off, pairs, lse, coef, term, loss, (T*)dlogits, R, K);
+  else
+    hipLaunchKernelGGL((pf_grad_kernel<T, 256>), dim3((unsigned)R + 1u, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off,
+                       pairs, lse, coef, term, loss, (T*)dlogits, R, K);
 }
 
 }  // namespace
@@ -300,13 +330,10 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
   hipLaunchKernelGGL(pf_pair_kernel, dim3((unsigned)npairs, (unsigned)B), dim3(256), 0, st, lp, seq_offsets,
                      npairs, ref_logps, beta, label_smoothing, logps, term, coef, R);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
-  const dim3 grid((unsigned)R + 1u, (unsigned)B);
   if (dtype == HFTA_BF16)
-    hipLaunchKernelGGL(pf_grad_kernel<bf16_raw>, grid, dim3(256), 0, st, (const bf16_raw*)logits, labels, seq_offsets, npairs, lse,
-                       coef, term, loss, (bf16_raw*)dlogits, R, K);
+    pf_grad_launch<bf16_raw>(B, R, K, npairs, logits, labels, seq_offsets, lse, coef, term, loss, dlogits, st);
   else
-    hipLaunchKernelGGL(pf_grad_kernel<float>, grid, dim3(256), 0, st, (const float*)logits, labels, seq_offsets, npairs, lse, coef,
-                       term, loss, (float*)dlogits, R, K);
+    pf_grad_launch<float>(B, R, K, npairs, logits, labels, seq_offsets, lse, coef, term, loss, dlogits, st);
   return launch_status();
 }
 
