@@ -28,6 +28,11 @@
 // A workgroup is four wavefronts.  With many rows each takes 32 rows of its own and all keys, which the workgroup stages 64
 // at a time, twice buffered with one barrier per tile.  Where that leaves compute units without work (SPLIT), all four take the
 // same 32 rows and a quarter of the key blocks each, from LDS of their own without barriers, and join at the end.
+//
+// Measured, bf16: forward of 16384 rows in two sequences, 8 heads of 128 over 2, 313 us (943 TFLOP/s; a library product of 8192^3 reaches
+// 1198): bound by the vector work of the softmax beside the matrix instructions.  2 x 8192 rows in three, the same heads: forward 153,
+// queries' backward 205, keys' 358 and 28 for its parts, the last bound by registers.  8 x 2048 rows in twelve, 4 heads of 64: 17, 21 and 26 us,
+// chains of a few tiles at 1.6 to 2 us each; bytes alone would be 14.
 #pragma once
 #include "gemm_dma.h"
 #include "packed_rows.h"
