@@ -9,7 +9,7 @@
 // leaves a partial sum, and a workgroup adds them, in order, so that a frequent token (padding, the first words
 // of a text) costs no serial walk.  The sort: digits of at most eight bits from the lowest on, a count and a scatter each.
 //
-// Measured, 2 x 60000 bf16 rows of 1024 columns, 32001 tokens: lookup 105 us (4.7 TB/s), sort 31 in four launches, sums 123, long runs 14; 8
+// Measured, 2 x 60000 bf16 rows of 1024 columns, 32001 tokens: lookup 105 us (4.7 TB/s), sort 31 in four launches, sums 112, long runs 14; 8
 // x 8192 rows of 256, 8192 tokens: 13, 18, 18 and 6, launches and chains of loads.
 #include "packed_rows.h"
 
@@ -326,7 +326,9 @@ template <bool VEC> __device__ __forceinline__ void ep_store(float* dst, int c, 
 // A run that begins in a stretch and ends in it or the next one is added by the wavefront of the first.  part [B][chunks][2][E]: of a
 // stretch, the sum of a longer run's rows that came in from the stretch before (0), and that begin here (1).  `beside`: wavefronts of
 // a workgroup on one stretch, next to each other in its columns, so that a wide row is read at once.  Workgroups behind the `sums` that
-// add clear the rows of tokens that no row has: a lane looks for one token each.  (Clearing the whole table beside the sort writes the
+// add clear the rows of tokens that no row has: a workgroup takes 64 tokens, a lane
+// looks for one each, and each wavefront clears a quarter of those missing (64 tokens a wavefront: 371 fp32 rows of 681 columns, 411 tokens, 22 us
+// instead of 10; 2 x 60000 of 1024, 32001 tokens, 123 instead of 112).  (Clearing the whole table beside the sort writes the
 // other rows twice: 278 us with the lookup for 2 x 60000 rows, 32001 tokens of 1024 columns.)
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void ep_sum_kernel(const T* __restrict__ dY, const uint2* __restrict__ sorted, float* __restrict__ dtable,
@@ -335,14 +337,14 @@ __global__ __launch_bounds__(256) void ep_sum_kernel(const T* __restrict__ dY, c
   const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= sums) {
     const uint2* s = sorted + (int64_t)b * R;
-    const int64_t v0 = (((int64_t)(blockIdx.x - sums) * gridDim.z + blockIdx.z) * 4 + wave) * 64, v = v0 + lane;
+    const int64_t v0 = ((int64_t)(blockIdx.x - sums) * gridDim.z + blockIdx.z) * 64, v = v0 + lane;
     int a = 0, z = R;                                 // the first place whose token is not below v
     while (a < z) {
       const int mid = a + ((z - a) >> 1);
       if ((int64_t)s[mid].x < v) a = mid + 1;
       else z = mid;
     }
-    unsigned long long none = __ballot(v < V && (a == R || (int64_t)s[a].x != v));
+    unsigned long long none = __ballot(v < V && (lane & 3) == wave && (a == R || (int64_t)s[a].x != v));
     const float zero[4] = {};
     for (; none; none &= none - 1) {
       float* row = dtable + ((int64_t)b * V + v0 + __builtin_ctzll(none)) * E;
@@ -563,7 +565,7 @@ int hfta_embedding_bwd_sorted(int B, int R, int V, int E, int nseq, int dtype, c
   const bool vec = E % 4 == 0 && reinterpret_cast<uintptr_t>(dY) % (4 * es) == 0 && reinterpret_cast<uintptr_t>(dtable) % 16 == 0;
   const int slices = (E + SORT_SLICE - 1) / SORT_SLICE, beside = slices > 2 ? 4 : slices;
   const int sums = (pl.chunks + 4 / beside - 1) / (4 / beside), groups = (slices + beside - 1) / beside;
-  const dim3 gs((unsigned)(sums + (V + (int64_t)256 * groups - 1) / (256 * groups)), (unsigned)B, (unsigned)groups);
+  const dim3 gs((unsigned)(sums + (V + (int64_t)64 * groups - 1) / (64 * groups)), (unsigned)B, (unsigned)groups);
   const dim3 gj((unsigned)((pl.chunks + 3) / 4), (unsigned)B, (unsigned)slices);
 #define EP_SUM(T, VEC) hipLaunchKernelGGL((ep_sum_kernel<T, VEC>), gs, dim3(256), 0, st, (const T*)dY, in.pairs, dtable, part, R, V, E, \
                                           pl.chunks, beside, sums, scale)
