@@ -43,7 +43,9 @@ __device__ __forceinline__ uint4 pf_pack(const float (&x)[8]) {
 __device__ __forceinline__ uint4 pf_pack(const float (&x)[4]) {
   return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
 }
-__device__ __forceinline__ float pf_exp(float x, float top) { return __builtin_amdgcn_exp2f(fmaf(x, PF_LOG2E, -top * PF_LOG2E)); }
+// exp(x - top), top >= x.  The difference first: it is exact or rounded by its own size, where the rounding of top log2(e) would be a factor common
+// to all terms of a row, as large as the logits are (1000 of them around 1000: log-probabilities off by 4e-5, this way 1e-6).
+__device__ __forceinline__ float pf_exp(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * PF_LOG2E); }
 
 // which of its workgroup's rows NT threads take
 template <int NT> __device__ __forceinline__ int pf_row_of() { return NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0; }
@@ -54,11 +56,13 @@ __device__ __forceinline__ void pf_rows(const int32_t* off, int s, int R, int& l
   hi = min(max(off[s + 1], 0), R);
 }
 
-// ------------------------------------------------------------------ rows: log-sum-exp and the label's log-probability
+// ------------------------------------------------------------------ rows: the label's log-probability, and what the gradient needs of a row:
+// its largest value, and one over the sum of the exponentials of distances from it.  (Joined as log-sum-exp they would be rounded as one number: a
+// probability formed from that is off by as much as the logits are large, and can pass 1.)
 template <typename T, int NT>
 __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logits, const int32_t* __restrict__ labels,
-                                                      const int32_t* __restrict__ off, int nseq, float* __restrict__ lse,
-                                                      float* __restrict__ lp, int R, int K) {
+                                                      const int32_t* __restrict__ off, int nseq, float* __restrict__ top,
+                                                      float* __restrict__ inv, float* __restrict__ lp, int R, int K) {
   constexpr int EPP = PfRow<T>::EPP, NV = 4;
   __shared__ float sm[4], ss[4];
   const int r = blockIdx.x * (256 / NT) + pf_row_of<NT>(), b = blockIdx.y, t = threadIdx.x % NT;
@@ -120,9 +124,11 @@ __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logi
     s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
   }
   if (t == 0) {
-    const float rest = logf(s);
-    if (lse) lse[row] = M + rest;
-    lp[row] = (label_score(z, y, K) - M) - rest;     // the two large terms first: what is left is rounded once
+    if (top) {
+      top[row] = M;
+      inv[row] = 1.f / s;
+    }
+    lp[row] = (label_score(z, y, K) - M) - logf(s);  // the two large terms first
   }
 }
 
@@ -196,9 +202,9 @@ __global__ __launch_bounds__(256) void pf_pair_kernel(const float* __restrict__ 
 // model adds its pairs' terms (in order)
 template <typename T, int NT>
 __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int32_t* __restrict__ labels,
-                                                      const int32_t* __restrict__ off, int pairs, const float* __restrict__ lse,
-                                                      const float* __restrict__ coef, const float* __restrict__ term,
-                                                      float* __restrict__ loss, T* dlogits, int R, int K) {
+                                                      const int32_t* __restrict__ off, int pairs, const float* __restrict__ top,
+                                                      const float* __restrict__ inv, const float* __restrict__ coef,
+                                                      const float* __restrict__ term, float* __restrict__ loss, T* dlogits, int R, int K) {
   constexpr int EPP = PfRow<T>::EPP, NV = 4;
   __shared__ double sh[4];
   // the last rows first: what the pass before read last may still be in the last-level cache
@@ -229,8 +235,8 @@ __global__ __launch_bounds__(256) void pf_grad_kernel(const T* logits, const int
     if (t < g.head + g.tail) Elem<T>::store(dz + (t < g.head ? t : K - g.tail + t - g.head), 0.f);
     return;
   }
-  const float c = coef[row], ls = lse[row];
-  auto grad = [&](float x, int k) { return c * ((k == y ? 1.f : 0.f) - pf_exp(x, ls)); };
+  const float c = coef[row], M = top[row], is = inv[row];
+  auto grad = [&](float x, int k) { return c * fmaf(-pf_exp(x, M), is, k == y ? 1.f : 0.f); };
   if (((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0) {
     const uint4* zv = reinterpret_cast<const uint4*>(z + g.head);
     for (int v0 = t; v0 < g.nv; v0 += NT * NV) {
@@ -268,25 +274,25 @@ int pf_check(int B, int R, int K, int nseq, int dtype) {
 bool pf_narrow(int K, size_t es) { return (size_t)K * es <= 4096; }
 
 template <typename T>
-void pf_rows_launch(int B, int R, int K, int nseq, const void* logits, const int32_t* labels, const int32_t* off, float* lse,
-                    float* lp, hipStream_t st) {
+void pf_rows_launch(int B, int R, int K, int nseq, const void* logits, const int32_t* labels, const int32_t* off, float* top,
+                    float* inv, float* lp, hipStream_t st) {
   if (pf_narrow(K, sizeof(T)))
     hipLaunchKernelGGL((pf_rows_kernel<T, 64>), dim3((unsigned)(R + 3) / 4, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off,
-                       nseq, lse, lp, R, K);
+                       nseq, top, inv, lp, R, K);
   else
     hipLaunchKernelGGL((pf_rows_kernel<T, 256>), dim3((unsigned)R, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off, nseq,
-                       lse, lp, R, K);
+                       top, inv, lp, R, K);
 }
 
 template <typename T>
-void pf_grad_launch(int B, int R, int K, int pairs, const void* logits, const int32_t* labels, const int32_t* off, const float* lse,
-                    const float* coef, const float* term, float* loss, void* dlogits, hipStream_t st) {
+void pf_grad_launch(int B, int R, int K, int pairs, const void* logits, const int32_t* labels, const int32_t* off, const float* top,
+                    const float* inv, const float* coef, const float* term, float* loss, void* dlogits, hipStream_t st) {
   if (pf_narrow(K, sizeof(T)))
     hipLaunchKernelGGL((pf_grad_kernel<T, 64>), dim3((unsigned)(R + 3) / 4 + 1u, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels,
-                       off, pairs, lse, coef, term, loss, (T*)dlogits, R, K);
+                       off, pairs, top, inv, coef, term, loss, (T*)dlogits, R, K);
   else
     hipLaunchKernelGGL((pf_grad_kernel<T, 256>), dim3((unsigned)R + 1u, (unsigned)B), dim3(256), 0, st, (const T*)logits, labels, off,
-                       pairs, lse, coef, term, loss, (T*)dlogits, R, K);
+                       pairs, top, inv, coef, term, loss, (T*)dlogits, R, K);
 }
 
 }  // namespace
@@ -302,8 +308,8 @@ int hfta_seq_logps(int B, int R, int K, int nseq, int dtype, const void* logits,
   if (rc == HFTA_EINVAL || !logits || !labels || !seq_offsets || !token_logps || !logps) return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
   hipStream_t st = as_stream(stream);
-  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
-  else pf_rows_launch<float>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, token_logps, st);
+  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, nullptr, token_logps, st);
+  else pf_rows_launch<float>(B, R, K, nseq, logits, labels, seq_offsets, nullptr, nullptr, token_logps, st);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
   hipLaunchKernelGGL(pf_seq_kernel, dim3((unsigned)nseq, (unsigned)B), dim3(256), 0, st, token_logps, seq_offsets, nseq,
                      logps, R);
@@ -312,7 +318,7 @@ int hfta_seq_logps(int B, int R, int K, int nseq, int dtype, const void* logits,
 
 size_t hfta_preference_loss_workspace_bytes(int B, int R, int npairs) {
   if (B <= 0 || R <= 0 || npairs <= 0 || npairs > PACKED_MAX / 2) return 0;
-  return ((size_t)B * R * 3 + (size_t)B * npairs) * sizeof(float);     // lse, label terms and factors of the rows; pair terms
+  return ((size_t)B * R * 4 + (size_t)B * npairs) * sizeof(float);     // largest value, inverse sum, label term and factor of the rows; pair terms
 }
 
 int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void* logits, const int32_t* labels,
@@ -326,17 +332,17 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
     return HFTA_EWORKSPACE;
   hipStream_t st = as_stream(stream);
   const size_t rows = (size_t)B * R;
-  float *lse = (float*)workspace, *lp = lse + rows, *coef = lp + rows, *term = coef + rows;
-  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
-  else pf_rows_launch<float>(B, R, K, 2 * npairs, logits, labels, seq_offsets, lse, lp, st);
+  float *top = (float*)workspace, *inv = top + rows, *lp = inv + rows, *coef = lp + rows, *term = coef + rows;
+  if (dtype == HFTA_BF16) pf_rows_launch<bf16_raw>(B, R, K, 2 * npairs, logits, labels, seq_offsets, top, inv, lp, st);
+  else pf_rows_launch<float>(B, R, K, 2 * npairs, logits, labels, seq_offsets, top, inv, lp, st);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
   hipLaunchKernelGGL(pf_pair_kernel, dim3((unsigned)npairs, (unsigned)B), dim3(256), 0, st, lp, seq_offsets,
                      npairs, ref_logps, beta, label_smoothing, logps, term, coef, R);
   if (launch_status() != HFTA_OK) return HFTA_ELAUNCH;
   if (dtype == HFTA_BF16)
-    pf_grad_launch<bf16_raw>(B, R, K, npairs, logits, labels, seq_offsets, lse, coef, term, loss, dlogits, st);
+    pf_grad_launch<bf16_raw>(B, R, K, npairs, logits, labels, seq_offsets, top, inv, coef, term, loss, dlogits, st);
   else
-    pf_grad_launch<float>(B, R, K, npairs, logits, labels, seq_offsets, lse, coef, term, loss, dlogits, st);
+    pf_grad_launch<float>(B, R, K, npairs, logits, labels, seq_offsets, top, inv, coef, term, loss, dlogits, st);
   return launch_status();
 }
 
