@@ -337,18 +337,21 @@ __global__ __launch_bounds__(256) void ep_sum_kernel(const T* __restrict__ dY, c
   const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= sums) {
     const uint2* s = sorted + (int64_t)b * R;
-    const int64_t v0 = ((int64_t)(blockIdx.x - sums) * gridDim.z + blockIdx.z) * 64, v = v0 + lane;
-    int a = 0, z = R;                                 // the first place whose token is not below v
-    while (a < z) {
-      const int mid = a + ((z - a) >> 1);
-      if ((int64_t)s[mid].x < v) a = mid + 1;
-      else z = mid;
-    }
-    unsigned long long none = __ballot(v < V && (lane & 3) == wave && (a == R || (int64_t)s[a].x != v));
-    const float zero[4] = {};
-    for (; none; none &= none - 1) {
-      float* row = dtable + ((int64_t)b * V + v0 + __builtin_ctzll(none)) * E;
-      for (int c = ep_col<VEC>(0, lane); c < E; c += SORT_SLICE) ep_store<VEC>(row, c, E, zero, 1.f);
+    const int64_t step = (int64_t)(gridDim.x - sums) * gridDim.z * 64;
+    for (int64_t v0 = ((int64_t)(blockIdx.x - sums) * gridDim.z + blockIdx.z) * 64; v0 < V; v0 += step) {
+      const int64_t v = v0 + lane;
+      int a = 0, z = R;                               // the first place whose token is not below v
+      while (a < z) {
+        const int mid = a + ((z - a) >> 1);
+        if ((int64_t)s[mid].x < v) a = mid + 1;
+        else z = mid;
+      }
+      unsigned long long none = __ballot(v < V && (lane & 3) == wave && (a == R || (int64_t)s[a].x != v));
+      const float zero[4] = {};
+      for (; none; none &= none - 1) {
+        float* row = dtable + ((int64_t)b * V + v0 + __builtin_ctzll(none)) * E;
+        for (int c = ep_col<VEC>(0, lane); c < E; c += SORT_SLICE) ep_store<VEC>(row, c, E, zero, 1.f);
+      }
     }
     return;
   }
@@ -565,7 +568,9 @@ int hfta_embedding_bwd_sorted(int B, int R, int V, int E, int nseq, int dtype, c
   const bool vec = E % 4 == 0 && reinterpret_cast<uintptr_t>(dY) % (4 * es) == 0 && reinterpret_cast<uintptr_t>(dtable) % 16 == 0;
   const int slices = (E + SORT_SLICE - 1) / SORT_SLICE, beside = slices > 2 ? 4 : slices;
   const int sums = (pl.chunks + 4 / beside - 1) / (4 / beside), groups = (slices + beside - 1) / beside;
-  const dim3 gs((unsigned)(sums + (V + (int64_t)64 * groups - 1) / (64 * groups)), (unsigned)B, (unsigned)groups);
+  // (sums are at most 2^23 and a launch has fewer than 2^24 workgroups in x: of more than 2^28 tokens a workgroup clears several times 64)
+  const int64_t clears = (V + (int64_t)64 * groups - 1) / (64 * groups);
+  const dim3 gs((unsigned)(sums + (clears < 1 << 22 ? clears : 1 << 22)), (unsigned)B, (unsigned)groups);
   const dim3 gj((unsigned)((pl.chunks + 3) / 4), (unsigned)B, (unsigned)slices);
 #define EP_SUM(T, VEC) hipLaunchKernelGGL((ep_sum_kernel<T, VEC>), gs, dim3(256), 0, st, (const T*)dY, in.pairs, dtable, part, R, V, E, \
                                           pl.chunks, beside, sums, scale)
