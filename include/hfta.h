@@ -672,7 +672,8 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
  *   and strides multiples of 8 bf16 / 4 fp32, pointers 16-byte aligned) take wide loads; any others are taken element by element.
  *   scale > 0 and finite (EINVAL).  LSE [B][Hq][R] fp32: log of the sum of exponentials of each row, which the backward call reads.
  *   bwd: all three gradients, from the forward call's CTX and LSE; dK and dV sum over the heads of a group.  Workspace
- *   hfta_attention_packed_bwd_workspace_bytes, 16-byte aligned (EWORKSPACE).  Outputs may not overlap inputs.
+ *   hfta_attention_packed_bwd_workspace_bytes, 16-byte aligned (EWORKSPACE): it grows with R and does not depend on nseq, so that the size
+ *   for the most rows serves every batch of as many or fewer, in any sequences.  Outputs may not overlap inputs.
  *   A value that is not finite reaches the rows that see it (an infinity as an infinity or a NaN) and no others.
  * embedding_packed_fwd: out[b,r,:] = scale * table[b, idx[b,r], :] + pos[min(r - start of r's sequence, S - 1), :] (pos fp32 [S][E] or
  *   NULL); storage dtype; indices clamped to [0, V).

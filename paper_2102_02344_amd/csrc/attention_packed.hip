@@ -19,16 +19,30 @@ int pk_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, float sc
 // a part is two tiles, or one in fp32, whose products take four times as long: 3 x 777 rows, 5 sequences, 6 fp32 heads of 48 over
 // 2: 141, with 8 parts 27 and 6; 3 x 201 rows, 8 sequences, 2 fp32 heads of 96 over 1: 48, with 5 parts 18 and 7; 2883 rows, 55 sequences, 4
 // heads of 40 over 2: 25, with 4 parts 14 and 5.
+constexpr int PK_WANT = 2048;
 int pk_parts(int B, int R, int nseq, int Hq, int Hkv, int dtype) {
   const int64_t base = (int64_t)pk_tiles(R, 2 * PK_WT) * B * Hkv;
   const int64_t rows = R / nseq + 2 * PK_WT < R ? R / nseq + 2 * PK_WT : R, tiles = rows * (Hq / Hkv) / PK_WT;
   const int64_t least = base >= 256 ? 8 : dtype == HFTA_BF16 ? 2 : 1;
-  int64_t p = 2048 / base;
+  int64_t p = PK_WANT / base;
   if (p > PK_PARTS_MAX) p = PK_PARTS_MAX;
   if (p > tiles / least) p = tiles / least;
   return p < 1 ? 1 : (int)p;
 }
 size_t pk_sums(int B, int R, int Hq) { return ((size_t)B * Hq * R * sizeof(float) + 255) / 256 * 256; }     // bytes of D
+// Bytes of the backward's workspace: D, and the largest sums of parts that any call has with as many rows or fewer.  p parts need at most
+// PK_WANT / p tiles, so there are p R words per column at most with R up to that; the rows and sequences of a batch change from step to step, and a
+// workspace for the largest serves them all (two fp32 words for each of PK_WANT tiles' columns: 134 MB at d = 128).
+size_t pk_workspace(int B, int R, int Hq, int Hkv, int d) {
+  const int64_t heads = (int64_t)B * Hkv;
+  size_t most = 0;
+  for (int p = 2; p <= PK_PARTS_MAX; ++p) {
+    const int64_t rows = 2 * PK_WT * (PK_WANT / p / heads);
+    const size_t n = (size_t)p * (size_t)(rows < R ? rows : R);
+    if (n > most) most = n;
+  }
+  return pk_sums(B, R, Hq) + most * 2 * (size_t)heads * d * sizeof(float);
+}
 void pk_places(PkArgs& a) {
   a.by_heads = PkDiv((uint32_t)(a.B * a.Hkv));
   a.by_hkv = PkDiv((uint32_t)a.Hkv);
@@ -88,8 +102,7 @@ int hfta_attention_packed_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
 
 size_t hfta_attention_packed_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   if (pk_check(B, R, nseq, Hq, Hkv, d, dtype, 1.f) != HFTA_OK) return 0;
-  const int parts = pk_parts(B, R, nseq, Hq, Hkv, dtype);
-  return pk_sums(B, R, Hq) + (parts > 1 ? (size_t)parts * 2 * B * R * Hkv * d * sizeof(float) : 0);
+  return pk_workspace(B, R, Hq, Hkv, d);
 }
 
 int hfta_attention_packed_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
