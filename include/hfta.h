@@ -670,7 +670,7 @@ int hfta_attention_bwd(int B, int N, int S, int E, int H, int dtype, const void*
  *   s[0] b + s[1] r + s[2] h + c with element strides s[3] (host): qs for Q, kvs for K and V, cs for CTX and dCTX, dqs for dQ,
  *   dkvs for dK and dV.  Packed projections [R][q | k | v] are three pointers with one set of strides.  Rows in 16-byte pieces (d
  *   and strides multiples of 8 bf16 / 4 fp32, pointers 16-byte aligned) take wide loads; any others are taken element by element.
- *   scale > 0 and finite (EINVAL).  LSE [B][Hq][R] fp32: log of the sum of exponentials of each row, which the backward call reads.
+ *   scale > 0, log2(e) scale finite (EINVAL).  LSE [B][Hq][R] fp32: log of the sum of exponentials of each row, which the backward call reads.
  *   bwd: all three gradients, from the forward call's CTX and LSE; dK and dV sum over the heads of a group.  Workspace
  *   hfta_attention_packed_bwd_workspace_bytes, 16-byte aligned (EWORKSPACE): it grows with R and does not depend on nseq, so that the size
  *   for the most rows serves every batch of as many or fewer, in any sequences.  Outputs may not overlap inputs.

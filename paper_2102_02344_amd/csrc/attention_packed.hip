@@ -6,7 +6,7 @@ namespace {
 
 int pk_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, float scale) {
   if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || !(scale > 0.f) ||
-      isinf(scale) || R > 0x7fffffff - 128)
+      isinf(scale * PK_LOG2E) || R > 0x7fffffff - 128)
     return HFTA_EINVAL;
   // (a launch has fewer than 2^32 threads; tiles are of at least 64 rows where there are many)
   return d > 128 || nseq > PACKED_MAX || (int64_t)B * Hq > 0xffffff / pk_tiles(R, 2 * PK_WT) ? HFTA_EUNSUPPORTED : HFTA_OK;
