@@ -100,8 +100,9 @@ __global__ __launch_bounds__(256) void pf_rows_kernel(const T* __restrict__ logi
     take(mt, [&](float mu) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
+        if (v0 + NT * j < g.nv)                     // (512 bf16 columns are one of a lane's four pieces: 44 -> 32 us for 131072 rows)
 #pragma unroll
-        for (int e = 0; e < EPP; ++e) s += pf_exp(x[j][e], mu);
+          for (int e = 0; e < EPP; ++e) s += pf_exp(x[j][e], mu);
     });
   }
   if (t < g.head + g.tail) {
@@ -270,7 +271,8 @@ int pf_check(int B, int R, int K, int nseq, int dtype) {
 }
 
 // A wavefront takes a row of up to 4 KB at once, four pieces a lane.  A workgroup each and a wavefront each, log-probabilities and loss of
-// bf16 rows: 131072 of 512 classes 137 / 61 and 220 / 107 us, 32768 of 2048 49 / 28 and 91 / 70, 16384 of 8192 43 / 46 and 146 / 154.
+// bf16 rows (8 models, 16 pairs, 60 % of the rows with a label): 131072 of 512 classes 91 / 32 and 177 / 66 us, 32768 of 2048 29 / 19 and 60 / 49,
+// 16384 of 8192 28 / 32 and 93 / 103; fp32 rows of 512 classes 89 / 34 and 193 / 97, of 2048 31 / 26 and 93 / 97.
 bool pf_narrow(int K, size_t es) { return (size_t)K * es <= 4096; }
 
 template <typename T>
