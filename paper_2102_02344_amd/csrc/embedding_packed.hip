@@ -76,6 +76,9 @@ __global__ __launch_bounds__(256) void ep_fwd_kernel(const T* __restrict__ table
 }
 
 // ------------------------------------------------------------------ sort
+// Blocks add up the counts of those before them by themselves up to SORT_SELF of them, else a launch does (one workgroup per model).  The whole gradient
+// of 8 columns and 8192 tokens, us by blocks and by a launch: 8 models of 20000 rows 41 / 47, 65536 76 / 79, 131072 157 / 130, 500000 1000 / 440; one model of 65536
+// rows 34 / 43, 131072 46 / 63, 500000 145 / 182.
 constexpr int SORT_BLK = 1024, SORT_BINS = 256, SORT_SELF = 64, SORT_ONE = 2048, SORT_CH = 32, SORT_SLICE = 256;
 
 // Token of a row: its index, or V (past every token) for a row outside the sequences.  The first pass reads the indices,

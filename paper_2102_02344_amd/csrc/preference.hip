@@ -9,8 +9,8 @@
 // a sequence is written once; rows without one are not read.  A workgroup takes a row, or a wavefront one where rows are
 // narrow, with 16-byte pieces from its first aligned element on.  Sums over a sequence are taken in 64 bits: the loss is a difference of long sums.
 //
-// Measured, bf16: 8 x 2048 rows of 8192 classes: rows 25 to 31 us, pairs 5, gradient 57; 4 x 4096 rows of 32001: 136, 5
-// and 281 (1.05 GB of logits).  Pieces of 16 bytes, four in flight a thread (eight: 25 -> 33 us).
+// Measured, bf16: 8 x 2048 rows of 8192 classes: rows 26 to 32 us, pairs 5, gradient 57; 4 x 4096 rows of 32001: 139, 5
+// and 282 (1.05 GB of logits).  Pieces of 16 bytes, four in flight a thread (eight: 25 -> 33 us).
 #include "packed_rows.h"
 
 namespace hfta {
