@@ -72,6 +72,8 @@ typedef enum hfta_act {
   HFTA_ACT_GELU = 4   /* exact: x * Phi(x), Phi via erf */
 } hfta_act;
 
+typedef enum hfta_norm { HFTA_NORM_LAYER = 0, HFTA_NORM_RMS = 1 } hfta_norm;
+
 const char* hfta_status_string(int status);
 int hfta_version(void);
 
@@ -715,6 +717,74 @@ size_t hfta_preference_loss_workspace_bytes(int B, int R, int npairs);
 int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void* logits, const int32_t* labels,
                          const int32_t* seq_offsets, const float* ref_logps, const float* beta, const float* label_smoothing,
                          float* loss, float* logps, void* dlogits, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A decoder layer with a recurrent memory, on packed sequences (fusion rules table rows "Embedding", "MultiheadAttention",
+ * "LayerNorm", "Dropout").  Sequences, rows outside of them and offsets are as above; results are the same bit for bit on every run.
+ *
+ * rotary_packed: positions as rotations of query and key heads.  X, Y hold H heads of d columns, element (b, r, h, c) at s[0] b + s[1] r +
+ *   s[2] h + c with element strides s[3] (host); Y may be X itself with the same strides (query and key heads that lie next to each other
+ *   in a packed projection take one call).  `pairs` pairs of columns (2 pairs <= d) are turned by the angle
+ *   positions[b][r][axis[i]] * freq[b][i], formed in 64 bits: pair i is columns (2i, 2i + 1) where `interleaved`, otherwise (i, i + pairs); the
+ *   columns behind them are copied.  positions: int32 [B][R][naxes]; axis: int32 [pairs], taken into [0, naxes); freq: fp32 [B][pairs], each
+ *   model its own; all device.  naxes 1: axis may be NULL, and positions too, which then are a row's place in its sequence (without
+ *   seq_offsets: the row).  seq_offsets NULL: all rows, nseq is not looked at.  inverse != 0 turns the other way: the gradient.
+ * linear_attention: per key head a state S [d][d], S_t = lambda S_t-1 + k_t v_t^T, ctx_t = scale q_t S_t for each query head of its group,
+ *   lambda = exp(log_decay[b][h]) (fp32 [B][Hkv], device; -infinity: no memory; above 0 counts as 0), scale > 0 with a finite inverse
+ *   (EINVAL).  Heads, strides and alignment as in attention_packed, d <= 128 (EUNSUPPORTED).  In front of sequence s a state is
+ *   state_in[b][s][h] (fp32 [B][nseq][Hkv][d][d]; NULL: zeros), behind it state_out[b][s][h] (NULL: not wanted; an empty sequence's
+ *   state_in).  state_out may be state_in itself.  bwd: gradients of Q, K, V from the same state_in and, where state_out is used
+ *   further, its gradient dstate_out (or NULL); dstate_in (or NULL) gets the gradient of state_in, and may be dstate_out itself.  log_decay is a
+ *   hyper-parameter without a gradient.  Workspaces *_workspace_bytes, 16-byte aligned (EWORKSPACE); one for the most rows and sequences serves
+ *   every smaller batch.  A value that is not finite reaches the rows that see it, as an infinity or a NaN, and no others.
+ *   States and sums are fp32.
+ * linear_attention_step: one token of each of n rows: Q, CTX [Hq], K, V [Hkv] heads at s[0] b + s[1] i + s[2] h + c, the state of row i in place
+ *   slot[b][i] (int32 [B][n], device; NULL: place i) of state, fp32 [B][slots][Hkv][d][d], and the new one in the same place of new_state,
+ *   which may be state itself.  A row whose slot lies outside [0, slots) takes no part: its CTX is left as it was, as are new
+ *   states that no row names.  Rows that name the same slot are tokens of one sequence, in order of i.
+ * gated_residual_norm: u = N(F) w1 + b1;  S = X + res sigma(G) u;  Y = N(S) w2 + b2, N over the last dimension of [B][R][E] (contiguous),
+ *   with or without the mean (`norm`), E <= 16384 (EUNSUPPORTED).  w1, b1, w2, b2: fp32 [B][E]; res: fp32 [B]; G: [B][R][E].  b1, b2, res, G may
+ *   be NULL (0, 0, 1, a gate of 1).  F NULL: the norm in front of a first block alone, Y = N(X) w2 + b2; then G, w1, b1, res, S and
+ *   what belongs to them below are NULL.  Y is made of S before S is rounded to the storage dtype.  mean1, inv1, mean2, inv2 (fp32
+ *   [B][R]): what the backward call reads (RMS: means are not looked at).
+ *   bwd: dS (or NULL): the gradient that reaches S on the residual path; dX: the whole gradient of S, which is X's; dF; dG (exactly where G
+ *   is); dw1, dw2; db1 (exactly where b1 is), db2 (or NULL); dres [B] (or NULL).  dX may be dS itself.  Sums over rows are added in a fixed order.
+ *   Workspace gated_residual_norm_bwd_workspace_bytes, 4-byte aligned (EWORKSPACE).
+ * dropout_counter: Y = X / (1 - p[b]) where kept, 0 elsewhere, whatever stands there; count elements per model, p: fp32 [B] (taken into [0, 1]).
+ *   The mask is a function of place alone and never stored: element i is kept where word i % 4 of the Philox4x32-10 block (Salmon et al.,
+ *   SC 2011) of counter (i / 4 low, i / 4 high, site, *step) under the key seed[b] (low word first) is at least 2^32 p[b].  seed: 64 bits [B], step: 32
+ *   bits [1] (NULL: 0), device, so that a captured graph draws anew when the caller counts `step` on; site tells calls of one
+ *   step apart.  The same call on dY is the backward.  Y may be X itself.
+ * EUNSUPPORTED above 65535 models, 2^24 - 2 sequences of a model, and launches of 2^24 workgroups or more.
+ * ---------------------------------------------------------------------- */
+int hfta_rotary_packed(int B, int R, int nseq, int H, int d, int dtype, const void* X, const int64_t xs[3], const int32_t* positions,
+                       int naxes, const int32_t* axis, int pairs, const float* freq, int interleaved, const int32_t* seq_offsets,
+                       int inverse, void* Y, const int64_t ys[3], void* stream);
+size_t hfta_linear_attention_fwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype);
+int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
+                              const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, const float* log_decay,
+                              float scale, const float* state_in, void* CTX, const int64_t cs[3], float* state_out, void* workspace,
+                              size_t ws_bytes, void* stream);
+size_t hfta_linear_attention_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype);
+int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
+                              const void* K, const void* V, const int64_t kvs[3], const int32_t* seq_offsets, const float* log_decay,
+                              float scale, const float* state_in, const void* dCTX, const int64_t cs[3], const float* dstate_out,
+                              void* dQ, const int64_t dqs[3], void* dK, void* dV, const int64_t dkvs[3], float* dstate_in,
+                              void* workspace, size_t ws_bytes, void* stream);
+int hfta_linear_attention_step(int B, int n, int slots, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3],
+                               const void* K, const void* V, const int64_t kvs[3], const int32_t* slot, const float* log_decay,
+                               float scale, const float* state, void* CTX, const int64_t cs[3], float* new_state, void* stream);
+int hfta_gated_residual_norm_fwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
+                                 const float* b1, const float* res, const float* w2, const float* b2, float eps, void* S, void* Y,
+                                 float* mean1, float* inv1, float* mean2, float* inv2, void* stream);
+size_t hfta_gated_residual_norm_bwd_workspace_bytes(int B, int R, int E);
+int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
+                                 const float* b1, const float* res, const float* w2, const float* mean1, const float* inv1,
+                                 const float* mean2, const float* inv2, const void* dS, const void* dY, void* dX, void* dF, void* dG,
+                                 float* dw1, float* db1, float* dw2, float* db2, float* dres, void* workspace, size_t ws_bytes,
+                                 void* stream);
+int hfta_dropout_counter(int B, int64_t count, int dtype, const void* X, const float* p, const uint64_t* seed, const uint32_t* step,
+                         uint32_t site, void* Y, void* stream);
 
 /* ------------------------------------------------------------------------
  * Fused Adadelta over the same parameter-major arena, and the fused step learning-rate schedule

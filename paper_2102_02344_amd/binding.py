@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(HERE, "libhfta.so")
 
 F32, BF16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_LEAKY, ACT_TANH, ACT_GELU = 0, 1, 2, 3, 4
+NORM_LAYER, NORM_RMS = 0, 1
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH = 0, -1, -2, -3, -4
 
 
@@ -114,6 +115,16 @@ _SIGS = {
     "hfta_seq_logps": (_i, [_i] * 5 + [_p] * 6),
     "hfta_preference_loss_workspace_bytes": (_sz, [_i] * 3),
     "hfta_preference_loss": (_i, [_i] * 5 + [_p] * 10 + [_sz, _p]),
+    "hfta_rotary_packed": (_i, [_i] * 6 + [_p, _s4, _p, _i, _p, _i, _p, _i, _p, _i, _p, _s4, _p]),
+    "hfta_linear_attention_fwd_workspace_bytes": (_sz, [_i] * 7),
+    "hfta_linear_attention_fwd": (_i, [_i] * 7 + [_p, _s4, _p, _p, _s4, _p, _p, _f, _p, _p, _s4, _p, _p, _sz, _p]),
+    "hfta_linear_attention_bwd_workspace_bytes": (_sz, [_i] * 7),
+    "hfta_linear_attention_bwd": (_i, [_i] * 7 + [_p, _s4, _p, _p, _s4, _p, _p, _f, _p, _p, _s4, _p, _p, _s4, _p, _p, _s4, _p, _p, _sz, _p]),
+    "hfta_linear_attention_step": (_i, [_i] * 7 + [_p, _s4, _p, _p, _s4, _p, _p, _f, _p, _p, _s4, _p, _p]),
+    "hfta_gated_residual_norm_fwd": (_i, [_i] * 5 + [_p] * 8 + [_f] + [_p] * 7),
+    "hfta_gated_residual_norm_bwd_workspace_bytes": (_sz, [_i] * 3),
+    "hfta_gated_residual_norm_bwd": (_i, [_i] * 5 + [_p] * 22 + [_sz, _p]),
+    "hfta_dropout_counter": (_i, [_i, _i64, _i, _p, _p, _p, _p, C.c_uint32, _p, _p]),
     "hfta_adadelta_step_multi": (_i, [_i, _i, _s4, _i] + [_p] * 9 + [_p]),
     "hfta_steplr": (_i, [_i, _p, _p, _p, _i, _p, _p]),
     "hfta_add_sample_bias": (_i, [_i] * 5 + [_p] * 7),
@@ -795,3 +806,64 @@ def preference_loss(B, R, K, npairs, dtype, logits, labels, seq_offsets, ref_log
     _check(_lib.hfta_preference_loss(B, R, K, npairs, dtype, _ptr(logits), _ptr(labels), _ptr(seq_offsets), _ptr(ref_logps), _ptr(beta),
                                      _ptr(label_smoothing), _ptr(loss), _ptr(logps), _ptr(dlogits), wp, wb, _stream(stream)),
            "hfta_preference_loss")
+
+
+def rotary_packed(B, R, nseq, H, d, dtype, X, xs, positions, naxes, axis, pairs, freq, interleaved, seq_offsets, inverse, Y, ys, stream=None):
+    _check(_lib.hfta_rotary_packed(B, R, nseq, H, d, dtype, _ptr(X), _strides(xs, 3), _ptr(positions), naxes, _ptr(axis), pairs, _ptr(freq),
+                                   int(interleaved), _ptr(seq_offsets), int(inverse), _ptr(Y), _strides(ys, 3), _stream(stream)),
+           "rotary_packed")
+
+
+def linear_attention_fwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype) -> int:
+    return _lib.hfta_linear_attention_fwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype)
+
+
+def linear_attention_fwd(B, R, nseq, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, seq_offsets, log_decay, scale, state_in, CTX, cs, state_out=None,
+                         workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_linear_attention_fwd(B, R, nseq, Hq, Hkv, d, dtype, _ptr(Q), _strides(qs, 3), _ptr(K), _ptr(V), _strides(kvs, 3),
+                                          _ptr(seq_offsets), _ptr(log_decay), scale, _ptr(state_in), _ptr(CTX), _strides(cs, 3),
+                                          _ptr(state_out), wp, wb, _stream(stream)), "linear_attention_fwd")
+
+
+def linear_attention_bwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype) -> int:
+    return _lib.hfta_linear_attention_bwd_workspace_bytes(B, R, nseq, Hq, Hkv, d, dtype)
+
+
+def linear_attention_bwd(B, R, nseq, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, seq_offsets, log_decay, scale, state_in, dCTX, cs, dstate_out, dQ,
+                         dqs, dK, dV, dkvs, dstate_in=None, workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_linear_attention_bwd(B, R, nseq, Hq, Hkv, d, dtype, _ptr(Q), _strides(qs, 3), _ptr(K), _ptr(V), _strides(kvs, 3),
+                                          _ptr(seq_offsets), _ptr(log_decay), scale, _ptr(state_in), _ptr(dCTX), _strides(cs, 3),
+                                          _ptr(dstate_out), _ptr(dQ), _strides(dqs, 3), _ptr(dK), _ptr(dV), _strides(dkvs, 3),
+                                          _ptr(dstate_in), wp, wb, _stream(stream)), "linear_attention_bwd")
+
+
+def linear_attention_step(B, n, slots, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, slot, log_decay, scale, state, CTX, cs, new_state, stream=None):
+    _check(_lib.hfta_linear_attention_step(B, n, slots, Hq, Hkv, d, dtype, _ptr(Q), _strides(qs, 3), _ptr(K), _ptr(V), _strides(kvs, 3),
+                                           _ptr(slot), _ptr(log_decay), scale, _ptr(state), _ptr(CTX), _strides(cs, 3), _ptr(new_state),
+                                           _stream(stream)), "linear_attention_step")
+
+
+def gated_residual_norm_fwd(B, R, E, dtype, norm, X, F, G, w1, b1, res, w2, b2, eps, S, Y, mean1, inv1, mean2, inv2, stream=None):
+    _check(_lib.hfta_gated_residual_norm_fwd(B, R, E, dtype, norm, _ptr(X), _ptr(F), _ptr(G), _ptr(w1), _ptr(b1), _ptr(res), _ptr(w2), _ptr(b2),
+                                             eps, _ptr(S), _ptr(Y), _ptr(mean1), _ptr(inv1), _ptr(mean2), _ptr(inv2), _stream(stream)),
+           "gated_residual_norm_fwd")
+
+
+def gated_residual_norm_bwd_workspace_bytes(B, R, E) -> int:
+    return _lib.hfta_gated_residual_norm_bwd_workspace_bytes(B, R, E)
+
+
+def gated_residual_norm_bwd(B, R, E, dtype, norm, X, F, G, w1, b1, res, w2, mean1, inv1, mean2, inv2, dS, dY, dX, dF, dG, dw1, db1, dw2, db2,
+                            dres, workspace=None, stream=None):
+    wp, wb = _ws(workspace)
+    _check(_lib.hfta_gated_residual_norm_bwd(B, R, E, dtype, norm, _ptr(X), _ptr(F), _ptr(G), _ptr(w1), _ptr(b1), _ptr(res), _ptr(w2),
+                                             _ptr(mean1), _ptr(inv1), _ptr(mean2), _ptr(inv2), _ptr(dS), _ptr(dY), _ptr(dX), _ptr(dF), _ptr(dG),
+                                             _ptr(dw1), _ptr(db1), _ptr(dw2), _ptr(db2), _ptr(dres), wp, wb, _stream(stream)),
+           "gated_residual_norm_bwd")
+
+
+def dropout_counter(B, count, dtype, X, p, seed, step, site, Y, stream=None):
+    _check(_lib.hfta_dropout_counter(B, count, dtype, _ptr(X), _ptr(p), _ptr(seed), _ptr(step), site, _ptr(Y), _stream(stream)),
+           "dropout_counter")

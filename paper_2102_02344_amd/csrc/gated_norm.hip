@@ -1,0 +1,353 @@
+// What stands between two blocks of a decoder layer, in one call per direction (fusion rules table rows "LayerNorm" and element-wise):
+// the block's own norm, its gate and residual scale, the sum with the residual stream and the norm in front of the next block.
+//
+//   u = N(F) w1 + b1,   S = X + res sigma(G) u,   Y = N(S) w2 + b2
+//   N(z) = (z - mean z) / sqrt(var z + eps),  or  z / sqrt(mean z^2 + eps)  (RMS)
+//
+// and backwards, with sh = N(S), fh = N(F), h = sigma(G), and t of a norm with inverse deviation i: N'(t, zh, i) = i (t - mean t - zh mean(t zh)):
+//   ds = dS + N'(dY w2, sh, i2),   dX = ds,   du = res h ds,   dF = N'(du w1, fh, i1),   dG = res ds u h (1 - h)
+//   dw1 = sum du fh,  db1 = sum du,  dw2 = sum dY sh,  db2 = sum dY,  dres = sum h u ds      (sums over rows)
+//
+// Bound by memory: a row is read once and stays in registers, a thread's share of 8 or 16 elements, through both norms; a wavefront or a
+// workgroup has a row.  The backward call forms S again from X, F and G rather than read its rounded copy (as many bytes, and the
+// gradients are those of what Y was made of).  Sums over rows stay in registers across a workgroup's rows, pass through the
+// workspace and are added in order.
+#include "pieces.h"
+
+namespace hfta {
+namespace {
+
+struct GnArgs {
+  const void *X, *F, *G, *dS, *dY;
+  const float *w1, *b1, *res, *w2, *b2;
+  void *S, *Y, *dX, *dF, *dG;
+  float *m1, *i1, *m2, *i2, *part;
+  float eps;
+  int R, E, blocks;                // blocks: workgroups of a model
+  int need_db;
+};
+constexpr int GN_MAX_BLOCKS = 512;
+
+template <int TPR> struct GnSum {
+  float lds[2][2][TPR > 64 ? TPR / 64 : 1];
+};
+// two sums over the TPR threads of a row; `turn` alternates between calls, so that one barrier is enough
+template <int TPR> __device__ __forceinline__ void gn_sum(GnSum<TPR>& s, int turn, float& x, float& y) {
+  x = wave_sum(x);
+  y = wave_sum(y);
+  if constexpr (TPR > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) { s.lds[turn][0][w] = x; s.lds[turn][1][w] = y; }
+    __syncthreads();
+    x = y = 0.f;
+#pragma unroll
+    for (int i = 0; i < TPR / 64; ++i) { x += s.lds[turn][0][i]; y += s.lds[turn][1][i]; }
+  }
+}
+
+// a thread's share of a row: NP pieces, TPR pieces apart
+template <typename T, int NP, int TPR> struct GnRow {
+  typedef Piece16<T> P;
+  static constexpr int N = NP * P::N;
+  static __device__ __forceinline__ int col(int p) { return (p * TPR + (int)(threadIdx.x % TPR)) * P::N; }
+  static __device__ __forceinline__ void load(float (&x)[NP][P::N], const T* row, int E) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) P::load(x[p], row + col(p), E - col(p));
+  }
+  static __device__ __forceinline__ void store(T* row, const float (&x)[NP][P::N], int E) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) P::store(row + col(p), x[p], E - col(p));
+  }
+  // fp32 rows of weights
+  static __device__ __forceinline__ void weights(float (&x)[NP][P::N], const float* row, int E, float none) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int e = 0; e < P::N; ++e) x[p][e] = row && col(p) + e < E ? row[col(p) + e] : none;
+  }
+};
+#define GN_EACH(NP, N)                 \
+  _Pragma("unroll") for (int p = 0; p < NP; ++p) _Pragma("unroll") for (int e = 0; e < N; ++e)
+
+// the statistics of a row; x becomes x - mean where means are taken (zeros behind the row stay zeros)
+template <typename T, int NP, int TPR, bool RMS>
+__device__ __forceinline__ void gn_stats(GnSum<TPR>& sum, int& turn, float (&x)[NP][Piece16<T>::N], int E, float eps, float& mean, float& inv) {
+  typedef GnRow<T, NP, TPR> Row;
+  constexpr int N = Piece16<T>::N;
+  float s = 0.f, z = 0.f;
+  mean = 0.f;
+  if constexpr (!RMS) {
+    GN_EACH(NP, N) s += x[p][e];
+    gn_sum<TPR>(sum, turn, s, z);
+    turn ^= 1;
+    mean = s / (float)E;
+    GN_EACH(NP, N) x[p][e] = Row::col(p) + e < E ? x[p][e] - mean : 0.f;
+  }
+  s = z = 0.f;
+  GN_EACH(NP, N) s = fmaf(x[p][e], x[p][e], s);
+  gn_sum<TPR>(sum, turn, s, z);
+  turn ^= 1;
+  inv = 1.f / sqrtf(s / (float)E + eps);
+}
+
+__device__ __forceinline__ float gn_sigma(float x) { return 1.f / (1.f + expf(-x)); }
+
+template <typename T, int NP, int TPR, bool RMS, bool BLOCK>
+__global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_fwd_kernel(GnArgs a) {
+  typedef GnRow<T, NP, TPR> Row;
+  constexpr int N = Piece16<T>::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  __shared__ GnSum<TPR> sum;
+  const int b = blockIdx.y, E = a.E;
+  const int r = blockIdx.x * RPB + threadIdx.x / TPR;
+  if (r >= a.R) return;                                          // (a whole wavefront; workgroups of one row never)
+  const int64_t row = (int64_t)b * a.R + r, at = row * E;
+  int turn = 0;
+  float f[NP][N], x[NP][N];
+  Row::load(x, reinterpret_cast<const T*>(a.X) + at, E);
+  if constexpr (BLOCK) {
+    Row::load(f, reinterpret_cast<const T*>(a.F) + at, E);
+    float w[NP][N], c[NP][N], mean, inv;
+    Row::weights(w, a.w1 + (int64_t)b * E, E, 0.f);
+    Row::weights(c, a.b1 ? a.b1 + (int64_t)b * E : nullptr, E, 0.f);
+    const float res = a.res ? a.res[b] : 1.f;
+    float g[NP][N];
+    if (a.G) Row::load(g, reinterpret_cast<const T*>(a.G) + at, E);
+    gn_stats<T, NP, TPR, RMS>(sum, turn, f, E, a.eps, mean, inv);
+    if (threadIdx.x % TPR == 0) {
+      if (!RMS) a.m1[row] = mean;
+      a.i1[row] = inv;
+    }
+    GN_EACH(NP, N) {
+      const float h = a.G ? res * gn_sigma(g[p][e]) : res;
+      if (Row::col(p) + e < E) x[p][e] = fmaf(h, fmaf(f[p][e] * inv, w[p][e], c[p][e]), x[p][e]);
+    }
+    Row::store(reinterpret_cast<T*>(a.S) + at, x, E);
+  }
+  float w[NP][N], c[NP][N], mean, inv;
+  Row::weights(w, a.w2 + (int64_t)b * E, E, 0.f);
+  Row::weights(c, a.b2 ? a.b2 + (int64_t)b * E : nullptr, E, 0.f);
+  gn_stats<T, NP, TPR, RMS>(sum, turn, x, E, a.eps, mean, inv);
+  if (threadIdx.x % TPR == 0) {
+    if (!RMS) a.m2[row] = mean;
+    a.i2[row] = inv;
+  }
+  GN_EACH(NP, N) x[p][e] = fmaf(x[p][e] * inv, w[p][e], c[p][e]);
+  Row::store(reinterpret_cast<T*>(a.Y) + at, x, E);
+}
+
+// Partial sums of a workgroup's rows, in part[model][workgroup][5][E] (dw2, db2, dw1, db1, and dres in the first word of the last)
+template <typename T, int NP, int TPR, bool RMS, bool BLOCK>
+__global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs a) {
+  typedef GnRow<T, NP, TPR> Row;
+  constexpr int N = Piece16<T>::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  __shared__ GnSum<TPR> sum;
+  const int b = blockIdx.y, E = a.E;
+  const float res = BLOCK && a.res ? a.res[b] : 1.f;
+  const float *w1 = a.w1 + (int64_t)b * E, *b1 = a.b1 ? a.b1 + (int64_t)b * E : nullptr, *w2 = a.w2 + (int64_t)b * E;
+  float dw1[NP][N], db1[NP][N], dw2[NP][N], db2[NP][N], dres = 0.f;
+  GN_EACH(NP, N) dw1[p][e] = db1[p][e] = dw2[p][e] = db2[p][e] = 0.f;
+  const int part = blockIdx.x * RPB + threadIdx.x / TPR, parts = a.blocks * RPB;
+  int turn = 0;
+  for (int r = part; r < a.R; r += parts) {
+    const int64_t row = (int64_t)b * a.R + r, at = row * E;
+    float x[NP][N], f[NP][N], g[NP][N], dy[NP][N], ds[NP][N], w[NP][N], u[NP][N];
+    Row::load(x, reinterpret_cast<const T*>(a.X) + at, E);
+    if constexpr (BLOCK) {
+      Row::load(f, reinterpret_cast<const T*>(a.F) + at, E);
+      if (a.G) Row::load(g, reinterpret_cast<const T*>(a.G) + at, E);
+    }
+    Row::load(dy, reinterpret_cast<const T*>(a.dY) + at, E);
+    if (a.dS) Row::load(ds, reinterpret_cast<const T*>(a.dS) + at, E);
+    const float i2 = a.i2[row], m2 = RMS ? 0.f : a.m2[row];
+    float i1 = 0.f;
+    if constexpr (BLOCK) {
+      i1 = a.i1[row];
+      const float m1 = RMS ? 0.f : a.m1[row];
+      float c[NP][N];
+      Row::weights(w, w1, E, 0.f);
+      Row::weights(c, b1, E, 0.f);
+      GN_EACH(NP, N) {
+        f[p][e] = Row::col(p) + e < E ? (f[p][e] - m1) * i1 : 0.f;
+        u[p][e] = fmaf(f[p][e], w[p][e], c[p][e]);
+        g[p][e] = a.G ? gn_sigma(g[p][e]) : 1.f;
+        x[p][e] = fmaf(res * g[p][e], u[p][e], x[p][e]);
+      }
+    }
+    float s = 0.f, z = 0.f;
+    float v[NP][N];
+    Row::weights(v, w2, E, 0.f);
+    GN_EACH(NP, N) {
+      x[p][e] = Row::col(p) + e < E ? (x[p][e] - m2) * i2 : 0.f;
+      dw2[p][e] = fmaf(dy[p][e], x[p][e], dw2[p][e]);
+      if (a.need_db) db2[p][e] += dy[p][e];
+      dy[p][e] *= v[p][e];
+      s = fmaf(dy[p][e], x[p][e], s);
+      if (!RMS) z += dy[p][e];
+    }
+    gn_sum<TPR>(sum, turn, s, z);
+    turn ^= 1;
+    s /= (float)E;
+    z /= (float)E;
+    GN_EACH(NP, N) ds[p][e] = i2 * (dy[p][e] - z - x[p][e] * s) + (a.dS ? ds[p][e] : 0.f);
+    Row::store(reinterpret_cast<T*>(a.dX) + at, ds, E);
+    if constexpr (BLOCK) {
+      s = z = 0.f;
+      GN_EACH(NP, N) {
+        const float hd = Row::col(p) + e < E ? g[p][e] * ds[p][e] : 0.f, du = res * hd;      // (z makes ds not zero behind the row)
+        dres = fmaf(hd, u[p][e], dres);
+        dw1[p][e] = fmaf(du, f[p][e], dw1[p][e]);
+        if (a.need_db) db1[p][e] += du;
+        if (a.G) g[p][e] = du * u[p][e] * (1.f - g[p][e]);       // dG
+        dy[p][e] = du * w[p][e];
+        s = fmaf(dy[p][e], f[p][e], s);
+        if (!RMS) z += dy[p][e];
+      }
+      if (a.G) Row::store(reinterpret_cast<T*>(a.dG) + at, g, E);
+      gn_sum<TPR>(sum, turn, s, z);
+      turn ^= 1;
+      s /= (float)E;
+      z /= (float)E;
+      GN_EACH(NP, N) dy[p][e] = i1 * (dy[p][e] - z - f[p][e] * s);
+      Row::store(reinterpret_cast<T*>(a.dF) + at, dy, E);
+    }
+  }
+  float* out = a.part + ((int64_t)b * parts + part) * (4 * (int64_t)E + 4);
+  GN_EACH(NP, N) {
+    const int c = Row::col(p) + e;
+    if (c < E) {
+      out[c] = dw2[p][e];
+      if (a.need_db) out[E + c] = db2[p][e];
+      if constexpr (BLOCK) {
+        out[2 * (int64_t)E + c] = dw1[p][e];
+        if (a.need_db) out[3 * (int64_t)E + c] = db1[p][e];
+      }
+    }
+  }
+  if constexpr (BLOCK) {
+    if constexpr (TPR > 64) {
+      float none = 0.f;
+      gn_sum<TPR>(sum, turn, dres, none);
+    } else {
+      dres = wave_sum(dres);
+    }
+    if (threadIdx.x % TPR == 0) out[4 * (int64_t)E] = dres;
+  }
+}
+
+// The parts of a model added in order: four threads of a column take a quarter of them each
+__global__ __launch_bounds__(256) void gn_add_kernel(const float* part, int parts, int E, float* dw2, float* db2, float* dw1, float* db1, float* dres) {
+  __shared__ double lds[4][64];
+  const int b = blockIdx.y, q = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t width = 4 * (int64_t)E + 4, c = (int64_t)blockIdx.x * 64 + lane;
+  const float* src = part + (int64_t)b * parts * width;
+  const int which = c < 4 * (int64_t)E ? (int)(c / E) : 4;
+  float* out = which == 0 ? dw2 : which == 1 ? db2 : which == 2 ? dw1 : which == 3 ? db1 : dres;
+  const bool has = out && c <= 4 * (int64_t)E;
+  double s = 0.0;
+  if (has)
+    for (int i = q; i < parts; i += 4) s += (double)src[i * width + c];
+  lds[q][lane] = s;
+  __syncthreads();
+  if (has && q == 0) {
+    const float x = (float)((lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]));
+    if (which < 4) out[(int64_t)b * E + (c - which * (int64_t)E)] = x;
+    else out[b] = x;
+  }
+}
+
+constexpr int GN_MAX_E = 16384;
+int gn_rows(int E) { return E <= 512 ? 4 : 1; }                  // rows of a workgroup
+int gn_blocks(int B, int R, int E) {
+  const int rows = (R + gn_rows(E) - 1) / gn_rows(E);
+  int most = 1024 / B;
+  if (most < 32) most = 32;
+  if (most > GN_MAX_BLOCKS) most = GN_MAX_BLOCKS;
+  return rows < most ? rows : most;
+}
+
+int gn_check(int B, int R, int E, int dtype, int norm) {
+  if (B <= 0 || R <= 0 || E <= 0 || !valid_dtype(dtype) || (norm != HFTA_NORM_RMS && norm != HFTA_NORM_LAYER)) return HFTA_EINVAL;
+  return E > GN_MAX_E || B > 65535 || R > 0x7fffffff - 4096 || (R + gn_rows(E) - 1) / gn_rows(E) > 0x3fffff ? HFTA_EUNSUPPORTED : HFTA_OK;
+}
+
+// elements of a thread and threads of a row
+#define GN_LAUNCH(kernel, EL, TPR) \
+  hipLaunchKernelGGL((kernel<T, EL / Piece16<T>::N, TPR, RMS, BLOCK>), grid, dim3(TPR == 64 ? 256 : TPR), 0, st, a)
+#define GN_FORMS(kernel)                                 \
+  if (a.E <= 512) GN_LAUNCH(kernel, 8, 64);              \
+  else if (a.E <= 1024) GN_LAUNCH(kernel, 8, 128);       \
+  else if (a.E <= 2048) GN_LAUNCH(kernel, 8, 256);       \
+  else if (a.E <= 4096) GN_LAUNCH(kernel, 8, 512);       \
+  else if (a.E <= 8192) GN_LAUNCH(kernel, 8, 1024);      \
+  else GN_LAUNCH(kernel, 16, 1024);                      \
+  return launch_status();
+
+template <typename T, bool RMS, bool BLOCK> int gn_fwd(const GnArgs& a, int B, hipStream_t st) {
+  const dim3 grid((unsigned)((a.R + gn_rows(a.E) - 1) / gn_rows(a.E)), (unsigned)B);
+  GN_FORMS(gn_fwd_kernel)
+}
+template <typename T, bool RMS, bool BLOCK> int gn_bwd(const GnArgs& a, int B, hipStream_t st) {
+  const dim3 grid((unsigned)a.blocks, (unsigned)B);
+  GN_FORMS(gn_bwd_kernel)
+}
+#define GN_PICK(fn, a, B, st)                                                                                                \
+  (dtype == HFTA_BF16 ? (norm == HFTA_NORM_RMS ? (F ? fn<bf16_raw, true, true>(a, B, st) : fn<bf16_raw, true, false>(a, B, st))    \
+                                               : (F ? fn<bf16_raw, false, true>(a, B, st) : fn<bf16_raw, false, false>(a, B, st))) \
+                      : (norm == HFTA_NORM_RMS ? (F ? fn<float, true, true>(a, B, st) : fn<float, true, false>(a, B, st))          \
+                                               : (F ? fn<float, false, true>(a, B, st) : fn<float, false, false>(a, B, st))))
+
+}  // namespace
+}  // namespace hfta
+
+using namespace hfta;
+
+extern "C" {
+
+int hfta_gated_residual_norm_fwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
+                                 const float* b1, const float* res, const float* w2, const float* b2, float eps, void* S, void* Y,
+                                 float* mean1, float* inv1, float* mean2, float* inv2, void* stream) {
+  const int rc = gn_check(B, R, E, dtype, norm);
+  const bool means = norm == HFTA_NORM_LAYER;
+  if (rc == HFTA_EINVAL || !X || !w2 || !Y || !inv2 || !(eps >= 0.f) || (means && !mean2)) return HFTA_EINVAL;
+  if (F ? (!w1 || !S || !inv1 || (means && !mean1)) : (G || w1 || b1 || res || S)) return HFTA_EINVAL;
+  if (rc != HFTA_OK) return rc;
+  GnArgs a{};
+  a.X = X; a.F = F; a.G = G; a.w1 = w1; a.b1 = b1; a.res = res; a.w2 = w2; a.b2 = b2; a.eps = eps; a.S = S; a.Y = Y;
+  a.m1 = mean1; a.i1 = inv1; a.m2 = mean2; a.i2 = inv2; a.R = R; a.E = E;
+  return GN_PICK(gn_fwd, a, B, as_stream(stream));
+}
+
+size_t hfta_gated_residual_norm_bwd_workspace_bytes(int B, int R, int E) {
+  if (gn_check(B, R, E, HFTA_F32, HFTA_NORM_RMS) != HFTA_OK) return 0;
+  return (size_t)B * gn_blocks(B, R, E) * gn_rows(E) * (4 * (size_t)E + 4) * sizeof(float);
+}
+
+int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
+                                 const float* b1, const float* res, const float* w2, const float* mean1, const float* inv1,
+                                 const float* mean2, const float* inv2, const void* dS, const void* dY, void* dX, void* dF, void* dG,
+                                 float* dw1, float* db1, float* dw2, float* db2, float* dres, void* workspace, size_t ws_bytes,
+                                 void* stream) {
+  const int rc = gn_check(B, R, E, dtype, norm);
+  const bool means = norm == HFTA_NORM_LAYER;
+  if (rc == HFTA_EINVAL || !X || !w2 || !inv2 || !dY || !dX || !dw2 || (means && !mean2)) return HFTA_EINVAL;
+  if (F ? (!w1 || !inv1 || (means && !mean1) || !dF || !dw1 || (!G != !dG) || (!b1 != !db1) || (!res && dres))
+        : (G || w1 || b1 || res || dF || dG || dw1 || db1 || dres))
+    return HFTA_EINVAL;
+  if (rc != HFTA_OK) return rc;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 4 || ws_bytes < hfta_gated_residual_norm_bwd_workspace_bytes(B, R, E))
+    return HFTA_EWORKSPACE;
+  GnArgs a{};
+  a.X = X; a.F = F; a.G = G; a.w1 = w1; a.b1 = b1; a.res = res; a.w2 = w2; a.dS = dS; a.dY = dY; a.dX = dX; a.dF = dF; a.dG = dG;
+  a.m1 = const_cast<float*>(mean1); a.i1 = const_cast<float*>(inv1); a.m2 = const_cast<float*>(mean2); a.i2 = const_cast<float*>(inv2);
+  a.R = R; a.E = E; a.part = reinterpret_cast<float*>(workspace);
+  a.blocks = gn_blocks(B, R, E);
+  a.need_db = db1 || db2;
+  hipStream_t st = as_stream(stream);
+  const int r = GN_PICK(gn_bwd, a, B, st);
+  if (r != HFTA_OK) return r;
+  const dim3 grid((unsigned)((4 * (int64_t)E + 1 + 63) / 64), (unsigned)B);
+  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(256), 0, st, a.part, a.blocks * gn_rows(E), E, dw2, db2, dw1, db1, dres);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,168 @@
+"""The plain 64-bit forms that the operators of a decoder layer with a recurrent memory are tested against: gradients are the
+formula's, autograd's and what differences give, the generator gives its published words.  And the operators' refusals, which come
+before any launch (no GPU)."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import decoder_ref as dr
+
+ONE = C.c_void_p(256)
+S3 = (C.c_int64 * 3)(1, 2, 3)
+T3 = (C.c_int64 * 3)(1, 2, 4)
+
+
+def _normal(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def test_linear_attention_is_the_recurrence_and_its_derivative():
+    B, R, Hq, Hkv, d, nseq = 2, 13, 4, 2, 3, 4
+    off = dr.offsets([[4, 0, 1, 6], [2, 9, 0, 1]], 1)
+    x = [_normal(i, *s) for i, s in enumerate(((B, R, Hq, d), (B, R, Hkv, d), (B, R, Hkv, d), (B, nseq, Hkv, d, d)))]
+    dctx, dsf = _normal(7, B, R, Hq, d), _normal(8, B, nseq, Hkv, d, d)
+    ld = -torch.rand(B, Hkv, generator=torch.Generator().manual_seed(9), dtype=torch.float64) * 2
+    ref = dr.linear_attention(x[0], x[1], x[2], off, ld, 0.7, x[3], dctx, dsf)
+
+    def total(q, k, v, s0):
+        loss = 0.0
+        for b in range(B):
+            for i in range(nseq):
+                for h in range(Hkv):
+                    S = s0[b, i, h]
+                    for t in range(int(off[b, i]), int(off[b, i + 1])):
+                        S = torch.exp(ld[b, h]) * S + torch.outer(k[b, t, h], v[b, t, h])
+                        for g in range(2 * h, 2 * h + 2):
+                            o = 0.7 * q[b, t, g] @ S
+                            assert float((o - ref["ctx"][b, t, g]).abs().max()) < 1e-12
+                            loss = loss + (o * dctx[b, t, g]).sum()
+                    assert float((S - ref["state"][b, i, h]).abs().max()) < 1e-12
+                    loss = loss + (S * dsf[b, i, h]).sum()
+        return loss
+    y = [t.clone().requires_grad_() for t in x]
+    total(*y).backward()
+    for n, t in zip(("dq", "dk", "dv", "ds0"), y):
+        assert float((ref[n] - t.grad).abs().max()) < 1e-12, n
+    # differences: the value is linear in each argument by itself, so that a step of 1e-3 is off by rounding alone
+    val = lambda q, k, v, s0: float(sum((a * b).sum() for a, b in zip((lambda r: (r["ctx"], r["state"]))(
+        dr.linear_attention(q, k, v, off, ld, 0.7, s0)), (dctx, dsf))))
+    for n, i in (("dq", 0), ("dk", 1), ("dv", 2), ("ds0", 3)):
+        for at in torch.randperm(x[i].numel(), generator=torch.Generator().manual_seed(5))[:20].tolist():
+            step = torch.zeros(x[i].numel(), dtype=torch.float64)
+            step[at] = 1e-3
+            step = step.view_as(x[i])
+            up, dn = (val(*[t + sg * step if j == i else t for j, t in enumerate(x)]) for sg in (1, -1))
+            assert abs(float(ref[n].reshape(-1)[at]) - (up - dn) / 2e-3) < 1e-9
+
+
+def test_rotary_inverse_is_the_gradient():
+    B, R, H, d, pairs = 2, 5, 3, 10, 4
+    x, g = _normal(1, B, R, H, d), _normal(2, B, R, H, d)
+    pos = torch.randint(0, 1000, (B, R, 2), generator=torch.Generator().manual_seed(3))
+    axis, freq = torch.tensor([0, 1, 1, 0]), torch.rand(B, pairs, generator=torch.Generator().manual_seed(4))
+    rows = torch.ones(B, R, dtype=torch.bool)
+    for inter in (False, True):
+        y = x.clone().requires_grad_()
+        (dr.rotary(y, pos, axis, freq, inter, rows)[0] * g).sum().backward()
+        assert float((dr.rotary(g, pos, axis, freq, inter, rows, inverse=True)[0] - y.grad).abs().max()) < 1e-13
+
+
+def test_philox_words():
+    """Known answers of the generator's authors (Random123, kat_vectors: philox4x32, 10 rounds)."""
+    w = dr.philox(np.array([[0, 0, 0, 0]]), (0, 0))[0]
+    assert [hex(int(v)) for v in w] == ["0x6627e8d5", "0xe169c58d", "0xbc57ac4c", "0x9b00dbd8"]
+    f = 0xffffffff
+    w = dr.philox(np.array([[f, f, f, f]], dtype=np.uint64), (f, f))[0]
+    assert [hex(int(v)) for v in w] == ["0x408f276d", "0x41c83b0e", "0xa20bc7c6", "0x6d5451fd"]
+    w = dr.philox(np.array([[0x243f6a88, 0x85a308d3, 0x13198a2e, 0x03707344]], dtype=np.uint64), (0xa4093822, 0x299f31d0))[0]
+    assert [hex(int(v)) for v in w] == ["0xd16cfe09", "0x94fdcceb", "0x5001e420", "0x24126ea1"]
+
+
+# ------------------------------------------------------------------ refusals
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2102_02344_amd import binding
+    return binding
+
+
+def test_rotary_refusals(lib):
+    def call(B=1, R=8, nseq=1, H=2, d=8, dtype=1, X=ONE, xs=S3, pos=ONE, naxes=2, axis=ONE, pairs=4, freq=ONE, off=ONE, Y=C.c_void_p(512), ys=S3):
+        return lib.raw().hfta_rotary_packed(B, R, nseq, H, d, dtype, X, xs, pos, naxes, axis, pairs, freq, 0, off, 0, Y, ys, None)
+    for bad in (dict(B=0), dict(R=0), dict(R=0x7fffffff), dict(nseq=0), dict(H=0), dict(d=0), dict(dtype=3), dict(X=None), dict(xs=None),
+                dict(naxes=0), dict(pos=None), dict(axis=None), dict(pairs=0), dict(pairs=5), dict(freq=None), dict(Y=None), dict(ys=None),
+                dict(Y=ONE, ys=T3)):
+        assert call(**bad) == lib.EINVAL, bad
+    for bad in (dict(B=65536), dict(nseq=1 << 24), dict(R=0x7ffffe00, d=1024, pairs=512)):
+        assert call(**bad) == lib.EUNSUPPORTED, bad
+
+
+def test_linear_attention_refusals(lib):
+    def size(o):
+        return [o.get(n, v) for n, v in dict(B=2, R=64, nseq=3, Hq=4, Hkv=2, d=16, dtype=1).items()]
+
+    def fwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, ctx=ONE, cs=S3, ws=ONE, wb=1 << 40, **o):
+        return lib.raw().hfta_linear_attention_fwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, None, ctx, cs, None, ws, wb, None)
+
+    def bwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, dctx=ONE, cs=S3, dQ=ONE, dqs=S3, dK=ONE, dV=ONE, dkvs=S3, ws=ONE,
+            wb=1 << 40, **o):
+        return lib.raw().hfta_linear_attention_bwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, None, dctx, cs, None, dQ, dqs, dK, dV, dkvs, None,
+                                                   ws, wb, None)
+    sizes = [dict(B=0), dict(R=0), dict(R=0x7fffffff), dict(nseq=0), dict(Hq=0), dict(Hq=3), dict(Hkv=0), dict(d=0), dict(dtype=2)]
+    more = [dict(Q=None), dict(qs=None), dict(K=None), dict(V=None), dict(kvs=None), dict(off=None), dict(ld=None), dict(scale=0.0),
+            dict(scale=-1.0), dict(scale=math.nan), dict(scale=1e-40), dict(cs=None)]
+    for bad in sizes + more + [dict(ctx=None)]:
+        assert fwd(**bad) == lib.EINVAL, bad
+    for bad in sizes + more + [dict(dctx=None), dict(dQ=None), dict(dqs=None), dict(dK=None), dict(dV=None), dict(dkvs=None)]:
+        assert bwd(**bad) == lib.EINVAL, bad
+    for bad in (dict(d=129), dict(nseq=1 << 24), dict(B=65536)):
+        assert fwd(**bad) == lib.EUNSUPPORTED and bwd(**bad) == lib.EUNSUPPORTED, bad
+
+
+def test_linear_attention_step_refusals(lib):
+    def call(B=2, n=4, slots=8, Hq=4, Hkv=2, d=16, dtype=1, Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, slot=ONE, ld=ONE, scale=1.0, state=ONE, ctx=ONE,
+             cs=S3, new=ONE):
+        return lib.raw().hfta_linear_attention_step(B, n, slots, Hq, Hkv, d, dtype, Q, qs, K, V, kvs, slot, ld, scale, state, ctx, cs, new, None)
+    for bad in (dict(B=0), dict(n=0), dict(slots=0), dict(Hq=0), dict(Hq=3), dict(Hkv=0), dict(d=0), dict(dtype=5), dict(Q=None), dict(qs=None),
+                dict(K=None), dict(V=None), dict(kvs=None), dict(ld=None), dict(scale=math.inf), dict(scale=math.nan), dict(state=None),
+                dict(ctx=None), dict(cs=None), dict(new=None), dict(slot=None, n=9)):
+        assert call(**bad) == lib.EINVAL, bad
+    for bad in (dict(d=129), dict(B=65536), dict(n=1 << 23, slots=1 << 23)):
+        assert call(**bad) == lib.EUNSUPPORTED, bad
+
+
+def test_gated_norm_refusals(lib):
+    F = dict(F=ONE, G=ONE, w1=ONE, b1=ONE, res=ONE, S=ONE, m1=ONE, i1=ONE)
+
+    def fwd(B=2, R=8, E=32, dtype=1, norm=0, X=ONE, w2=ONE, b2=ONE, eps=1e-5, Y=ONE, m2=ONE, i2=ONE, **o):
+        o = {**F, **o}
+        return lib.raw().hfta_gated_residual_norm_fwd(B, R, E, dtype, norm, X, o["F"], o["G"], o["w1"], o["b1"], o["res"], w2, b2, eps, o["S"], Y,
+                                                      o["m1"], o["i1"], m2, i2, None)
+
+    def bwd(B=2, R=8, E=32, dtype=1, norm=0, X=ONE, w2=ONE, m2=ONE, i2=ONE, dS=ONE, dY=ONE, dX=ONE, dF=ONE, dG=ONE, dw1=ONE, db1=ONE, dw2=ONE,
+            db2=ONE, dres=ONE, ws=ONE, wb=1 << 40, **o):
+        o = {**F, **o}
+        return lib.raw().hfta_gated_residual_norm_bwd(B, R, E, dtype, norm, X, o["F"], o["G"], o["w1"], o["b1"], o["res"], w2, o["m1"], o["i1"],
+                                                      m2, i2, dS, dY, dX, dF, dG, dw1, db1, dw2, db2, dres, ws, wb, None)
+    both = [dict(B=0), dict(R=0), dict(E=0), dict(dtype=7), dict(norm=2), dict(X=None), dict(w2=None), dict(m2=None), dict(i2=None), dict(w1=None),
+            dict(m1=None), dict(i1=None), dict(F=None)]
+    for bad in both + [dict(eps=-1.0), dict(eps=math.nan), dict(S=None), dict(Y=None)]:
+        assert fwd(**bad) == lib.EINVAL, bad
+    for bad in both + [dict(dY=None), dict(dX=None), dict(dF=None), dict(dG=None), dict(G=None), dict(dw1=None), dict(db1=None), dict(b1=None),
+                       dict(dw2=None), dict(res=None)]:
+        assert bwd(**bad) == lib.EINVAL, bad
+    for call in (fwd, bwd):
+        assert call(E=16385) == lib.EUNSUPPORTED and call(B=65536) == lib.EUNSUPPORTED
+    need = lib.gated_residual_norm_bwd_workspace_bytes(2, 8, 32)
+    assert need > 0
+    assert bwd(wb=need - 1) == lib.EWORKSPACE and bwd(ws=None) == lib.EWORKSPACE and bwd(ws=C.c_void_p(258)) == lib.EWORKSPACE
+
+
+def test_dropout_refusals(lib):
+    def call(B=2, count=8, dtype=1, X=ONE, p=ONE, seed=ONE, Y=ONE):
+        return lib.raw().hfta_dropout_counter(B, count, dtype, X, p, seed, None, 0, Y, None)
+    for bad in (dict(B=0), dict(count=0), dict(count=1 << 62), dict(dtype=2), dict(X=None), dict(p=None), dict(seed=None), dict(Y=None)):
+        assert call(**bad) == lib.EINVAL, bad
+    assert call(B=65536) == lib.EUNSUPPORTED
