@@ -733,9 +733,9 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
  *   lambda = exp(log_decay[b][h]) (fp32 [B][Hkv], device; -infinity: no memory; above 0 counts as 0), scale > 0 with a finite inverse
  *   (EINVAL).  Heads, strides and alignment as in attention_packed, d <= 128 (EUNSUPPORTED).  In front of sequence s a state is
  *   state_in[b][s][h] (fp32 [B][nseq][Hkv][d][d]; NULL: zeros), behind it state_out[b][s][h] (NULL: not wanted; an empty sequence's
- *   state_in).  state_out may be state_in itself.  bwd: gradients of Q, K, V from the same state_in and, where state_out is used
- *   further, its gradient dstate_out (or NULL); dstate_in (or NULL) gets the gradient of state_in, and may be dstate_out itself.  log_decay is a
- *   hyper-parameter without a gradient.  Workspaces *_workspace_bytes, 16-byte aligned (EWORKSPACE); one for the most rows and sequences serves
+ *   state_in); state_out may not overlap state_in (EINVAL where it is state_in).  bwd: gradients of Q, K, V from the same state_in and, where state_out is used
+ *   further, its gradient dstate_out (or NULL); dstate_in (or NULL) gets the gradient of state_in, and may not overlap dstate_out (EINVAL).
+ *   log_decay is a hyper-parameter without a gradient.  Workspaces *_workspace_bytes, 16-byte aligned (EWORKSPACE); one for the most rows and sequences serves
  *   every smaller batch.  A value that is not finite reaches the rows that see it, as an infinity or a NaN, and no others.
  *   States and sums are fp32.
  * linear_attention_step: one token of each of n rows: Q, CTX [Hq], K, V [Hkv] heads at s[0] b + s[1] i + s[2] h + c, the state of row i in place

@@ -1,87 +1,57 @@
-// Linear attention with a decay for each key head over packed sequences:
-//
-//   S_t = lambda S_t-1 + k_t v_t^T,   ctx_t = scale q_t S_t            lambda = exp(log_decay), S in front of a sequence: state_in, or zeros
-//
-// Forward and backward are sums of one form, f(A, B, C)_t = sum_{s <= t} lambda^(t-s) (a_t . b_s) c_s, taken from the first row to the last or back:
-//   ctx = scale f(q, k, v);   dq = scale f(dctx, v, k);   from the last row: dv = scale f(k, q, dctx), dk = scale f(v, dctx, q), over a group's heads
-// A workgroup walks one sequence of one head with the state in LDS, a thread a column of it.
-#include "packed_rows.h"
-
-#include <math.h>
+// Linear attention with decays over packed sequences: the entry points (linear_attention.h).
+#include "linear_attention.h"
 
 namespace hfta {
 namespace {
 
-struct LaStr { int64_t b, r, h; };
-struct LaJob {
-  const void *A, *B, *C;
-  void* O;
-  LaStr as, bs, cs, os;
-  const float* S0;
-  float* S1;
-  int rev, flip;                   // flip: the state's rows and columns change places in memory
-};
-struct LaArgs {
-  LaJob job[3];
-  const int32_t* off;
-  const float* ld;
-  int R, nseq, Hq, Hkv, d;
-  float scale;
-};
-
-template <typename T> __global__ __launch_bounds__(128) void la_walk_kernel(LaArgs a, int jobs) {
-  __shared__ float S[128 * 129], sa[128], sb[128], sc[128];
-  const int c = threadIdx.x, d = a.d, G = a.Hq / a.Hkv;
-  const int j = blockIdx.z, b = blockIdx.y, hk = blockIdx.x % a.Hkv, s = blockIdx.x / a.Hkv;
-  const LaJob& J = a.job[j];
-  const int32_t* off = a.off + (int64_t)b * (a.nseq + 1);
-  const int lo = min(max(off[s], 0), a.R), hi = min(max(off[s + 1], lo), a.R);
-  const float g = a.ld[(int64_t)b * a.Hkv + hk], lambda = expf(g > 0.f ? 0.f : g);
-  const int64_t at = (((int64_t)b * a.nseq + s) * a.Hkv + hk) * d * d;
-  for (int i = c; i < d * d; i += 128) S[(i / d) * 129 + i % d] = J.S0 ? J.flip ? J.S0[at + (i % d) * d + i / d] : J.S0[at + i] : 0.f;
-  __syncthreads();
-  for (int n = 0; n < hi - lo; ++n) {
-    const int r = J.rev ? hi - 1 - n : lo + n;
-    const int heads_b = J.rev ? G : 1, heads_a = J.rev ? 1 : G;
-    // forward, the state decays before a row is added; backward, S0 is the gradient of the state behind the last row
-    if (c < d && (!J.rev || n > 0))
-      for (int i = 0; i < d; ++i) S[i * 129 + c] *= lambda;
-    for (int h = 0; h < heads_b; ++h) {
-      __syncthreads();
-      const int hb = J.rev ? hk * G + h : hk;
-      if (c < d) {
-        sb[c] = Elem<T>::load(reinterpret_cast<const T*>(J.B) + b * J.bs.b + r * J.bs.r + hb * J.bs.h + c) * (J.rev ? a.scale : 1.f);
-        sc[c] = Elem<T>::load(reinterpret_cast<const T*>(J.C) + b * J.cs.b + r * J.cs.r + hb * J.cs.h + c);
-      }
-      __syncthreads();
-      if (c < d)
-        for (int i = 0; i < d; ++i) S[i * 129 + c] = fmaf(sb[i], sc[c], S[i * 129 + c]);
-    }
-    for (int h = 0; h < heads_a; ++h) {
-      __syncthreads();
-      const int ha = J.rev ? hk : hk * G + h;
-      if (c < d) sa[c] = Elem<T>::load(reinterpret_cast<const T*>(J.A) + b * J.as.b + r * J.as.r + ha * J.as.h + c);
-      __syncthreads();
-      if (c < d && J.O) {
-        float o = 0.f;
-        for (int i = 0; i < d; ++i) o = fmaf(sa[i], S[i * 129 + c], o);
-        Elem<T>::store(reinterpret_cast<T*>(J.O) + b * J.os.b + r * J.os.r + ha * J.os.h + c, J.rev ? o : a.scale * o);
-      }
-    }
-  }
-  __syncthreads();
-  if (J.S1)
-    for (int i = c; i < d * d; i += 128) {
-      const float x = S[(i / d) * 129 + i % d] * (J.rev && hi > lo ? lambda : 1.f);
-      J.S1[J.flip ? at + (i % d) * d + i / d : at + i] = x;
-    }
-}
-
-LaStr la_str(const int64_t* s) { return LaStr{s[0], s[1], s[2]}; }
-
 int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || R > 0x7fffffff - 4096) return HFTA_EINVAL;
-  return d > 128 || nseq > PACKED_MAX || B > 65535 || (int64_t)nseq * Hkv > 0xffffff ? HFTA_EUNSUPPORTED : HFTA_OK;
+  // (a launch has fewer than 2^32 threads: three jobs, a workgroup for each head and tile at most)
+  return d > 128 || nseq > PACKED_MAX || B > 65535 || (int64_t)B * Hq > 0x3fffff / ((R + LA_T - 1) / LA_T) ? HFTA_EUNSUPPORTED : HFTA_OK;
+}
+// Blocks of tiles: about LA_WANT of all heads together.  With R their number only grows, so that the workspace for the most rows serves fewer.
+constexpr int LA_WANT = 512, LA_SCAN = 8;
+int64_t la_limit(int B, int Hkv) { return (int64_t)B * Hkv < LA_WANT ? LA_WANT / ((int64_t)B * Hkv) : 1; }
+void la_cut(LaArgs& a) {
+  const int64_t most = la_limit(a.B, a.Hkv);
+  a.tiles = (a.R + LA_T - 1) / LA_T;
+  a.per = (int)((a.tiles + most - 1) / most);
+  a.blocks = (a.tiles + a.per - 1) / a.per;
+  a.scanned = a.blocks > LA_SCAN;
+}
+size_t la_workspace(int B, int R, int Hkv, int d, int jobs) {
+  const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hkv), n = tiles < most ? tiles : most;
+  if (n == 1) return 0;
+  const int64_t D = la_pad(d);
+  return (size_t)(jobs * n * B * Hkv * D * D * 4 + (jobs * n * B * 4 + 15) / 16 * 16);
+}
+void la_place(LaArgs& a, void* workspace) {
+  if (a.blocks == 1) return;
+  const int64_t D = la_pad(a.d);
+  a.sums = reinterpret_cast<float*>(workspace);
+  a.spans = reinterpret_cast<int*>(a.sums + (int64_t)a.jobs * a.blocks * a.B * a.Hkv * D * D);
+}
+bool la_ws_ok(void* workspace, size_t have, size_t need) { return need == 0 || (workspace && reinterpret_cast<uintptr_t>(workspace) % 16 == 0 && have >= need); }
+PkStr la_str(const int64_t* s) { return PkStr{s[0], s[1], s[2]}; }
+// rows in whole 16-byte pieces: pointers, strides and head widths
+bool la_vec(const LaArgs& a, int dtype, const void* const* p, int n) {
+  const int64_t m = dtype == HFTA_BF16 ? 8 : 4;
+  uintptr_t bits = 0;
+  for (int i = 0; i < n; ++i) bits |= reinterpret_cast<uintptr_t>(p[i]);
+  bool vec = a.d % m == 0 && bits % 16 == 0;
+  for (int j = 0; j < a.jobs; ++j) {
+    const PkStr* s[] = {&a.job[j].as, &a.job[j].bs, &a.job[j].cs, &a.job[j].os};
+    for (const PkStr* x : s) vec = vec && x->b % m == 0 && x->r % m == 0 && x->h % m == 0 && x->r >= 0 && x->r <= PK_LD_MAX;
+  }
+  return vec;
+}
+int la_run(const LaArgs& a, int dtype, bool vec, hipStream_t st) {
+  const LaForm f{dtype == HFTA_BF16, vec};
+  if (a.blocks > 1) {
+    const int rc = la_states(a, f, st);
+    if (rc != HFTA_OK) return rc;
+  }
+  return la_main(a, f, st);
 }
 
 }  // namespace
@@ -91,24 +61,31 @@ using namespace hfta;
 
 extern "C" {
 
-size_t hfta_linear_attention_fwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) { return 0; }
-size_t hfta_linear_attention_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) { return 0; }
+size_t hfta_linear_attention_fwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
+  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 1) : 0;
+}
+size_t hfta_linear_attention_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
+  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 3) : 0;
+}
 
 int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3], const void* K,
                               const void* V, const int64_t kvs[3], const int32_t* seq_offsets, const float* log_decay, float scale,
                               const float* state_in, void* CTX, const int64_t cs[3], float* state_out, void* workspace, size_t ws_bytes,
                               void* stream) {
   const int rc = la_check(B, R, nseq, Hq, Hkv, d, dtype);
-  if (rc == HFTA_EINVAL || !Q || !qs || !K || !V || !kvs || !seq_offsets || !log_decay || !(scale > 0.f) || !isfinite(1.f / scale) || !CTX || !cs)
+  if (rc == HFTA_EINVAL || !Q || !qs || !K || !V || !kvs || !seq_offsets || !log_decay || !(scale > 0.f) || !isfinite(1.f / scale) || !CTX || !cs ||
+      (state_out && state_out == state_in))
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
+  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 1))) return HFTA_EWORKSPACE;
   LaArgs a{};
-  a.off = seq_offsets; a.ld = log_decay; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.scale = scale;
-  a.job[0] = LaJob{Q, K, V, CTX, la_str(qs), la_str(kvs), la_str(kvs), la_str(cs), state_in, state_out, 0, 0};
-  const dim3 grid((unsigned)(nseq * Hkv), (unsigned)B, 1);
-  if (dtype == HFTA_BF16) hipLaunchKernelGGL(la_walk_kernel<bf16_raw>, grid, dim3(128), 0, as_stream(stream), a, 1);
-  else hipLaunchKernelGGL(la_walk_kernel<float>, grid, dim3(128), 0, as_stream(stream), a, 1);
-  return launch_status();
+  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 1;
+  const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs);
+  a.job[0] = LaJob{Q, K, V, CTX, q, kv, kv, c, state_in, state_out, 0, 0, Hq, Hq / Hkv, 1, scale, 1.f};
+  la_cut(a);
+  la_place(a, workspace);
+  const void* p[] = {Q, K, V, CTX};
+  return la_run(a, dtype, la_vec(a, dtype, p, 4), as_stream(stream));
 }
 
 int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3], const void* K,
@@ -118,18 +95,21 @@ int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
                               size_t ws_bytes, void* stream) {
   const int rc = la_check(B, R, nseq, Hq, Hkv, d, dtype);
   if (rc == HFTA_EINVAL || !Q || !qs || !K || !V || !kvs || !seq_offsets || !log_decay || !(scale > 0.f) || !isfinite(1.f / scale) || !dCTX || !cs ||
-      !dQ || !dqs || !dK || !dV || !dkvs)
+      !dQ || !dqs || !dK || !dV || !dkvs || (dstate_in && dstate_in == dstate_out))
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
+  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 3))) return HFTA_EWORKSPACE;
   LaArgs a{};
-  a.off = seq_offsets; a.ld = log_decay; a.R = R; a.nseq = nseq; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.scale = scale;
-  a.job[0] = LaJob{dCTX, V, K, dQ, la_str(cs), la_str(kvs), la_str(kvs), la_str(dqs), state_in, nullptr, 0, 1};
-  a.job[1] = LaJob{K, Q, dCTX, dV, la_str(kvs), la_str(qs), la_str(cs), la_str(dkvs), dstate_out, dstate_in, 1, 0};
-  a.job[2] = LaJob{V, dCTX, Q, dK, la_str(kvs), la_str(cs), la_str(qs), la_str(dkvs), dstate_out, nullptr, 1, 1};
-  const dim3 grid((unsigned)(nseq * Hkv), (unsigned)B, 3);
-  if (dtype == HFTA_BF16) hipLaunchKernelGGL(la_walk_kernel<bf16_raw>, grid, dim3(128), 0, as_stream(stream), a, 3);
-  else hipLaunchKernelGGL(la_walk_kernel<float>, grid, dim3(128), 0, as_stream(stream), a, 3);
-  return launch_status();
+  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3;
+  const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs), dq = la_str(dqs), dkv = la_str(dkvs);
+  const int G = Hq / Hkv;
+  a.job[0] = LaJob{dCTX, V, K, dQ, c, kv, kv, dq, state_in, nullptr, 0, 1, Hq, G, 1, scale, 1.f};
+  a.job[1] = LaJob{K, Q, dCTX, dV, kv, q, c, dkv, dstate_out, dstate_in, 1, 0, Hkv, 1, G, scale, scale};
+  a.job[2] = LaJob{V, dCTX, Q, dK, kv, c, q, dkv, dstate_out, nullptr, 1, 1, Hkv, 1, G, scale, scale};
+  la_cut(a);
+  la_place(a, workspace);
+  const void* p[] = {Q, K, V, dCTX, dQ, dK, dV};
+  return la_run(a, dtype, la_vec(a, dtype, p, 7), as_stream(stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,135 @@
+// Linear attention: the states that blocks of tiles hand on, and their sums along the sequences (linear_attention.h).
+#include "linear_attention.h"
+
+namespace hfta {
+namespace {
+
+// What the sequence of a block's last row, if it goes on, has gathered in this block
+template <typename T, int D, bool VEC> __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void la_block_kernel(LaArgs a) {
+  typedef LaStage<T, D, VEC> Stage;
+  constexpr int TH = LaWave<D>::TH;
+  constexpr int JOIN = (TH - 1) * D * D * 4;                     // bytes of partial states
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[JOIN > 2 * Stage::BYTES ? JOIN : 2 * Stage::BYTES];
+  __shared__ PackedRows<LA_T> pr;
+  __shared__ __attribute__((aligned(16))) float pw[LA_T], wt[LA_T];
+  const LaWave<D> wv;
+  const LaPlace at(a, true);
+  const LaJob& J = a.job[at.job];
+  const int rev = J.rev, t = threadIdx.x, hk = at.h;
+  const int first = at.blk * a.per, last = first + a.per - 1;
+  if (at.blk == a.blocks - 1) return;                            // hands on nothing
+  const int32_t* off = a.off + (int64_t)at.b * (a.nseq + 1);
+  const float g = la_decay(a.ld[(int64_t)at.b * a.Hkv + hk]);
+  if (t < LA_T) pw[t] = la_pow(g, t);
+  const int a0 = (rev ? a.tiles - 1 - last : last) * LA_T, j = rev ? 0 : LA_T - 1;
+  pr.template scan<256>(off, a.nseq, a.R, a0);
+  int start, end;
+  const bool on = a0 + j < a.R && pr.range(a0, j, start, end) && (rev ? start < a0 : end > a0 + LA_T);
+  const int begin = rev ? a.tiles * LA_T - end : start;          // of the sequence, in the order of the walk
+  if (t == 0 && hk == 0) a.spans[((int64_t)at.job * a.B + at.b) * a.blocks + at.blk] = !on ? 0 : begin < first * LA_T ? 2 : 1;
+  if (!on) return;
+  pk_f16 s[D / 32];
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n) s[n] = pk_f16{};
+  const bool fresh = begin >= first * LA_T;
+  if (fresh && J.S0 && (TH == 1 || wv.th == 0)) {
+    int lo = 0, n = a.nseq;                                      // the last sequence that begins at or before the row
+    const int r = a0 + j;
+    while (n > 1) {
+      const int half = n >> 1;
+      if (off[lo + half] <= r) { lo += half; n -= half; } else n = half;
+    }
+    la_load_state<T, D>(s, J, a, at.b, lo, hk, wv);
+  }
+  const T* pb = pk_at<T>(J.B, J.bs, at.b, 0);
+  const T* pc = pk_at<T>(J.C, J.cs, at.b, 0);
+  for (int tile = fresh ? begin / LA_T : first; tile <= last; ++tile) {
+    const int c0 = max(begin - tile * LA_T, 0), m0 = (rev ? a.tiles - 1 - tile : tile) * LA_T;
+    // against the order, what comes in behind the last row has not faded when that row is taken
+    la_fade(s, la_powm1(g, LA_T - c0 - (rev && fresh && tile == begin / LA_T ? 1 : 0)));
+    for (int h = 0; h < J.gb; ++h) {
+      const int hb = hk * J.gb + h;
+      __syncthreads();
+      if (t < LA_T) wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
+      Stage::fetch(tiles, pb + hb * J.bs.h + (int64_t)m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
+      Stage::fetch(tiles + Stage::BYTES, pc + hb * J.cs.h + (int64_t)m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
+      la_land<VEC>();
+      la_update<T, D, TH>(s, tiles, tiles + Stage::BYTES, wt, c0, LA_T, c0 > 0, J.S1 != nullptr, wv, wv.th);
+    }
+  }
+  float* sums = a.sums + ((((int64_t)at.job * a.B + at.b) * a.Hkv + hk) * a.blocks + at.blk) * (D * D);
+  if constexpr (TH > 1) {                                        // wavefronts that took other rows of the same columns
+    float* lds = reinterpret_cast<float*>(tiles);
+    __syncthreads();
+    if (wv.th > 0) {
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) lds[(((wv.th - 1) * (D / 32) + wv.cs) * (D / 32) + n) * 1024 + i * 64 + wv.lane] = s[n][i];
+    }
+    __syncthreads();
+    if (wv.th > 0) return;
+    for (int w = 0; w < TH - 1; ++w)
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] += lds[((w * (D / 32) + wv.cs) * (D / 32) + n) * 1024 + i * 64 + wv.lane];
+  }
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *la_sum<D>(sums, wv.cs, n, q, wv.lane) = make_float4(s[n][4 * q], s[n][4 * q + 1], s[n][4 * q + 2], s[n][4 * q + 3]);
+}
+
+// Sums along the sequences, in place: a thread has four entries of a state and walks the blocks, eight blocks' loads in flight
+__global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, int entries) {
+  constexpr int AHEAD = 8;
+  const int64_t state = blockIdx.y;                              // job, model, key head
+  const int64_t jb = state / a.Hkv;
+  const int hk = (int)(state % a.Hkv), b = (int)(jb % a.B);
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= entries) return;
+  const float m1 = la_powm1(la_decay(a.ld[(int64_t)b * a.Hkv + hk]), a.per * LA_T);
+  const int* spans = a.spans + jb * a.blocks;
+  float4* p = reinterpret_cast<float4*>(a.sums) + (state * a.blocks) * entries + i;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < a.blocks - 1; k0 += AHEAD) {
+    float4 v[AHEAD];
+    int sp[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      sp[k] = k0 + k < a.blocks - 1 ? spans[k0 + k] : 0;
+      if (sp[k]) v[k] = p[(int64_t)(k0 + k) * entries];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (sp[k]) {
+        if (sp[k] == 2) {
+          v[k].x += fmaf(s.x, m1, s.x);
+          v[k].y += fmaf(s.y, m1, s.y);
+          v[k].z += fmaf(s.z, m1, s.z);
+          v[k].w += fmaf(s.w, m1, s.w);
+          p[(int64_t)(k0 + k) * entries] = v[k];
+        }
+        s = v[k];
+      }
+  }
+}
+
+template <typename T, int D> int launch(const LaArgs& a, const LaForm& f, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.blocks * a.B * a.Hkv * a.jobs)), block(256);
+  if (f.vec) hipLaunchKernelGGL((la_block_kernel<T, D, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((la_block_kernel<T, D, false>), grid, block, 0, st, a);
+  if (a.scanned) {
+    const int entries = D * D / 4;
+    hipLaunchKernelGGL(la_scan_kernel, dim3((entries + 255) / 256, (unsigned)(a.jobs * a.B * a.Hkv)), dim3(256), 0, st, a, entries);
+  }
+  return launch_status();
+}
+
+}  // namespace
+
+int la_states(const LaArgs& a, const LaForm& f, hipStream_t st) { return PK_BY_SIZE(launch); }
+
+}  // namespace hfta

@@ -103,22 +103,28 @@ def test_linear_attention_refusals(lib):
     def size(o):
         return [o.get(n, v) for n, v in dict(B=2, R=64, nseq=3, Hq=4, Hkv=2, d=16, dtype=1).items()]
 
-    def fwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, ctx=ONE, cs=S3, ws=ONE, wb=1 << 40, **o):
-        return lib.raw().hfta_linear_attention_fwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, None, ctx, cs, None, ws, wb, None)
-
-    def bwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, dctx=ONE, cs=S3, dQ=ONE, dqs=S3, dK=ONE, dV=ONE, dkvs=S3, ws=ONE,
+    def fwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, s0=None, ctx=ONE, cs=S3, s1=None, ws=ONE,
             wb=1 << 40, **o):
-        return lib.raw().hfta_linear_attention_bwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, None, dctx, cs, None, dQ, dqs, dK, dV, dkvs, None,
-                                                   ws, wb, None)
+        return lib.raw().hfta_linear_attention_fwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, s0, ctx, cs, s1, ws, wb, None)
+
+    def bwd(Q=ONE, qs=S3, K=ONE, V=ONE, kvs=S3, off=ONE, ld=ONE, scale=1.0, dctx=ONE, cs=S3, d1=None, dQ=ONE, dqs=S3, dK=ONE, dV=ONE, dkvs=S3,
+            d0=None, ws=ONE, wb=1 << 40, **o):
+        return lib.raw().hfta_linear_attention_bwd(*size(o), Q, qs, K, V, kvs, off, ld, scale, None, dctx, cs, d1, dQ, dqs, dK, dV, dkvs, d0, ws,
+                                                   wb, None)
     sizes = [dict(B=0), dict(R=0), dict(R=0x7fffffff), dict(nseq=0), dict(Hq=0), dict(Hq=3), dict(Hkv=0), dict(d=0), dict(dtype=2)]
     more = [dict(Q=None), dict(qs=None), dict(K=None), dict(V=None), dict(kvs=None), dict(off=None), dict(ld=None), dict(scale=0.0),
             dict(scale=-1.0), dict(scale=math.nan), dict(scale=1e-40), dict(cs=None)]
-    for bad in sizes + more + [dict(ctx=None)]:
+    for bad in sizes + more + [dict(ctx=None), dict(s0=ONE, s1=ONE)]:
         assert fwd(**bad) == lib.EINVAL, bad
-    for bad in sizes + more + [dict(dctx=None), dict(dQ=None), dict(dqs=None), dict(dK=None), dict(dV=None), dict(dkvs=None)]:
+    for bad in sizes + more + [dict(dctx=None), dict(dQ=None), dict(dqs=None), dict(dK=None), dict(dV=None), dict(dkvs=None), dict(d0=ONE, d1=ONE)]:
         assert bwd(**bad) == lib.EINVAL, bad
-    for bad in (dict(d=129), dict(nseq=1 << 24), dict(B=65536)):
+    for bad in (dict(d=129), dict(nseq=1 << 24), dict(B=65536), dict(R=1 << 28, B=8)):
         assert fwd(**bad) == lib.EUNSUPPORTED and bwd(**bad) == lib.EUNSUPPORTED, bad
+    for call, need in ((fwd, lib.linear_attention_fwd_workspace_bytes(2, 1000, 3, 4, 2, 16, 1)),
+                       (bwd, lib.linear_attention_bwd_workspace_bytes(2, 1000, 3, 4, 2, 16, 1))):
+        assert need > 0
+        for bad in (dict(wb=need - 1), dict(ws=None), dict(ws=C.c_void_p(264))):
+            assert call(R=1000, **bad) == lib.EWORKSPACE, bad
 
 
 def test_linear_attention_step_refusals(lib):
