@@ -31,6 +31,8 @@ namespace hfta {
 constexpr int LA_T = 64;                                         // rows of a tile
 constexpr int LA_SPAN = 512;                                     // rows whose sequences are looked up at once
 
+typedef __attribute__((address_space(3))) unsigned char* la_lds;
+
 struct LaJob {
   const void *A, *B, *C;
   void* O;
@@ -83,12 +85,12 @@ template <typename T, int D, bool VEC> struct LaStage {
   static constexpr int BYTES = LA_T * Tile::ROW, PIECES = BYTES / 16, N = PIECES / 256, EPP = 16 / (int)sizeof(T);
   static_assert(PIECES % 256 == 0, "whole pieces for every thread");
   // src: the tile's first row in memory, rows: how many there are
-  static __device__ __forceinline__ void fetch(unsigned char* tile, const T* src, int64_t ld, int rows, int d, bool flip) {
+  static __device__ __forceinline__ void fetch(la_lds tile, const T* src, int64_t ld, int rows, int d, bool flip) {
     rows = min(rows, LA_T);
     if constexpr (VEC) {
       const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * (int)ld + d) * (uint32_t)sizeof(T) : 0u;
       const dma_i32x4 rs = dma_rsrc(src, bytes);
-      const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile);
+      const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile);
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
@@ -110,7 +112,7 @@ template <typename T, int D, bool VEC> struct LaStage {
             for (int e = 0; e < EPP; ++e)
               if (c + e < d) v.e[e] = p[e];
         }
-        *reinterpret_cast<piece_u4*>(tile + q * 16) = v.u;
+        *(__attribute__((address_space(3))) piece_u4*)(tile + q * 16) = v.u;
       }
     }
   }
@@ -137,13 +139,17 @@ typedef __attribute__((address_space(3))) pk_s4* la_lds4;
 union LaFrag { uint32_t u[4]; pk_s4 h[2]; pk_bf8 v; bf16_raw e[8]; };
 
 // Columns of a staged bf16 tile over 16 rows as a matrix operand: lane l holds column col0 + l%32 (SWAP: with bits 2 and 3 of l exchanged), its
-// slots rows row0 + 4 (l/32) + 0..3 and 8 + 4 (l/32) + 0..3
-template <int D, bool SWAP> __device__ __forceinline__ void la_cols(LaFrag& f, const unsigned char* tile, int row0, int col0, int lane) {
-  typedef PkTile<bf16_raw, D> Tile;
-  const int r = lane & 15, q = SWAP ? ((r & 1) << 1 | (r >> 1 & 1)) : r & 3, row = 4 * (lane >> 5) + (r >> 2);
+// slots rows row0 + 4 (l/32) + 0..3 and 8 + 4 (l/32) + 0..3.  row0: a multiple of 16, col0: of 32
+template <int D, bool SWAP> __device__ __forceinline__ uint32_t la_cols_at(int lane) {
+  const int r = lane & 15, q = SWAP ? ((r & 1) << 1 | (r >> 1 & 1)) : r & 3;
+  uint32_t a = (uint32_t)PkTile<bf16_raw, D>::at(4 * (lane >> 5) + (r >> 2), (16 * ((lane >> 4) & 1) + 4 * q) * 2);
+  asm volatile("" : "+v"(a));                                    // (formed where it is needed)
+  return a;
+}
+template <int D> __device__ __forceinline__ void la_cols(LaFrag& f, la_lds tile, uint32_t at, int row0, int col0) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + Tile::at(row0 + row + 8 * h, (col0 + 16 * ((lane >> 4) & 1) + 4 * q) * 2)));
+  for (int h = 0; h < 2; ++h)                                    // eight rows on: another bit of the key
+    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + (at ^ (uint32_t)(col0 << 1 | h << 5)) + (row0 + 8 * h) * PkTile<bf16_raw, D>::ROW));
 }
 
 // A state in the accumulators of the wavefronts: s[kb], rows b's columns 32 kb + .., columns c's column 32 cs + lane % 32
@@ -158,15 +164,16 @@ template <int D> __device__ __forceinline__ float4* la_sum(float* sums, int cs, 
 // s += sum over tile rows [c0, c1) of w[row] b[row]^T c[row], w: LDS.  STEP: a wavefront takes every STEP-th sixteen rows from `from` on.
 // `part`: rows outside of [c0, c1) may hold anything (else there are none).  three: c w as three words
 template <typename T, int D, int STEP>
-__device__ __forceinline__ void la_update(pk_f16 (&s)[D / 32], const unsigned char* tb, const unsigned char* tc, const float* w, int c0, int c1,
+__device__ __forceinline__ void la_update(pk_f16 (&s)[D / 32], la_lds tb, la_lds tc, const float* w, int c0, int c1,
                                           bool part, bool three, const LaWave<D>& wv, int from) {
   const int lane = wv.lane, g = wv.g;
   if constexpr (sizeof(T) == 2) {
+    const uint32_t at = la_cols_at<D, false>(lane), swapped = la_cols_at<D, true>(lane);
 #pragma unroll
     for (int ks = 0; ks < LA_T / 16; ks += STEP) {
       const int row0 = 16 * (ks + from);
       LaFrag c, hi, lo, ll;
-      la_cols<D, false>(c, tc, row0, 32 * wv.cs, lane);
+      la_cols<D>(c, tc, at, row0, 32 * wv.cs);
       const float4 w0 = *reinterpret_cast<const float4*>(w + row0 + 4 * g), w1 = *reinterpret_cast<const float4*>(w + row0 + 8 + 4 * g);
       const float wt[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
       uint32_t in = 0xffu;                                       // slots whose rows take part
@@ -198,7 +205,7 @@ __device__ __forceinline__ void la_update(pk_f16 (&s)[D / 32], const unsigned ch
 #pragma unroll
       for (int kb = 0; kb < D / 32; ++kb) {
         LaFrag b;
-        la_cols<D, true>(b, tb, row0, 32 * kb, lane);
+        la_cols<D>(b, tb, swapped, row0, 32 * kb);
         if (__builtin_expect(part, 0)) {
 #pragma unroll
           for (int p = 0; p < 4; ++p) b.u[p] &= (in >> (2 * p) & 1 ? 0xffffu : 0u) | (in >> (2 * p + 1) & 1 ? 0xffff0000u : 0u);
@@ -210,17 +217,20 @@ __device__ __forceinline__ void la_update(pk_f16 (&s)[D / 32], const unsigned ch
     }
   } else {
     typedef PkTile<T, D> Tile;
-#pragma unroll 2
-    for (int ks = 0; ks < LA_T / 16; ks += STEP)
+    uint32_t at = (uint32_t)Tile::at(4 * g, (lane & 31) * 4);    // row 16 ks + 8 (i / 4) + 4 g + i % 4: other bits of the key, or none
+    asm volatile("" : "+v"(at));
+#pragma unroll 1
+    for (int ks = from; ks < LA_T / 16; ks += STEP)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int row = 16 * (ks + from) + 8 * (i >> 2) + 4 * g + (i & 3);
-        float c = *reinterpret_cast<const float*>(tc + Tile::at(row, (32 * wv.cs + (lane & 31)) * 4)) * w[row];
+        const int r = 8 * (i >> 2) + (i & 3), row = 16 * ks + r + 4 * g;
+        const uint32_t to = (uint32_t)(16 * ks + r) * Tile::ROW, key = (uint32_t)Tile::key(r) << 4;
+        float c = *(__attribute__((address_space(3))) const float*)(tc + (at ^ (key ^ (uint32_t)(wv.cs << 7))) + to) * w[row];
         const bool out = part && (row < c0 || row >= c1);
         if (out) c = 0.f;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
-          float b = *reinterpret_cast<const float*>(tb + Tile::at(row, (32 * kb + (lane & 31)) * 4));
+          float b = *(__attribute__((address_space(3))) const float*)(tb + (at ^ (key ^ (uint32_t)(kb << 7))) + to);
           if (out) b = 0.f;
           s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(b, c, s[kb], 0, 0, 0);
         }
@@ -269,25 +279,5 @@ struct LaPlace {
     h = bh % heads;
   }
 };
-
-// Sequences of the rows of tile i (in the order of the walk), with a lookup of the next LA_SPAN rows where `fresh`.  Ends with a barrier; a
-// barrier has to stand between the last reads of rel and this.
-__device__ __forceinline__ void la_rows(LaRows& lr, const int32_t* off, const LaArgs& a, int rev, int tile, bool fresh) {
-  const int a0 = (rev ? a.tiles - 1 - tile : tile) * LA_T;       // the tile's first row in memory
-  if (fresh) {
-    const int t0 = rev ? a0 + LA_T - LA_SPAN : a0;
-    lr.pr.template scan<256>(off, a.nseq, a.R, t0);
-    if (threadIdx.x == 0) lr.t0 = t0;
-    __syncthreads();
-  }
-  if (threadIdx.x < LA_T) {
-    const int j = threadIdx.x, r = rev ? a0 + LA_T - 1 - j : a0 + j;
-    int start, end;
-    const bool in = r < a.R && lr.pr.range(lr.t0, r - lr.t0, start, end);
-    lr.rel[j] = !in ? LA_NONE : max(rev ? a0 + LA_T - end : start - a0, -1);
-    lr.seqend[j] = in && (rev ? r == start : r == end - 1);
-  }
-  __syncthreads();
-}
 
 }  // namespace hfta

@@ -51,10 +51,10 @@ template <typename T, int D, bool VEC> __global__ __launch_bounds__(256, (D * si
       const int hb = hk * J.gb + h;
       __syncthreads();
       if (t < LA_T) wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
-      Stage::fetch(tiles, pb + hb * J.bs.h + (int64_t)m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
-      Stage::fetch(tiles + Stage::BYTES, pc + hb * J.cs.h + (int64_t)m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
+      Stage::fetch((la_lds)tiles, pb + hb * J.bs.h + (int64_t)m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
+      Stage::fetch((la_lds)tiles + Stage::BYTES, pc + hb * J.cs.h + (int64_t)m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
       la_land<VEC>();
-      la_update<T, D, TH>(s, tiles, tiles + Stage::BYTES, wt, c0, LA_T, c0 > 0, J.S1 != nullptr, wv, wv.th);
+      la_update<T, D, TH>(s, (la_lds)tiles, (la_lds)tiles + Stage::BYTES, wt, c0, LA_T, c0 > 0, J.S1 != nullptr, wv, wv.th);
     }
   }
   float* sums = a.sums + ((((int64_t)at.job * a.B + at.b) * a.Hkv + hk) * a.blocks + at.blk) * (D * D);
