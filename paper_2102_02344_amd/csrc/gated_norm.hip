@@ -58,12 +58,23 @@ template <typename T, int NP, int TPR> struct GnRow {
 #pragma unroll
     for (int p = 0; p < NP; ++p) P::store(row + col(p), x[p], E - col(p));
   }
-  // fp32 rows of weights
+  // fp32 rows of weights (NULL: `none`)
   static __device__ __forceinline__ void weights(float (&x)[NP][P::N], const float* row, int E, float none) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
+      if (!row) {
 #pragma unroll
-      for (int e = 0; e < P::N; ++e) x[p][e] = row && col(p) + e < E ? row[col(p) + e] : none;
+        for (int e = 0; e < P::N; ++e) x[p][e] = none;
+        continue;
+      }
+#pragma unroll
+      for (int q = 0; q < P::N / 4; ++q) {
+        float w[4];
+        Piece16<float>::load(w, row + col(p) + 4 * q, E - col(p) - 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[p][4 * q + e] = w[e];
+      }
+    }
   }
 };
 #define GN_EACH(NP, N)                 \
@@ -234,24 +245,34 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs 
   }
 }
 
-// The parts of a model added in order: four threads of a column take a quarter of them each
-__global__ __launch_bounds__(256) void gn_add_kernel(const float* part, int parts, int E, float* dw2, float* db2, float* dw1, float* db1, float* dres) {
-  __shared__ double lds[4][64];
+// The parts of a model added in order: a workgroup takes 64 columns, each of its wavefronts a sixteenth of the parts, eight in flight
+constexpr int GN_ADD = 1024;
+__global__ __launch_bounds__(GN_ADD) void gn_add_kernel(const float* part, int parts, int E, float* dw2, float* db2, float* dw1, float* db1, float* dres) {
+  constexpr int W = GN_ADD / 64, AHEAD = 8;
+  __shared__ double lds[W][64];
   const int b = blockIdx.y, q = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t width = 4 * (int64_t)E + 4, c = (int64_t)blockIdx.x * 64 + lane;
-  const float* src = part + (int64_t)b * parts * width;
   const int which = c < 4 * (int64_t)E ? (int)(c / E) : 4;
   float* out = which == 0 ? dw2 : which == 1 ? db2 : which == 2 ? dw1 : which == 3 ? db1 : dres;
   const bool has = out && c <= 4 * (int64_t)E;
+  if (!__syncthreads_or(has)) return;                            // (sums that nobody asked for)
+  const float* src = part + (int64_t)b * parts * width + c;
   double s = 0.0;
   if (has)
-    for (int i = q; i < parts; i += 4) s += (double)src[i * width + c];
+    for (int i = q; i < parts; i += W * AHEAD) {
+      float x[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) x[k] = i + k * W < parts ? src[(i + k * W) * width] : 0.f;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) s += (double)x[k];
+    }
   lds[q][lane] = s;
   __syncthreads();
   if (has && q == 0) {
-    const float x = (float)((lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]));
-    if (which < 4) out[(int64_t)b * E + (c - which * (int64_t)E)] = x;
-    else out[b] = x;
+#pragma unroll
+    for (int k = 1; k < W; ++k) s += lds[k][lane];
+    if (which < 4) out[(int64_t)b * E + (c - which * (int64_t)E)] = (float)s;
+    else out[b] = (float)s;
   }
 }
 
@@ -346,7 +367,7 @@ int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const
   const int r = GN_PICK(gn_bwd, a, B, st);
   if (r != HFTA_OK) return r;
   const dim3 grid((unsigned)((4 * (int64_t)E + 1 + 63) / 64), (unsigned)B);
-  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(256), 0, st, a.part, a.blocks * gn_rows(E), E, dw2, db2, dw1, db1, dres);
+  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks * gn_rows(E), E, dw2, db2, dw1, db1, dres);
   return launch_status();
 }
 

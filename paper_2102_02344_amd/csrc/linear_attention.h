@@ -15,9 +15,9 @@
 // row 63 - j in memory.  Blocks of tiles run side by side: a first launch forms the state that each block's last sequence
 // takes with it, a second adds them up along each sequence, or, where blocks are few, the third does that for itself before it walks its tiles.
 //
-// A wavefront keeps 32 columns of c of the state in the matrix instruction's accumulators, fp32, for the whole walk; they are
-// the operand of the product with A without a shuffle, because the update gives b's columns to the accumulator's rows in the order in which
-// rows of A lie in registers.  (A B^T) . D passes through LDS.  bf16: what is rounded to bf16 as an operand (S, W C, the masked
+// A wavefront keeps 16 columns of c of the state in the matrix instruction's accumulators, fp32, for the whole walk (D / 16 wavefronts are a
+// workgroup); they are the operand of the product with A without a shuffle, because the update gives b's columns to the accumulator's rows in
+// the order in which rows of A are read.  (A B^T) . D passes through LDS.  bf16: what is rounded to bf16 as an operand (S, W C, the masked
 // products) goes in as two words, value and rest, and W C as three where states are returned: results have the error of their own rounding alone.
 //
 // Entries that a row does not see are taken out by selects; values of C that are not finite and lie in a tile beside rows that do
@@ -43,17 +43,19 @@ struct LaJob {
   int flip;                        // the state's rows and columns change places in memory
   int heads, ga, gb;               // workgroups' heads of a model; heads of A (B and C) that belong to one of them: h / ga, h * gb ..
   float fo, fi;                    // results times fo, states in memory times 1 / fi
+  int sum, turned;                 // which blocks' sums are its states, and whether they are of C and B instead (rows and columns change places)
 };
+enum { LA_ALONE = 0, LA_SUMS = 1, LA_SCANNED = 2, LA_WALK = 3 };   // one block; sums of blocks, added up by each block or along the sequences; none
 struct LaArgs {
-  LaJob job[3];
+  LaJob job[3];                    // by sum first: job[i] forms sum i for i < nsums
   const int32_t* off;
   const float* ld;
-  float* sums;                     // [job][model][key head][block][D * D], as accumulators lie
-  int* spans;                      // [job][model][block]: 0: no sequence goes on behind the block, 1: one that began in it, 2: one from before it
-  int B, R, nseq, Hkv, d, jobs, tiles, per, blocks;              // tiles in all and of a block, blocks
-  int scanned;                     // sums are added up along the sequences already
+  float* sums;                     // [sum][model][key head][block][D * D], as accumulators lie
+  int* spans;                      // [sum][model][block]: 0: no sequence goes on behind the block, 1: one that began in it, 2: one from before it
+  int B, R, nseq, Hkv, d, jobs, nsums, tiles, per, blocks;       // tiles in all and of a block, blocks
+  int mode;
 };
-struct LaForm { bool bf16, vec; };
+struct LaForm { bool bf16, vec, pieces; };                     // storage, rows in 16-byte pieces, states that come in or go out
 int la_states(const LaArgs& a, const LaForm& f, hipStream_t st); // linear_attention_states.hip
 int la_main(const LaArgs& a, const LaForm& f, hipStream_t st);   // linear_attention_main.hip
 static inline int la_pad(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
@@ -66,47 +68,51 @@ __device__ __forceinline__ float la_pow(float g, int n) {
 }
 __device__ __forceinline__ float la_powm1(float g, int n) { return n == 0 ? 0.f : expm1f((float)n * g); }
 
-// A wavefront's role: column block of c, block of 32 rows where two wavefronts share the columns
+typedef float la_f4 __attribute__((ext_vector_type(4)));
+// A wavefront's role: it has columns 16 cs + l%16 of c; a lane's quarter g = l / 16
 template <int D> struct LaWave {
-  static constexpr int CS = D / 32, TH = 4 / CS, NTB = TH == 1 ? 2 : 1;
-  int lane, wave, g, cs, th;
+  static constexpr int WAVES = D / 16, NT = 64 * WAVES, KT = D / 16;      // accumulators of a state: KT blocks of 16 x 16
+  int lane, cs, l, g;
   __device__ __forceinline__ LaWave() {
     lane = threadIdx.x & 63;
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    g = lane >> 5;
-    cs = wave % CS;
-    th = wave / CS;
+    cs = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    l = lane & 15;
+    g = lane >> 4;
   }
 };
 
-// 64 rows of a [row][D] matrix into LDS, rows that are not there and columns from d on zero; FLIP: the last row first
+// 64 rows of a [row][D] matrix into LDS, rows that are not there and columns from d on zero; flip: the last row first.  In whole pieces the loads
+// go through a buffer that ends with the last row, straight into LDS; a thread's pieces lie a multiple of 16 rows apart, with which the swizzle
+// repeats, so that one offset serves them all.
 template <typename T, int D, bool VEC> struct LaStage {
   typedef PkTile<T, D> Tile;
-  static constexpr int BYTES = LA_T * Tile::ROW, PIECES = BYTES / 16, N = PIECES / 256, EPP = 16 / (int)sizeof(T);
-  static_assert(PIECES % 256 == 0, "whole pieces for every thread");
+  static constexpr int NT = LaWave<D>::NT, BYTES = LA_T * Tile::ROW, PIECES = BYTES / 16, N = PIECES / NT, EPP = 16 / (int)sizeof(T), RPN = NT / Tile::PPR;
+  static_assert(PIECES % NT == 0 && RPN % 16 == 0, "whole pieces for every thread, the same swizzle for all of a thread's");
+  uint32_t at;                     // of the piece with the lowest offset
+  __device__ __forceinline__ void init(int64_t ld, int d, bool flip) {
+    const int row = threadIdx.x / Tile::PPR, byte = ((threadIdx.x % Tile::PPR) ^ Tile::key(row)) * 16, from = flip ? RPN - 1 - row : row;
+    at = byte < d * (int)sizeof(T) ? (uint32_t)(from * (int)ld) * (uint32_t)sizeof(T) + (uint32_t)byte : PK_OUT;
+  }
   // src: the tile's first row in memory, rows: how many there are
-  static __device__ __forceinline__ void fetch(la_lds tile, const T* src, int64_t ld, int rows, int d, bool flip) {
+  __device__ __forceinline__ void fetch(la_lds tile, const T* src, int64_t ld, int rows, int d, bool flip) const {
     rows = min(rows, LA_T);
     if constexpr (VEC) {
-      const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * (int)ld + d) * (uint32_t)sizeof(T) : 0u;
+      const uint32_t bytes = (uint32_t)((rows - 1) * (int)ld + d) * (uint32_t)sizeof(T);
       const dma_i32x4 rs = dma_rsrc(src, bytes);
-      const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile);
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile), step = (uint32_t)(RPN * (int)ld) * (uint32_t)sizeof(T);
+      const uint32_t to = lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024u;
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const int q = n * 256 + (int)threadIdx.x, row = q / Tile::PPR, byte = ((q % Tile::PPR) ^ Tile::key(row)) * 16, at = flip ? LA_T - 1 - row : row;
-        const uint32_t off = byte < d * (int)sizeof(T) ? (uint32_t)(at * (int)ld) * (uint32_t)sizeof(T) + (uint32_t)byte : PK_OUT;
-        dma_load(lds + (uint32_t)(n * 256 + wave * 64) * 16u, off, rs);
-      }
+      for (int n = 0; n < N; ++n)                                // (PK_OUT and a few steps lie behind every such buffer too)
+        dma_load(to + (uint32_t)n * NT * 16u, at + (uint32_t)(flip ? N - 1 - n : n) * step, rs);
     } else {
       union { piece_u4 u; T e[EPP]; } v;
 #pragma unroll 1
       for (int n = 0; n < N; ++n) {
-        const int q = n * 256 + (int)threadIdx.x, row = q / Tile::PPR, byte = ((q % Tile::PPR) ^ Tile::key(row)) * 16, at = flip ? LA_T - 1 - row : row;
+        const int q = n * NT + (int)threadIdx.x, row = q / Tile::PPR, byte = ((q % Tile::PPR) ^ Tile::key(row)) * 16, from = flip ? LA_T - 1 - row : row;
         const int c = byte / (int)sizeof(T);
-        const T* p = src + (int64_t)at * ld + c;
+        const T* p = src + (int64_t)from * ld + c;
         v.u = piece_u4{0, 0, 0, 0};
-        if (at < rows) {
+        if (from < rows) {
           if (c + EPP <= d) v.u = *reinterpret_cast<const piece_u4*>(p);
           else
             for (int e = 0; e < EPP; ++e)
@@ -123,13 +129,43 @@ template <bool VEC> __device__ __forceinline__ void la_land() {
   __syncthreads();
 }
 
-// The rows of a tile: where each one's sequence begins, counted in the tile's rows in the order of the walk; -1: before it, LA_NONE: in none
+// Where a row's sequence begins, counted in the tile's rows in the order of the walk: -1 before the tile; this: in no sequence
 constexpr int LA_NONE = 1 << 20;
-struct LaRows {
-  PackedRows<LA_SPAN> pr;
-  int t0;                          // (of the span, in memory)
-  int rel[LA_T];
-  int seqend[LA_T];                // whether the row is its sequence's last one in the order of the walk
+
+// The sequences of a tile's rows from a lookup of LA_SPAN rows: a lane's row r of the tile (in memory) lies in [start, end).  Every
+// word of the lookup is in a lane, the last one that begins before the tile and the first one behind it come out of two ballots.
+struct LaSpan {
+  uint32_t word;
+  uint64_t some;                   // words that are not empty
+  int t0, lo, hi, first, last;
+  template <typename P> __device__ __forceinline__ void take(const P& pr, int t0_, int lane) {
+    word = lane < LA_SPAN / 32 ? pr.mark[lane] : 0u;
+    some = __ballot(word != 0);
+    t0 = t0_;
+    lo = __builtin_amdgcn_readfirstlane(pr.lo);
+    hi = __builtin_amdgcn_readfirstlane(pr.hi);
+    first = __builtin_amdgcn_readfirstlane(pr.first);
+    last = __builtin_amdgcn_readfirstlane(pr.last);
+  }
+  // m0: the tile's first row, i: a row of it
+  __device__ __forceinline__ bool range(int m0, int i, int& start, int& end) const {
+    const int w = (m0 - t0) >> 5;
+    const uint64_t marks = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)word, w + 1) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)word, w);
+    const uint64_t before = some & ((1ull << w) - 1), behind = some >> (w + 2);
+    int from = lo, to = hi;
+    if (before) {
+      const int k = 63 - __builtin_clzll(before);
+      from = t0 + 32 * k + 31 - __builtin_clz((uint32_t)__builtin_amdgcn_readlane((int)word, k));
+    }
+    if (behind) {
+      const int k = w + 2 + __builtin_ctzll(behind);
+      to = t0 + 32 * k + __builtin_ctz((uint32_t)__builtin_amdgcn_readlane((int)word, k));
+    }
+    const uint64_t up = 2ull * ((1ull << i) - 1) + 1, at = marks & up, past = marks & ~up;       // bits 0 .. i, and the others
+    start = at ? m0 + 63 - __builtin_clzll(at) : from;
+    end = past ? m0 + __builtin_ctzll(past) : to;
+    return m0 + i >= first && m0 + i < last;
+  }
 };
 
 // bf16 pairs with infinities and NaNs have bit 15 of a half set in the result
@@ -138,103 +174,134 @@ __device__ __forceinline__ uint32_t la_odd(uint32_t u) { return (u & 0x7f807f80u
 typedef __attribute__((address_space(3))) pk_s4* la_lds4;
 union LaFrag { uint32_t u[4]; pk_s4 h[2]; pk_bf8 v; bf16_raw e[8]; };
 
-// Columns of a staged bf16 tile over 16 rows as a matrix operand: lane l holds column col0 + l%32 (SWAP: with bits 2 and 3 of l exchanged), its
-// slots rows row0 + 4 (l/32) + 0..3 and 8 + 4 (l/32) + 0..3.  row0: a multiple of 16, col0: of 32
-template <int D, bool SWAP> __device__ __forceinline__ uint32_t la_cols_at(int lane) {
-  const int r = lane & 15, q = SWAP ? ((r & 1) << 1 | (r >> 1 & 1)) : r & 3;
-  uint32_t a = (uint32_t)PkTile<bf16_raw, D>::at(4 * (lane >> 5) + (r >> 2), (16 * ((lane >> 4) & 1) + 4 * q) * 2);
+// Sixteen columns of a staged bf16 tile over 32 rows as a matrix operand: a lane's slots are rows row0 + 4 g + 0..3 and 16 + 4 g + 0..3; lane l%16
+// holds column col0 + l, or (SPREAD) column col0 + 8 (l / 4) + l%4.  `at`: la_cols_at(), row0: a multiple of 32, col0: of 16 (SPREAD: of 4, in each 32 the
+// first two)
+template <int D, bool SPREAD> __device__ __forceinline__ uint32_t la_cols_at(int lane) {
+  const int r = lane & 15;
+  uint32_t a = (uint32_t)PkTile<bf16_raw, D>::at(4 * (lane >> 4) + (r >> 2), (SPREAD ? 8 : 4) * (r & 3) * 2);
   asm volatile("" : "+v"(a));                                    // (formed where it is needed)
   return a;
 }
 template <int D> __device__ __forceinline__ void la_cols(LaFrag& f, la_lds tile, uint32_t at, int row0, int col0) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)                                    // eight rows on: another bit of the key
-    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + (at ^ (uint32_t)(col0 << 1 | h << 5)) + (row0 + 8 * h) * PkTile<bf16_raw, D>::ROW));
+  for (int h = 0; h < 2; ++h)                                    // (sixteen rows on the swizzle repeats)
+    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + (at ^ (uint32_t)(col0 << 1)) + (row0 + 16 * h) * PkTile<bf16_raw, D>::ROW));
 }
 
-// A state in the accumulators of the wavefronts: s[kb], rows b's columns 32 kb + .., columns c's column 32 cs + lane % 32
-template <typename T> __device__ __forceinline__ int la_row(int i, int g) {       // row of accumulator i, 0..31
-  return sizeof(T) == 2 ? 16 * (i >> 3) + 8 * g + 4 * (i >> 2 & 1) + (i & 3) : 8 * (i >> 2) + 4 * g + (i & 3);
+// A state in the accumulators of the wavefronts: s[kt][i], column 16 cs + l of c, and of b
+template <typename T> __device__ __forceinline__ int la_row(int kt, int i, int g) {
+  return sizeof(T) == 2 ? 32 * (kt >> 1) + 8 * g + 4 * (kt & 1) + i : 16 * kt + 4 * g + i;
 }
 // its place in a block's sums
-template <int D> __device__ __forceinline__ float4* la_sum(float* sums, int cs, int kb, int q, int lane) {
-  return reinterpret_cast<float4*>(sums) + ((cs * (D / 32) + kb) * 4 + q) * 64 + lane;
+template <int D> __device__ __forceinline__ la_f4* la_sum(float* sums, int cs, int kt, int lane) {
+  return reinterpret_cast<la_f4*>(sums) + (cs * (D / 16) + kt) * 64 + lane;
 }
 
-// s += sum over tile rows [c0, c1) of w[row] b[row]^T c[row], w: LDS.  STEP: a wavefront takes every STEP-th sixteen rows from `from` on.
-// `part`: rows outside of [c0, c1) may hold anything (else there are none).  three: c w as three words
-template <typename T, int D, int STEP>
-__device__ __forceinline__ void la_update(pk_f16 (&s)[D / 32], la_lds tb, la_lds tc, const float* w, int c0, int c1,
-                                          bool part, bool three, const LaWave<D>& wv, int from) {
+// a pair of values as two bf16 words, value and rest; x becomes what is left of it
+__device__ __forceinline__ uint32_t la_word(float& x0, float& x1) {
+  const uint32_t u = pack_bf16x2(x0, x1);
+  x0 -= __uint_as_float(u << 16);
+  x1 -= __uint_as_float(u & 0xffff0000u);
+  return u;
+}
+
+// s += a block's sum, or its transpose
+template <typename T, int D> __device__ __forceinline__ void la_add_sum(la_f4 (&s)[D / 16], float* sum, bool turned, const LaWave<D>& wv) {
+  if (!turned) {
+#pragma unroll
+    for (int kt = 0; kt < D / 16; ++kt) s[kt] += *la_sum<D>(sum, wv.cs, kt, wv.lane);
+  } else {                                                       // entry (row, column) is (column, row) of what lies there
+    const int c = 16 * wv.cs + wv.l;                             // the row there, and where it lies
+    const int k = sizeof(T) == 2 ? 2 * (c >> 5) + (c >> 2 & 1) : c >> 4, g = sizeof(T) == 2 ? c >> 3 & 3 : c >> 2 & 3;
+    const float* p = sum + (k * 64 + 16 * g) * 4 + (c & 3);
+#pragma unroll
+    for (int kt = 0; kt < D / 16; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = la_row<T>(kt, i, wv.g);
+        s[kt][i] += p[((r >> 4) * (D / 16) * 64 + (r & 15)) * 4];
+      }
+  }
+}
+
+// which of rows r and r + 1 lie in [c0, c1), as a mask of two halves
+__device__ __forceinline__ uint32_t la_rows(int r, int c0, int c1) {
+  return (r >= c0 && r < c1 ? 0xffffu : 0u) | (r + 1 >= c0 && r + 1 < c1 ? 0xffff0000u : 0u);
+}
+
+// s += sum over tile rows of w[row] b[row]^T c[row], w: LDS.  PART: rows outside of [c0, c1), whose weights are zero, may hold anything.
+// THREE: c w as three words
+template <typename T, int D, bool PART, bool THREE>
+__device__ __forceinline__ void la_update(la_f4 (&s)[D / 16], la_lds tb, la_lds tc, const float* w, int c0, int c1, const LaWave<D>& wv) {
   const int lane = wv.lane, g = wv.g;
+  int g4 = 4 * g;
+  if constexpr (PART) asm volatile("" : "+v"(c0), "+v"(c1), "+v"(g4));      // (masks are formed where they are needed)
   if constexpr (sizeof(T) == 2) {
-    const uint32_t at = la_cols_at<D, false>(lane), swapped = la_cols_at<D, true>(lane);
+    const uint32_t at = la_cols_at<D, false>(lane), spread = la_cols_at<D, true>(lane);
 #pragma unroll
-    for (int ks = 0; ks < LA_T / 16; ks += STEP) {
-      const int row0 = 16 * (ks + from);
+    for (int ks = 0; ks < LA_T / 32; ++ks) {
+      const int row0 = 32 * ks;
       LaFrag c, hi, lo, ll;
-      la_cols<D>(c, tc, at, row0, 32 * wv.cs);
-      const float4 w0 = *reinterpret_cast<const float4*>(w + row0 + 4 * g), w1 = *reinterpret_cast<const float4*>(w + row0 + 8 + 4 * g);
+      la_cols<D>(c, tc, at, row0, 16 * wv.cs);
+      const float4 w0 = *reinterpret_cast<const float4*>(w + row0 + 4 * g), w1 = *reinterpret_cast<const float4*>(w + row0 + 16 + 4 * g);
       const float wt[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-      uint32_t in = 0xffu;                                       // slots whose rows take part
-      if (__builtin_expect(part, 0)) {
-        in = 0;
+      if constexpr (PART) {                                      // zeros in the rows that do not take part
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int row = row0 + 4 * g + (e & 3) + 8 * (e >> 2);
-          if (row >= c0 && row < c1) in |= 1u << e;
-        }
+        for (int p = 0; p < 4; ++p) c.u[p] &= la_rows(row0 + g4 + 2 * (p & 1) + 16 * (p >> 1), c0, c1);
       }
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         float x0 = __uint_as_float(c.u[p] << 16) * wt[2 * p], x1 = __uint_as_float(c.u[p] & 0xffff0000u) * wt[2 * p + 1];
-        if (__builtin_expect(part, 0)) {
-          if (!(in >> (2 * p) & 1)) x0 = 0.f;
-          if (!(in >> (2 * p + 1) & 1)) x1 = 0.f;
-        }
-        hi.u[p] = pack_bf16x2(x0, x1);
-        x0 -= __uint_as_float(hi.u[p] << 16);
-        x1 -= __uint_as_float(hi.u[p] & 0xffff0000u);
-        lo.u[p] = pack_bf16x2(x0, x1);
-        if (three) {
-          x0 -= __uint_as_float(lo.u[p] << 16);
-          x1 -= __uint_as_float(lo.u[p] & 0xffff0000u);
-          ll.u[p] = pack_bf16x2(x0, x1);
-        }
+        hi.u[p] = la_word(x0, x1);
+        lo.u[p] = la_word(x0, x1);
+        if constexpr (THREE) ll.u[p] = la_word(x0, x1);
       }
 #pragma unroll
-      for (int kb = 0; kb < D / 32; ++kb) {
-        LaFrag b;
-        la_cols<D>(b, tb, swapped, row0, 32 * kb);
-        if (__builtin_expect(part, 0)) {
+      for (int k0 = 0; k0 < D / 16; k0 += 2) {                   // (four of b's columns' reads at once would take the registers of the state)
+        LaFrag b[2];
 #pragma unroll
-          for (int p = 0; p < 4; ++p) b.u[p] &= (in >> (2 * p) & 1 ? 0xffffu : 0u) | (in >> (2 * p + 1) & 1 ? 0xffff0000u : 0u);
+        for (int k = 0; k < 2; ++k) {
+          la_cols<D>(b[k], tb, spread, row0, 16 * k0 + 4 * k);
+          if constexpr (PART) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) b[k].u[p] &= la_rows(row0 + g4 + 2 * (p & 1) + 16 * (p >> 1), c0, c1);
+          }
         }
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v, hi.v, s[kb], 0, 0, 0);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v, lo.v, s[kb], 0, 0, 0);
-        if (three) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v, ll.v, s[kb], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k0 + k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[k].v, hi.v, s[k0 + k], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k0 + k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[k].v, lo.v, s[k0 + k], 0, 0, 0);
+        if constexpr (THREE) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) s[k0 + k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[k].v, ll.v, s[k0 + k], 0, 0, 0);
+        }
+        if (k0 % 4 == 2) __builtin_amdgcn_sched_barrier(0);
       }
     }
   } else {
     typedef PkTile<T, D> Tile;
-    uint32_t at = (uint32_t)Tile::at(4 * g, (lane & 31) * 4);    // row 16 ks + 8 (i / 4) + 4 g + i % 4: other bits of the key, or none
+    uint32_t at = (uint32_t)Tile::at(4 * g, wv.l * 4);           // row 16 ks + 4 g + i: other bits of the key
     asm volatile("" : "+v"(at));
 #pragma unroll 1
-    for (int ks = from; ks < LA_T / 16; ks += STEP)
+    for (int ks = 0; ks < LA_T / 16; ++ks) {
+      const float4 w4 = *reinterpret_cast<const float4*>(w + 16 * ks + 4 * g);
+      const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = 8 * (i >> 2) + (i & 3), row = 16 * ks + r + 4 * g;
-        const uint32_t to = (uint32_t)(16 * ks + r) * Tile::ROW, key = (uint32_t)Tile::key(r) << 4;
-        float c = *(__attribute__((address_space(3))) const float*)(tc + (at ^ (key ^ (uint32_t)(wv.cs << 7))) + to) * w[row];
-        const bool out = part && (row < c0 || row >= c1);
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * ks + 4 * g + i;
+        const uint32_t to = (uint32_t)(16 * ks + i) * Tile::ROW, key = (uint32_t)Tile::key(i) << 4;
+        const bool out = PART && (row < c0 || row >= c1);
+        float c = *(__attribute__((address_space(3))) const float*)(tc + (at ^ (key ^ (uint32_t)(wv.cs << 6))) + to) * wt[i];
         if (out) c = 0.f;
 #pragma unroll
-        for (int kb = 0; kb < D / 32; ++kb) {
-          float b = *(__attribute__((address_space(3))) const float*)(tb + (at ^ (key ^ (uint32_t)(kb << 7))) + to);
+        for (int kt = 0; kt < D / 16; ++kt) {
+          float b = *(__attribute__((address_space(3))) const float*)(tb + (at ^ (key ^ (uint32_t)(kt << 6))) + to);
           if (out) b = 0.f;
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(b, c, s[kb], 0, 0, 0);
+          s[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(b, c, s[kt], 0, 0, 0);
         }
       }
+    }
   }
 }
 
@@ -243,24 +310,46 @@ template <typename T, int D> __device__ __forceinline__ int64_t la_state_at(cons
   return (((int64_t)b * a.nseq + seq) * a.Hkv + hk) * a.d * a.d;
 }
 template <typename T, int D>
-__device__ __forceinline__ void la_load_state(pk_f16 (&s)[D / 32], const LaJob& J, const LaArgs& a, int b, int seq, int hk, const LaWave<D>& wv) {
+__device__ __forceinline__ void la_load_state(la_f4 (&s)[D / 16], const LaJob& J, const LaArgs& a, int b, int seq, int hk, const LaWave<D>& wv) {
   const float* p = J.S0 + la_state_at<T, D>(a, b, seq, hk);
-  const int col = 32 * wv.cs + (wv.lane & 31), rs = J.flip ? 1 : a.d, cs = J.flip ? a.d : 1;
+  int col = 16 * wv.cs + wv.l;
+  asm volatile("" : "+v"(col));
+  const int rs = J.flip ? 1 : a.d, cs = J.flip ? a.d : 1;
   const float f = 1.f / J.fi;
 #pragma unroll
-  for (int n = 0; n < D / 32; ++n)
+  for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = 32 * n + la_row<T>(i, wv.g);
-      s[n][i] = row < a.d && col < a.d ? f * p[row * rs + col * cs] : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const int row = la_row<T>(kt, i, wv.g);
+      s[kt][i] = row < a.d && col < a.d ? f * p[row * rs + col * cs] : 0.f;
     }
 }
+template <typename T, int D> __device__ __forceinline__ void la_store_state(const la_f4 (&s)[D / 16], float* p, int d, float f, const LaWave<D>& wv) {
+  int col = 16 * wv.cs + wv.l;
+  asm volatile("" : "+v"(col));
+#pragma unroll
+  for (int kt = 0; kt < D / 16; ++kt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = la_row<T>(kt, i, wv.g);
+      if (row < d && col < d) p[row * d + col] = f * s[kt][i];
+    }
+}
+// which sequence a row belongs to: the last one that begins at or before it
+__device__ __forceinline__ int la_sequence(const int32_t* off, int nseq, int r) {
+  int lo = 0;
+  for (int n = nseq; n > 1;) {
+    const int half = n >> 1;
+    if (off[lo + half] <= r) { lo += half; n -= half; } else n = half;
+  }
+  return lo;
+}
 
-template <int N> __device__ __forceinline__ void la_fade(pk_f16 (&s)[N], float m1) {       // s times 1 + m1
+template <int N> __device__ __forceinline__ void la_fade(la_f4 (&s)[N], float m1) {       // s times 1 + m1
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[n][i] = fmaf(s[n][i], m1, s[n][i]);
+    for (int i = 0; i < 4; ++i) s[n][i] = fmaf(s[n][i], m1, s[n][i]);
 }
 
 // Workgroup -> (job, model, head of the job, block)

@@ -10,26 +10,28 @@ int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   return d > 128 || nseq > PACKED_MAX || B > 65535 || (int64_t)B * Hq > 0x3fffff / ((R + LA_T - 1) / LA_T) ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 // Blocks of tiles: about LA_WANT of all heads together.  With R their number only grows, so that the workspace for the most rows serves fewer.
-constexpr int LA_WANT = 512, LA_SCAN = 8;
+constexpr int LA_WANT = 512, LA_SCAN = 8, LA_FEW = 64, LA_SHORT = 256;
 int64_t la_limit(int B, int Hkv) { return (int64_t)B * Hkv < LA_WANT ? LA_WANT / ((int64_t)B * Hkv) : 1; }
 void la_cut(LaArgs& a) {
   const int64_t most = la_limit(a.B, a.Hkv);
   a.tiles = (a.R + LA_T - 1) / LA_T;
   a.per = (int)((a.tiles + most - 1) / most);
   a.blocks = (a.tiles + a.per - 1) / a.per;
-  a.scanned = a.blocks > LA_SCAN;
+  // Short sequences are walked up to a block once more instead of summed: no launches for states.  A long one among them costs its tiles again,
+  // so that this is left to batches of few rows.
+  a.mode = a.blocks == 1 ? LA_ALONE : a.tiles <= LA_FEW && a.R / a.nseq <= LA_SHORT ? LA_WALK : a.blocks > LA_SCAN ? LA_SCANNED : LA_SUMS;
 }
-size_t la_workspace(int B, int R, int Hkv, int d, int jobs) {
+size_t la_workspace(int B, int R, int Hkv, int d, int sums) {
   const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hkv), n = tiles < most ? tiles : most;
   if (n == 1) return 0;
   const int64_t D = la_pad(d);
-  return (size_t)(jobs * n * B * Hkv * D * D * 4 + (jobs * n * B * 4 + 15) / 16 * 16);
+  return (size_t)(sums * n * B * Hkv * D * D * 4 + (sums * n * B * 4 + 15) / 16 * 16);
 }
 void la_place(LaArgs& a, void* workspace) {
   if (a.blocks == 1) return;
   const int64_t D = la_pad(a.d);
   a.sums = reinterpret_cast<float*>(workspace);
-  a.spans = reinterpret_cast<int*>(a.sums + (int64_t)a.jobs * a.blocks * a.B * a.Hkv * D * D);
+  a.spans = reinterpret_cast<int*>(a.sums + (int64_t)a.nsums * a.blocks * a.B * a.Hkv * D * D);
 }
 bool la_ws_ok(void* workspace, size_t have, size_t need) { return need == 0 || (workspace && reinterpret_cast<uintptr_t>(workspace) % 16 == 0 && have >= need); }
 PkStr la_str(const int64_t* s) { return PkStr{s[0], s[1], s[2]}; }
@@ -46,8 +48,9 @@ bool la_vec(const LaArgs& a, int dtype, const void* const* p, int n) {
   return vec;
 }
 int la_run(const LaArgs& a, int dtype, bool vec, hipStream_t st) {
-  const LaForm f{dtype == HFTA_BF16, vec};
-  if (a.blocks > 1) {
+  LaForm f{dtype == HFTA_BF16, vec, false};
+  for (int j = 0; j < a.jobs; ++j) f.pieces = f.pieces || a.job[j].S0 || a.job[j].S1;
+  if (a.mode == LA_SUMS || a.mode == LA_SCANNED) {
     const int rc = la_states(a, f, st);
     if (rc != HFTA_OK) return rc;
   }
@@ -65,7 +68,7 @@ size_t hfta_linear_attention_fwd_workspace_bytes(int B, int R, int nseq, int Hq,
   return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 1) : 0;
 }
 size_t hfta_linear_attention_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
-  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 3) : 0;
+  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 2) : 0;
 }
 
 int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3], const void* K,
@@ -79,9 +82,9 @@ int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   if (rc != HFTA_OK) return rc;
   if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 1))) return HFTA_EWORKSPACE;
   LaArgs a{};
-  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 1;
+  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = a.nsums = 1;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs);
-  a.job[0] = LaJob{Q, K, V, CTX, q, kv, kv, c, state_in, state_out, 0, 0, Hq, Hq / Hkv, 1, scale, 1.f};
+  a.job[0] = LaJob{Q, K, V, CTX, q, kv, kv, c, state_in, state_out, 0, 0, Hq, Hq / Hkv, 1, scale, 1.f, 0, 0};
   la_cut(a);
   la_place(a, workspace);
   const void* p[] = {Q, K, V, CTX};
@@ -98,14 +101,14 @@ int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
       !dQ || !dqs || !dK || !dV || !dkvs || (dstate_in && dstate_in == dstate_out))
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
-  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 3))) return HFTA_EWORKSPACE;
+  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 2))) return HFTA_EWORKSPACE;
   LaArgs a{};
-  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3;
+  a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3; a.nsums = 2;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs), dq = la_str(dqs), dkv = la_str(dkvs);
   const int G = Hq / Hkv;
-  a.job[0] = LaJob{dCTX, V, K, dQ, c, kv, kv, dq, state_in, nullptr, 0, 1, Hq, G, 1, scale, 1.f};
-  a.job[1] = LaJob{K, Q, dCTX, dV, kv, q, c, dkv, dstate_out, dstate_in, 1, 0, Hkv, 1, G, scale, scale};
-  a.job[2] = LaJob{V, dCTX, Q, dK, kv, c, q, dkv, dstate_out, nullptr, 1, 1, Hkv, 1, G, scale, scale};
+  a.job[0] = LaJob{dCTX, V, K, dQ, c, kv, kv, dq, state_in, nullptr, 0, 1, Hq, G, 1, scale, 1.f, 0, 0};
+  a.job[1] = LaJob{K, Q, dCTX, dV, kv, q, c, dkv, dstate_out, dstate_in, 1, 0, Hkv, 1, G, scale, scale, 1, 0};
+  a.job[2] = LaJob{V, dCTX, Q, dK, kv, c, q, dkv, dstate_out, nullptr, 1, 1, Hkv, 1, G, scale, scale, 1, 1};
   la_cut(a);
   la_place(a, workspace);
   const void* p[] = {Q, K, V, dCTX, dQ, dK, dV};

@@ -5,11 +5,10 @@ namespace hfta {
 namespace {
 
 // What the sequence of a block's last row, if it goes on, has gathered in this block
-template <typename T, int D, bool VEC> __global__ __launch_bounds__(256, (D * sizeof(T) <= 256 ? 2 : 1)) void la_block_kernel(LaArgs a) {
+template <typename T, int D, bool VEC, bool PIECES> __global__ __launch_bounds__(4 * D, (sizeof(T) == 2 || D < 128 ? 4 : 2)) void la_block_kernel(LaArgs a) {
   typedef LaStage<T, D, VEC> Stage;
-  constexpr int TH = LaWave<D>::TH;
-  constexpr int JOIN = (TH - 1) * D * D * 4;                     // bytes of partial states
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[JOIN > 2 * Stage::BYTES ? JOIN : 2 * Stage::BYTES];
+  constexpr int NT = LaWave<D>::NT;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * Stage::BYTES];
   __shared__ PackedRows<LA_T> pr;
   __shared__ __attribute__((aligned(16))) float pw[LA_T], wt[LA_T];
   const LaWave<D> wv;
@@ -19,67 +18,47 @@ template <typename T, int D, bool VEC> __global__ __launch_bounds__(256, (D * si
   const int first = at.blk * a.per, last = first + a.per - 1;
   if (at.blk == a.blocks - 1) return;                            // hands on nothing
   const int32_t* off = a.off + (int64_t)at.b * (a.nseq + 1);
-  const float g = la_decay(a.ld[(int64_t)at.b * a.Hkv + hk]);
-  if (t < LA_T) pw[t] = la_pow(g, t);
+  const float ld = la_decay(a.ld[(int64_t)at.b * a.Hkv + hk]);
+  if (t < LA_T) pw[t] = la_pow(ld, t);
   const int a0 = (rev ? a.tiles - 1 - last : last) * LA_T, j = rev ? 0 : LA_T - 1;
-  pr.template scan<256>(off, a.nseq, a.R, a0);
+  pr.template scan<NT>(off, a.nseq, a.R, a0);
   int start, end;
   const bool on = a0 + j < a.R && pr.range(a0, j, start, end) && (rev ? start < a0 : end > a0 + LA_T);
   const int begin = rev ? a.tiles * LA_T - end : start;          // of the sequence, in the order of the walk
   if (t == 0 && hk == 0) a.spans[((int64_t)at.job * a.B + at.b) * a.blocks + at.blk] = !on ? 0 : begin < first * LA_T ? 2 : 1;
   if (!on) return;
-  pk_f16 s[D / 32];
+  la_f4 s[D / 16];
 #pragma unroll
-  for (int n = 0; n < D / 32; ++n) s[n] = pk_f16{};
+  for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
   const bool fresh = begin >= first * LA_T;
-  if (fresh && J.S0 && (TH == 1 || wv.th == 0)) {
-    int lo = 0, n = a.nseq;                                      // the last sequence that begins at or before the row
-    const int r = a0 + j;
-    while (n > 1) {
-      const int half = n >> 1;
-      if (off[lo + half] <= r) { lo += half; n -= half; } else n = half;
-    }
-    la_load_state<T, D>(s, J, a, at.b, lo, hk, wv);
-  }
-  const T* pb = pk_at<T>(J.B, J.bs, at.b, 0);
-  const T* pc = pk_at<T>(J.C, J.cs, at.b, 0);
+  if (PIECES && fresh && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, a0 + j), hk, wv);
+  const T* pb = pk_at<T>(J.B, J.bs, at.b, hk * J.gb);
+  const T* pc = pk_at<T>(J.C, J.cs, at.b, hk * J.gb);
+  Stage sb, sc;
+  sb.init(J.bs.r, a.d, rev);
+  sc.init(J.cs.r, a.d, rev);
+  const la_lds lb = (la_lds)tiles, lc = (la_lds)tiles + Stage::BYTES;
+  const float m64 = la_powm1(ld, LA_T);
+#pragma unroll 1
   for (int tile = fresh ? begin / LA_T : first; tile <= last; ++tile) {
     const int c0 = max(begin - tile * LA_T, 0), m0 = (rev ? a.tiles - 1 - tile : tile) * LA_T;
     // against the order, what comes in behind the last row has not faded when that row is taken
-    la_fade(s, la_powm1(g, LA_T - c0 - (rev && fresh && tile == begin / LA_T ? 1 : 0)));
+    const int n = LA_T - c0 - (PIECES && J.S0 && rev && fresh && tile == begin / LA_T ? 1 : 0);
+    la_fade(s, n == LA_T ? m64 : la_powm1(ld, n));
+#pragma unroll 1
     for (int h = 0; h < J.gb; ++h) {
-      const int hb = hk * J.gb + h;
       __syncthreads();
       if (t < LA_T) wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
-      Stage::fetch((la_lds)tiles, pb + hb * J.bs.h + (int64_t)m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
-      Stage::fetch((la_lds)tiles + Stage::BYTES, pc + hb * J.cs.h + (int64_t)m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
+      sb.fetch(lb, pb + h * J.bs.h + m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
+      sc.fetch(lc, pc + h * J.cs.h + m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
       la_land<VEC>();
-      la_update<T, D, TH>(s, (la_lds)tiles, (la_lds)tiles + Stage::BYTES, wt, c0, LA_T, c0 > 0, J.S1 != nullptr, wv, wv.th);
+      if (c0 > 0) la_update<T, D, true, PIECES>(s, lb, lc, wt, c0, LA_T, wv);
+      else la_update<T, D, false, PIECES>(s, lb, lc, wt, c0, LA_T, wv);
     }
   }
   float* sums = a.sums + ((((int64_t)at.job * a.B + at.b) * a.Hkv + hk) * a.blocks + at.blk) * (D * D);
-  if constexpr (TH > 1) {                                        // wavefronts that took other rows of the same columns
-    float* lds = reinterpret_cast<float*>(tiles);
-    __syncthreads();
-    if (wv.th > 0) {
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) lds[(((wv.th - 1) * (D / 32) + wv.cs) * (D / 32) + n) * 1024 + i * 64 + wv.lane] = s[n][i];
-    }
-    __syncthreads();
-    if (wv.th > 0) return;
-    for (int w = 0; w < TH - 1; ++w)
-#pragma unroll
-      for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] += lds[((w * (D / 32) + wv.cs) * (D / 32) + n) * 1024 + i * 64 + wv.lane];
-  }
-#pragma unroll
-  for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *la_sum<D>(sums, wv.cs, n, q, wv.lane) = make_float4(s[n][4 * q], s[n][4 * q + 1], s[n][4 * q + 2], s[n][4 * q + 3]);
+  for (int kt = 0; kt < D / 16; ++kt) *la_sum<D>(sums, wv.cs, kt, wv.lane) = s[kt];
 }
 
 // Sums along the sequences, in place: a thread has four entries of a state and walks the blocks, eight blocks' loads in flight
@@ -118,12 +97,14 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, int entries) {
 }
 
 template <typename T, int D> int launch(const LaArgs& a, const LaForm& f, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.blocks * a.B * a.Hkv * a.jobs)), block(256);
-  if (f.vec) hipLaunchKernelGGL((la_block_kernel<T, D, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((la_block_kernel<T, D, false>), grid, block, 0, st, a);
-  if (a.scanned) {
+  const dim3 grid((unsigned)((int64_t)a.blocks * a.B * a.Hkv * a.nsums)), block(LaWave<D>::NT);
+  if (f.vec && f.pieces) hipLaunchKernelGGL((la_block_kernel<T, D, true, true>), grid, block, 0, st, a);
+  else if (f.vec) hipLaunchKernelGGL((la_block_kernel<T, D, true, false>), grid, block, 0, st, a);
+  else if (f.pieces) hipLaunchKernelGGL((la_block_kernel<T, D, false, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((la_block_kernel<T, D, false, false>), grid, block, 0, st, a);
+  if (a.mode == LA_SCANNED) {
     const int entries = D * D / 4;
-    hipLaunchKernelGGL(la_scan_kernel, dim3((entries + 255) / 256, (unsigned)(a.jobs * a.B * a.Hkv)), dim3(256), 0, st, a, entries);
+    hipLaunchKernelGGL(la_scan_kernel, dim3((entries + 255) / 256, (unsigned)(a.nsums * a.B * a.Hkv)), dim3(256), 0, st, a, entries);
   }
   return launch_status();
 }
