@@ -79,6 +79,15 @@ template <int D> struct LaWave {
     l = lane & 15;
     g = lane >> 4;
   }
+  // the same once more, hidden from the compiler: what follows from it is formed where it is needed, not kept in registers from before a loop
+  __device__ __forceinline__ LaWave again() const {
+    LaWave w = *this;
+    asm volatile("" : "+v"(w.lane));
+    w.l = w.lane & 15;
+    w.g = w.lane >> 4;
+    return w;
+  }
+  __device__ __forceinline__ int t() const { return 64 * cs + lane; }
 };
 
 // 64 rows of a [row][D] matrix into LDS, rows that are not there and columns from d on zero; flip: the last row first.  In whole pieces the loads
@@ -123,6 +132,14 @@ template <typename T, int D, bool VEC> struct LaStage {
     }
   }
 };
+// zeros in the first n rows of two tiles that lie behind each other; barriers around it are the caller's
+template <typename T, int D> __device__ __forceinline__ void la_clear(la_lds tile, int n) {
+  typedef __attribute__((address_space(3))) pk_i4* la_i4;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (int i = (int)threadIdx.x * 16; i < n * PkTile<T, D>::ROW; i += LaWave<D>::NT * 16)
+      *(la_i4)(tile + k * LA_T * PkTile<T, D>::ROW + i) = pk_i4{0, 0, 0, 0};
+}
 // until the loads into LDS have landed, for all wavefronts
 template <bool VEC> __device__ __forceinline__ void la_land() {
   if constexpr (VEC) pk_landed();

@@ -40,7 +40,7 @@ struct LaP {
 // sequence of a tile.  The next tile of A is on its way while one is computed, those of B and C when this one's have been read.  A result takes
 // the place of its rows of A, from where it is stored in whole pieces.  (Two workgroups of 128 columns of bf16 fill the LDS.)
 template <typename T, int D, bool VEC, bool PIECES>
-__global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) void la_main_kernel(LaArgs a) {
+__global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 : D == 128 ? 4 : 3)) void la_main_kernel(LaArgs a) {
   typedef LaStage<T, D, VEC> Stage;
   typedef PkTile<T, D> Tile;
   constexpr bool BF = sizeof(T) == 2;
@@ -50,8 +50,8 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
   __shared__ __attribute__((aligned(16))) LaStep steps[2];
   __shared__ float dw[2 * LA_T + 1], fade[LA_T + 1];             // lambda^n behind LA_T places of nothing; lambda^n - 1
   float* const pw = dw + LA_T;
-  const LaWave<D> wv;
-  const int lane = wv.lane, l = wv.l, g = wv.g, t = threadIdx.x;
+  const LaWave<D> wave;
+  const int t = threadIdx.x;
   const LaPlace at(a, false);
   const LaJob& J = a.job[at.job];
   const int rev = J.rev, hk = at.h / J.ga, G = J.gb;
@@ -92,8 +92,8 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
         const int s = s0 + t, lo = s < a.nseq ? min(max(off[s], 0), a.R) : 0, hi = s < a.nseq ? min(max(off[s + 1], 0), a.R) : 1;
         uint64_t m = __ballot(lo >= hi);
         for (; m; m &= m - 1) {
-          const int64_t p = la_state_at<T, D>(a, at.b, s0 + wv.cs * 64 + __builtin_ctzll(m), hk);
-          for (int i = lane; i < a.d * a.d; i += 64) J.S1[p + i] = J.S0 ? J.S0[p + i] : 0.f;
+          const int64_t p = la_state_at<T, D>(a, at.b, s0 + wave.cs * 64 + __builtin_ctzll(m), hk);
+          for (int i = wave.lane; i < a.d * a.d; i += 64) J.S1[p + i] = J.S0 ? J.S0[p + i] : 0.f;
         }
       }
   }
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
   auto look = [&](int m0) __attribute__((always_inline)) {                                      // up the sequences of the rows from the tile at m0 on, in the order of the walk
     const int t0 = rev ? m0 + LA_T - LA_SPAN : m0;
     pr.template scan<NT>(off, a.nseq, a.R, t0);
-    span.take(pr, t0, lane);
+    span.take(pr, t0, wave.lane);
   };
   look(row0(first));                                             // (its barriers make pw visible too)
 
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
     if (begin < first * LA_T) {
       if (a.mode == LA_WALK) {
         // sequences are short: their rows up to here once more.  c's and b's tiles lie where the walk's will
-        if (PIECES && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + r), hk, wv);
+        if (PIECES && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + r), hk, wave);
 #pragma unroll 1
         for (int tile = begin / LA_T; tile < first; ++tile) {
           const int c0 = max(begin - tile * LA_T, 0), n = LA_T - c0 - (PIECES && J.S0 && rev && tile == begin / LA_T ? 1 : 0);
@@ -129,8 +129,11 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
             if (t < LA_T) steps[0].wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
             fetch_bc(tile, h);
             la_land<VEC>();
-            if (c0 > 0) la_update<T, D, true, PIECES>(s, lb, lc, steps[0].wt, c0, LA_T, wv);
-            else la_update<T, D, false, PIECES>(s, lb, lc, steps[0].wt, c0, LA_T, wv);
+            if (c0 > 0) {
+              la_clear<T, D>(lb, c0);
+              __syncthreads();
+            }
+            la_update<T, D, false, PIECES>(s, lb, lc, steps[0].wt, 0, LA_T, wave);
           }
         }
         __syncthreads();
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
 #pragma unroll 1
         for (int k = a.mode == LA_SCANNED ? at.blk - 1 : begin / (a.per * LA_T); k < at.blk; ++k) {
           la_fade(s, m1);
-          la_add_sum<T, D>(s, sum + (int64_t)k * (D * D), J.turned, wv);
+          la_add_sum<T, D>(s, sum + (int64_t)k * (D * D), J.turned, wave);
         }
       }
     }
@@ -151,8 +154,9 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
   for (int tile = first; tile <= last; ++tile, x ^= 1) {
     const int m0 = row0(tile);
     if (tile > first && (tile - first) % (LA_SPAN / LA_T) == 0) look(m0);       // (behind a barrier, at the end of the last tile)
+    LaWave<D> wv = wave.again();
     int start, end;
-    const int r = rev ? LA_T - 1 - lane : lane;                  // (every wavefront for itself: a lane has a row)
+    const int r = rev ? LA_T - 1 - wv.lane : wv.lane;            // (every wavefront for itself: a lane has a row)
     const bool in = span.range(m0, r, start, end) && m0 + r < a.R;
     const int mine = !in ? LA_NONE : max(rev ? m0 + LA_T - end : start - m0, -1);
     const uint64_t there = __ballot(in), finals = PIECES ? __ballot(in && m0 + r == (rev ? start : end - 1)) : 0;
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
       const bool begins = PIECES && val >= 0 && val != LA_NONE;
       p1 = LA_T;
       if constexpr (PIECES) {
-        const uint64_t m = __ballot(mine != val && lane > p0);
+        const uint64_t m = __ballot(mine != val && wv.lane > p0);
         if (m) p1 = __builtin_ctzll(m);
       }
       const uint64_t rest = PIECES && p1 < LA_T ? there >> p1 << p1 : 0;
@@ -183,7 +187,9 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
       for (int n = 0; n < 4; ++n) acc[n] = la_f4{0.f, 0.f, 0.f, 0.f};
       for (int h = 0; h < G; ++h, ++step) {
         LaStep& S = steps[step & 1];
-        if (t < LA_T) {
+        wv = wave.again();
+        if (wv.cs == 0) {
+          const int t = wv.lane;
           S.rel[t] = mine;
           S.wt[t] = t >= c0 && t < p1 ? pw[p1 - 1 - t] : 0.f;
           S.fac[t] = PIECES ? (t >= p0 && t < p1 ? pw[t - p0 + 1 - late] : 0.f) : mine == -1 ? pw[t + 1] : 0.f;
@@ -193,9 +199,8 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
         if (!more_h && more_t) fetch_a(tile + 1, x ^ 1);
         const unsigned char* ta = tiles + x * Stage::BYTES;
         // a lane's piece of row l of a tile is 16 g bytes on; addresses are formed where they are needed, or they would fill the registers
-        uint32_t ar = (uint32_t)Tile::at(l, 16 * g);
-        int lr = l;
-        asm volatile("" : "+v"(ar), "+v"(lr));
+        wv = wave.again();
+        const uint32_t ar = (uint32_t)Tile::at(wv.l, 16 * wv.g);
         if (there) {
 #pragma unroll
           for (int u = 0; u < 6; u += WAVES) {                   // (A B^T) . D: 16 rows t by 32 rows s
@@ -219,10 +224,10 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
                 }
               }
             }
-            int self = 16 * ti + l - 32 * si - 4 * g;            // s counts from 32 si + 4 g: 16 k + i
-            asm volatile("" : "+v"(self));
+            const LaWave<D> wu = wave.again();
+            const int self = 16 * ti + wu.l - 32 * si - 4 * wu.g;       // s counts from 32 si + 4 g: 16 k + i
             if (mixed) {
-              const int rel = S.rel[self + 32 * si + 4 * g] - 32 * si - 4 * g;
+              const int rel = S.rel[16 * ti + wu.l] - 32 * si - 4 * wu.g;
 #pragma unroll
               for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -233,9 +238,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
             for (int k = 0; k < 2; ++k)
 #pragma unroll
               for (int i = 0; i < 4; ++i) y[k][i] = 16 * k + i <= self ? y[k][i] * decay[19 - 16 * k - i] : 0.f;
-            int lp = lane * 16;
-            asm volatile("" : "+v"(lp));
-            unsigned char* to = P + unit * LaP::PART + lp;
+            unsigned char* to = P + unit * LaP::PART + wu.lane * 16;
             if constexpr (BF) {
               LaFrag hi, lo;
 #pragma unroll
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
           }
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
-            const int row = 16 * n + lr;
+            const int row = 16 * n + wv.l;
             const float f = S.fac[row];
             const bool sees = PIECES ? row >= p0 && row < p1 : S.rel[row] == -1;
 #pragma unroll
@@ -289,13 +292,12 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
         }
         __syncthreads();
         if (there) {                                             // the masked products with c
-          int lp = lane * 16;
-          asm volatile("" : "+v"(lp));
-          const unsigned char* pl = P + lp;
+          wv = wave.again();
+          const unsigned char* pl = P + wv.lane * 16;
           if constexpr (BF) {
             LaFrag c[2];
             uint32_t odd = 0;
-            const uint32_t at_c = la_cols_at<D, false>(lane);
+            const uint32_t at_c = la_cols_at<D, false>(wv.lane);
 #pragma unroll
             for (int k = 0; k < 2; ++k) la_cols<D>(c[k], lc, at_c, 32 * k, 16 * wv.cs);
 #pragma unroll
@@ -329,8 +331,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
             if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, S.rel);
           } else {
             // a column's values of the four quarters' rows 16 q + 4 g + e
-            uint32_t ac = (uint32_t)Tile::at(4 * g, (16 * wv.cs + l) * 4);
-            asm volatile("" : "+v"(ac));
+            const uint32_t ac = (uint32_t)Tile::at(4 * wv.g, (16 * wv.cs + wv.l) * 4);
             auto value = [&](int row) __attribute__((always_inline)) { return *reinterpret_cast<const float*>(tc + (ac ^ (uint32_t)(Tile::key(row) << 4)) + row * ROW); };
             float c[16], z = 0.f;
 #pragma unroll
@@ -356,11 +357,11 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
             if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, S.rel);
           }
           if (h == G - 1) {                                      // the result's rows in place of A's
-            uint32_t ao = (uint32_t)Tile::at(l, (16 * wv.cs + 4 * g) * (int)sizeof(T));
-            asm volatile("" : "+v"(ao));
+            wv = wave.again();
+            const uint32_t ao = (uint32_t)Tile::at(wv.l, (16 * wv.cs + 4 * wv.g) * (int)sizeof(T));
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-              const int row = 16 * n + lr;
+              const int row = 16 * n + wv.l;
               if (PIECES && (row < p0 || row >= p1)) continue;
               unsigned char* p = tiles + x * Stage::BYTES + ao + 16 * n * ROW;
               const la_f4 o = J.fo * acc[n];
@@ -370,6 +371,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
           }
         }
         if (updates) {
+          wv = wave.again();
           if (h == 0) {
             if (!PIECES && val >= 0) {                           // a sequence that began in this tile
 #pragma unroll
@@ -378,8 +380,16 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
               la_fade(s, fade[p1 - c0 - late]);
             }
           }
-          if (c0 > 0 || p1 < LA_T) la_update<T, D, true, PIECES>(s, lb, lc, S.wt, c0, p1, wv);
-          else la_update<T, D, false, PIECES>(s, lb, lc, S.wt, c0, p1, wv);
+          if (PIECES && (c0 > 0 || p1 < LA_T)) {
+            la_update<T, D, true, PIECES>(s, lb, lc, S.wt, c0, p1, wv);
+          } else {
+            if (c0 > 0) {                                        // rows of other sequences: what stands there does not matter
+              __syncthreads();
+              la_clear<T, D>(lb, c0);
+              __syncthreads();
+            }
+            la_update<T, D, false, PIECES>(s, lb, lc, S.wt, 0, LA_T, wv);
+          }
         }
         __syncthreads();                                         // the step's tiles have been read, its results lie in LDS
         if (more_h || again) fetch_bc(tile, more_h ? h + 1 : 0);
@@ -395,9 +405,10 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 ? 2 : D == 128 ? 4 : 3)) voi
     if (there) {
       const unsigned char* from = tiles + x * Stage::BYTES;
       const int* rel = steps[(step + 1) & 1].rel;
+      wv = wave.again();
 #pragma unroll
       for (int n = 0; n < Stage::N; ++n) {
-        const int q = n * NT + t, row = q / Tile::PPR, c = ((q % Tile::PPR) ^ Tile::key(row)) * Stage::EPP;
+        const int q = n * NT + wv.t(), row = q / Tile::PPR, c = ((q % Tile::PPR) ^ Tile::key(row)) * Stage::EPP;
         if (rel[row] == LA_NONE || c >= a.d) continue;
         union { uint4 u; piece_u4 p; T e[Stage::EPP]; } v;
         v.u = *reinterpret_cast<const uint4*>(from + q * 16);

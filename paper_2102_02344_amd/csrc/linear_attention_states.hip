@@ -52,8 +52,11 @@ template <typename T, int D, bool VEC, bool PIECES> __global__ __launch_bounds__
       sb.fetch(lb, pb + h * J.bs.h + m0 * J.bs.r, J.bs.r, a.R - m0, a.d, rev);
       sc.fetch(lc, pc + h * J.cs.h + m0 * J.cs.r, J.cs.r, a.R - m0, a.d, rev);
       la_land<VEC>();
-      if (c0 > 0) la_update<T, D, true, PIECES>(s, lb, lc, wt, c0, LA_T, wv);
-      else la_update<T, D, false, PIECES>(s, lb, lc, wt, c0, LA_T, wv);
+      if (c0 > 0) {                                              // (what stands in rows of other sequences does not matter)
+        la_clear<T, D>(lb, c0);
+        __syncthreads();
+      }
+      la_update<T, D, false, PIECES>(s, lb, lc, wt, 0, LA_T, wv);
     }
   }
   float* sums = a.sums + ((((int64_t)at.job * a.B + at.b) * a.Hkv + hk) * a.blocks + at.blk) * (D * D);
