@@ -41,7 +41,7 @@ struct LaJob {
   float* S1;
   int rev;                         // against the order
   int flip;                        // the state's rows and columns change places in memory
-  int heads, ga, gb;               // workgroups' heads of a model; heads of A (B and C) that belong to one of them: h / ga, h * gb ..
+  int ga, gb;                      // a workgroup has a head h of A; the key head is h / ga, and it has gb heads of B and C
   float fo, fi;                    // results times fo, states in memory times 1 / fi
   int sum, turned;                 // which blocks' sums are its states, and whether they are of C and B instead (rows and columns change places)
 };
@@ -54,6 +54,7 @@ struct LaArgs {
   int* spans;                      // [sum][model][block]: 0: no sequence goes on behind the block, 1: one that began in it, 2: one from before it
   int B, R, nseq, Hkv, d, jobs, nsums, tiles, per, blocks;       // tiles in all and of a block, blocks
   int mode;
+  PkDiv by_heads, by_hq, by_key_heads, by_hkv;                   // B times query heads, query heads, and of key heads
 };
 struct LaForm { bool bf16, vec, pieces; };                     // storage, rows in 16-byte pieces, states that come in or go out
 int la_states(const LaArgs& a, const LaForm& f, hipStream_t st); // linear_attention_states.hip
@@ -352,12 +353,16 @@ template <typename T, int D> __device__ __forceinline__ void la_store_state(cons
       if (row < d && col < d) p[row * d + col] = f * s[kt][i];
     }
 }
-// which sequence a row belongs to: the last one that begins at or before it
+// which sequence a row belongs to: the last one that begins at or before it, sixty-four places a step (every lane the same row)
 __device__ __forceinline__ int la_sequence(const int32_t* off, int nseq, int r) {
+  const int lane = threadIdx.x & 63;
   int lo = 0;
   for (int n = nseq; n > 1;) {
-    const int half = n >> 1;
-    if (off[lo + half] <= r) { lo += half; n -= half; } else n = half;
+    const int step = (n + 63) >> 6;
+    const int le = __popcll(__ballot(lane * step < n && off[min(lo + lane * step, nseq - 1)] <= r));
+    const int skip = max(le - 1, 0) * step;
+    lo += skip;
+    n = min(step, n - skip);
   }
   return lo;
 }
@@ -369,20 +374,52 @@ template <int N> __device__ __forceinline__ void la_fade(la_f4 (&s)[N], float m1
     for (int i = 0; i < 4; ++i) s[n][i] = fmaf(s[n][i], m1, s[n][i]);
 }
 
-// Workgroup -> (job, model, head of the job, block)
+// Workgroup -> (job, model, head of the job, block).  Jobs with as many heads as each other take turns, eight workgroups each, so that a head's and
+// block's jobs, which read the same tiles, follow each other on the same XCD.
 struct LaPlace {
   int job, b, h, blk;
+  bool none;                       // past the last place
   __device__ __forceinline__ LaPlace(const LaArgs& a, bool key_heads) {
-    int64_t x = blockIdx.x;
-    for (job = 0;; ++job) {
-      const int64_t n = (int64_t)a.blocks * a.B * (key_heads ? a.Hkv : a.job[job].heads);
-      if (x < n || job == a.jobs - 1) break;
-      x -= n;
+    uint32_t x = blockIdx.x;
+    job = 0;
+    PkDiv by = key_heads ? a.by_key_heads : a.by_heads;          // (B times heads, heads)
+    PkDiv of = key_heads ? a.by_hkv : a.by_hq;
+    uint32_t n = (uint32_t)a.blocks * by.d;
+    if (key_heads) {
+      while (x >= n && job < a.nsums - 1) { x -= n; ++job; }
+    } else {
+      const int turns = a.jobs == 1 ? 1 : a.by_hq.d == a.by_hkv.d ? 3 : 2;       // jobs that take turns: all, or the last two
+      if (a.jobs == 3 && turns == 2) {
+        if (x < n) {
+          turns_of(x, 1);
+        } else {
+          x -= n;
+          by = a.by_key_heads;
+          of = a.by_hkv;
+          n = (uint32_t)a.blocks * by.d;
+          turns_of(x, 2);
+          ++job;
+        }
+      } else {
+        turns_of(x, turns);
+      }
     }
-    const int heads = key_heads ? a.Hkv : a.job[job].heads, bh = (int)(x % ((int64_t)a.B * heads));
-    blk = (int)(x / ((int64_t)a.B * heads));
-    b = bh / heads;
-    h = bh % heads;
+    none = x >= n;
+    const uint32_t k = by(x), bh = x - k * by.d;
+    blk = (int)k;
+    b = (int)of(bh);
+    h = (int)(bh - (uint32_t)b * of.d);
+  }
+  __device__ __forceinline__ void turns_of(uint32_t& x, int turns) {
+    if (turns == 1) return;
+    const uint32_t eight = x >> 3, q = turns == 2 ? eight >> 1 : eight / 3u;
+    job = (int)(eight - q * (uint32_t)turns);
+    x = q << 3 | (x & 7);
+  }
+  // workgroups in all
+  static int64_t count(const LaArgs& a, bool key_heads) {
+    const int64_t k = (int64_t)a.blocks * a.by_key_heads.d, q = (int64_t)a.blocks * a.by_heads.d, k8 = (k + 7) / 8 * 8, q8 = (q + 7) / 8 * 8;
+    return key_heads ? k * a.nsums : a.jobs == 1 ? q : a.by_hq.d == a.by_hkv.d ? 3 * q8 : q + 2 * k8;
   }
 };
 

@@ -11,9 +11,15 @@ int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
 }
 // Blocks of tiles: about LA_WANT of all heads together.  With R their number only grows, so that the workspace for the most rows serves fewer.
 constexpr int LA_WANT = 512, LA_SCAN = 8, LA_FEW = 64, LA_SHORT = 256;
-int64_t la_limit(int B, int Hkv) { return (int64_t)B * Hkv < LA_WANT ? LA_WANT / ((int64_t)B * Hkv) : 1; }
-void la_cut(LaArgs& a) {
-  const int64_t most = la_limit(a.B, a.Hkv);
+int64_t la_limit(int B, int Hkv, int want) { return (int64_t)B * Hkv < want ? want / ((int64_t)B * Hkv) : 1; }
+void la_cut(LaArgs& a, int Hq, int dtype) {
+  a.by_heads = PkDiv((uint32_t)(a.B * Hq));
+  a.by_hq = PkDiv((uint32_t)Hq);
+  a.by_key_heads = PkDiv((uint32_t)(a.B * a.Hkv));
+  a.by_hkv = PkDiv((uint32_t)a.Hkv);
+  bool states = false;
+  for (int j = 0; j < a.jobs; ++j) states = states || a.job[j].S0 || a.job[j].S1;
+  const int64_t most = la_limit(a.B, a.Hkv, a.d > 64 && (dtype == HFTA_F32 || states) ? LA_WANT / 2 : LA_WANT);
   a.tiles = (a.R + LA_T - 1) / LA_T;
   a.per = (int)((a.tiles + most - 1) / most);
   a.blocks = (a.tiles + a.per - 1) / a.per;
@@ -22,7 +28,7 @@ void la_cut(LaArgs& a) {
   a.mode = a.blocks == 1 ? LA_ALONE : a.tiles <= LA_FEW && a.R / a.nseq <= LA_SHORT ? LA_WALK : a.blocks > LA_SCAN ? LA_SCANNED : LA_SUMS;
 }
 size_t la_workspace(int B, int R, int Hkv, int d, int sums) {
-  const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hkv), n = tiles < most ? tiles : most;
+  const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hkv, LA_WANT), n = tiles < most ? tiles : most;
   if (n == 1) return 0;
   const int64_t D = la_pad(d);
   return (size_t)(sums * n * B * Hkv * D * D * 4 + (sums * n * B * 4 + 15) / 16 * 16);
@@ -84,8 +90,8 @@ int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   LaArgs a{};
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = a.nsums = 1;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs);
-  a.job[0] = LaJob{Q, K, V, CTX, q, kv, kv, c, state_in, state_out, 0, 0, Hq, Hq / Hkv, 1, scale, 1.f, 0, 0};
-  la_cut(a);
+  a.job[0] = LaJob{Q, K, V, CTX, q, kv, kv, c, state_in, state_out, 0, 0, Hq / Hkv, 1, scale, 1.f, 0, 0};
+  la_cut(a, Hq, dtype);
   la_place(a, workspace);
   const void* p[] = {Q, K, V, CTX};
   return la_run(a, dtype, la_vec(a, dtype, p, 4), as_stream(stream));
@@ -106,10 +112,10 @@ int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3; a.nsums = 2;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs), dq = la_str(dqs), dkv = la_str(dkvs);
   const int G = Hq / Hkv;
-  a.job[0] = LaJob{dCTX, V, K, dQ, c, kv, kv, dq, state_in, nullptr, 0, 1, Hq, G, 1, scale, 1.f, 0, 0};
-  a.job[1] = LaJob{K, Q, dCTX, dV, kv, q, c, dkv, dstate_out, dstate_in, 1, 0, Hkv, 1, G, scale, scale, 1, 0};
-  a.job[2] = LaJob{V, dCTX, Q, dK, kv, c, q, dkv, dstate_out, nullptr, 1, 1, Hkv, 1, G, scale, scale, 1, 1};
-  la_cut(a);
+  a.job[0] = LaJob{dCTX, V, K, dQ, c, kv, kv, dq, state_in, nullptr, 0, 1, G, 1, scale, 1.f, 0, 0};
+  a.job[1] = LaJob{K, Q, dCTX, dV, kv, q, c, dkv, dstate_out, dstate_in, 1, 0, 1, G, scale, scale, 1, 0};
+  a.job[2] = LaJob{V, dCTX, Q, dK, kv, c, q, dkv, dstate_out, nullptr, 1, 1, 1, G, scale, scale, 1, 1};
+  la_cut(a, Hq, dtype);
   la_place(a, workspace);
   const void* p[] = {Q, K, V, dCTX, dQ, dK, dV};
   return la_run(a, dtype, la_vec(a, dtype, p, 7), as_stream(stream));

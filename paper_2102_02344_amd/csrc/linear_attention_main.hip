@@ -53,6 +53,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   const LaWave<D> wave;
   const int t = threadIdx.x;
   const LaPlace at(a, false);
+  if (at.none) return;
   const LaJob& J = a.job[at.job];
   const int rev = J.rev, hk = at.h / J.ga, G = J.gb;
   const int32_t* off = a.off + (int64_t)at.b * (a.nseq + 1);
@@ -77,9 +78,16 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
     sb.fetch(lb, pb + h * J.bs.h + m0 * ldb, ldb, a.R - m0, a.d, rev);
     sc.fetch(lc, pc + h * J.cs.h + m0 * ldc, ldc, a.R - m0, a.d, rev);
   };
+  const float raw = a.ld[(int64_t)at.b * a.Hkv + hk];
   fetch_a(first, 0);
   if (a.mode != LA_WALK) fetch_bc(first, 0);
-  const float ld = la_decay(a.ld[(int64_t)at.b * a.Hkv + hk]);
+  la_f4 s[D / 16];
+#pragma unroll
+  for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
+  float* const sum = a.sums + (((int64_t)J.sum * a.B + at.b) * a.Hkv + hk) * a.blocks * (D * D);
+  const bool scanned = a.mode == LA_SCANNED && first > 0;
+  if (scanned) la_add_sum<T, D>(s, sum + (int64_t)(at.blk - 1) * (D * D), J.turned, wave);        // (before it is known whether a sequence goes on here)
+  const float ld = la_decay(raw);
   if (t <= LA_T) {
     pw[t] = la_pow(ld, t);
     fade[t] = la_powm1(ld, t);
@@ -87,20 +95,18 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   if (t < LA_T) dw[t] = 0.f;
 
   if constexpr (PIECES) {
-    if (keeps)                                                   // sequences without rows
-      for (int s0 = at.blk * NT; s0 < a.nseq; s0 += a.blocks * NT) {
-        const int s = s0 + t, lo = s < a.nseq ? min(max(off[s], 0), a.R) : 0, hi = s < a.nseq ? min(max(off[s + 1], 0), a.R) : 1;
+    if (keeps)                                                   // sequences without rows, by all wavefronts
+      for (int s0 = at.blk * 64; s0 < a.nseq; s0 += a.blocks * 64) {
+        const int s = s0 + wave.lane, lo = s < a.nseq ? min(max(off[s], 0), a.R) : 0, hi = s < a.nseq ? min(max(off[s + 1], 0), a.R) : 1;
         uint64_t m = __ballot(lo >= hi);
         for (; m; m &= m - 1) {
-          const int64_t p = la_state_at<T, D>(a, at.b, s0 + wave.cs * 64 + __builtin_ctzll(m), hk);
-          for (int i = wave.lane; i < a.d * a.d; i += 64) J.S1[p + i] = J.S0 ? J.S0[p + i] : 0.f;
+          const int64_t p = la_state_at<T, D>(a, at.b, s0 + __builtin_ctzll(m), hk);
+#pragma unroll 8
+          for (int i = t; i < a.d * a.d; i += NT) J.S1[p + i] = J.S0 ? J.S0[p + i] : 0.f;
         }
       }
   }
 
-  la_f4 s[D / 16];
-#pragma unroll
-  for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
   LaSpan span;
   auto look = [&](int m0) __attribute__((always_inline)) {                                      // up the sequences of the rows from the tile at m0 on, in the order of the walk
     const int t0 = rev ? m0 + LA_T - LA_SPAN : m0;
@@ -115,37 +121,37 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
     const int m0 = row0(first), r = rev ? LA_T - 1 : 0;
     const bool in = m0 + r < a.R && span.range(m0, r, start, end);
     const int begin = in ? rev ? a.tiles * LA_T - end : start : first * LA_T;
-    if (begin < first * LA_T) {
-      if (a.mode == LA_WALK) {
-        // sequences are short: their rows up to here once more.  c's and b's tiles lie where the walk's will
-        if (PIECES && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + r), hk, wave);
+    if (begin >= first * LA_T) {
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
+    } else if (a.mode == LA_SUMS) {
+      const float m1 = la_powm1(ld, a.per * LA_T);
 #pragma unroll 1
-        for (int tile = begin / LA_T; tile < first; ++tile) {
-          const int c0 = max(begin - tile * LA_T, 0), n = LA_T - c0 - (PIECES && J.S0 && rev && tile == begin / LA_T ? 1 : 0);
-          la_fade(s, fade[n]);
+      for (int k = begin / (a.per * LA_T); k < at.blk; ++k) {
+        la_fade(s, m1);
+        la_add_sum<T, D>(s, sum + (int64_t)k * (D * D), J.turned, wave);
+      }
+    } else if (a.mode == LA_WALK) {
+      // sequences are short: their rows up to here once more.  c's and b's tiles lie where the walk's will
+      if (PIECES && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + r), hk, wave);
 #pragma unroll 1
-          for (int h = 0; h < G; ++h) {
+      for (int tile = begin / LA_T; tile < first; ++tile) {
+        const int c0 = max(begin - tile * LA_T, 0), n = LA_T - c0 - (PIECES && J.S0 && rev && tile == begin / LA_T ? 1 : 0);
+        la_fade(s, fade[n]);
+#pragma unroll 1
+        for (int h = 0; h < G; ++h) {
+          __syncthreads();
+          if (t < LA_T) steps[0].wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
+          fetch_bc(tile, h);
+          la_land<VEC>();
+          if (c0 > 0) {
+            la_clear<T, D>(lb, c0);
             __syncthreads();
-            if (t < LA_T) steps[0].wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
-            fetch_bc(tile, h);
-            la_land<VEC>();
-            if (c0 > 0) {
-              la_clear<T, D>(lb, c0);
-              __syncthreads();
-            }
-            la_update<T, D, false, PIECES>(s, lb, lc, steps[0].wt, 0, LA_T, wave);
           }
-        }
-        __syncthreads();
-      } else {
-        const float m1 = la_powm1(ld, a.per * LA_T);
-        float* sum = a.sums + (((int64_t)J.sum * a.B + at.b) * a.Hkv + hk) * a.blocks * (D * D);
-#pragma unroll 1
-        for (int k = a.mode == LA_SCANNED ? at.blk - 1 : begin / (a.per * LA_T); k < at.blk; ++k) {
-          la_fade(s, m1);
-          la_add_sum<T, D>(s, sum + (int64_t)k * (D * D), J.turned, wave);
+          la_update<T, D, false, PIECES>(s, lb, lc, steps[0].wt, 0, LA_T, wave);
         }
       }
+      __syncthreads();
     }
   }
   if (a.mode == LA_WALK) fetch_bc(first, 0);
@@ -204,8 +210,10 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
         if (there) {
 #pragma unroll
           for (int u = 0; u < 6; u += WAVES) {                   // (A B^T) . D: 16 rows t by 32 rows s
-            const int unit = u + wv.cs, ti = unit < 4 ? unit : unit - 2, si = unit < 4 ? 0 : 1;
-            if (unit >= 6) break;
+            if (u + wv.cs >= 6) break;
+            // blocks 0 and 4 are half the others' work (their rows see the first sixteen of s only): four wavefronts take 0 and 5, 1 and 4, 2, 3
+            const int unit = WAVES == 4 && u > 0 ? 5 - wv.cs : u + wv.cs, ti = unit < 4 ? unit : unit - 2, si = unit < 4 ? 0 : 1;
+            const bool half = unit == 0 || unit == 4;
             la_f4 y[2] = {la_f4{0.f, 0.f, 0.f, 0.f}, la_f4{0.f, 0.f, 0.f, 0.f}};
             const unsigned char *xr = ta + 16 * ti * ROW, *br = tb + 32 * si * ROW;
 #pragma unroll
@@ -216,6 +224,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
               for (int k = 0; k < 2; ++k) b[k].u = *reinterpret_cast<const uint4*>(br + (ar ^ (uint32_t)(i << 6)) + 16 * k * ROW);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
+                if (k == 1 && half) break;
                 if constexpr (BF) {
                   y[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[k].v, q.v, y[k], 0, 0, 0);
                 } else {
@@ -427,9 +436,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 }
 
 template <typename T, int D> int launch(const LaArgs& a, const LaForm& f, hipStream_t st) {
-  int64_t n = 0;
-  for (int j = 0; j < a.jobs; ++j) n += (int64_t)a.blocks * a.B * a.job[j].heads;
-  const dim3 grid((unsigned)n), block(LaWave<D>::NT);
+  const dim3 grid((unsigned)LaPlace::count(a, false)), block(LaWave<D>::NT);
   if (f.vec && f.pieces) hipLaunchKernelGGL((la_main_kernel<T, D, true, true>), grid, block, 0, st, a);
   else if (f.vec) hipLaunchKernelGGL((la_main_kernel<T, D, true, false>), grid, block, 0, st, a);
   else if (f.pieces) hipLaunchKernelGGL((la_main_kernel<T, D, false, true>), grid, block, 0, st, a);

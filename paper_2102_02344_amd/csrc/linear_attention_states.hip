@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, int entries) {
 }
 
 template <typename T, int D> int launch(const LaArgs& a, const LaForm& f, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.blocks * a.B * a.Hkv * a.nsums)), block(LaWave<D>::NT);
+  const dim3 grid((unsigned)LaPlace::count(a, true)), block(LaWave<D>::NT);
   if (f.vec && f.pieces) hipLaunchKernelGGL((la_block_kernel<T, D, true, true>), grid, block, 0, st, a);
   else if (f.vec) hipLaunchKernelGGL((la_block_kernel<T, D, true, false>), grid, block, 0, st, a);
   else if (f.pieces) hipLaunchKernelGGL((la_block_kernel<T, D, false, true>), grid, block, 0, st, a);
