@@ -224,11 +224,11 @@ __device__ __forceinline__ uint32_t la_word(float& x0, float& x1) {
   return u;
 }
 
-// s += a block's sum, or its transpose
-template <typename T, int D> __device__ __forceinline__ void la_add_sum(la_f4 (&s)[D / 16], float* sum, bool turned, const LaWave<D>& wv) {
+// s = a block's sum, or its transpose
+template <typename T, int D> __device__ __forceinline__ void la_load_sum(la_f4 (&s)[D / 16], float* sum, bool turned, const LaWave<D>& wv) {
   if (!turned) {
 #pragma unroll
-    for (int kt = 0; kt < D / 16; ++kt) s[kt] += *la_sum<D>(sum, wv.cs, kt, wv.lane);
+    for (int kt = 0; kt < D / 16; ++kt) s[kt] = *la_sum<D>(sum, wv.cs, kt, wv.lane);
   } else {                                                       // entry (row, column) is (column, row) of what lies there
     const int c = 16 * wv.cs + wv.l;                             // the row there, and where it lies
     const int k = sizeof(T) == 2 ? 2 * (c >> 5) + (c >> 2 & 1) : c >> 4, g = sizeof(T) == 2 ? c >> 3 & 3 : c >> 2 & 3;
@@ -238,7 +238,7 @@ template <typename T, int D> __device__ __forceinline__ void la_add_sum(la_f4 (&
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = la_row<T>(kt, i, wv.g);
-        s[kt][i] += p[((r >> 4) * (D / 16) * 64 + (r & 15)) * 4];
+        s[kt][i] = p[((r >> 4) * (D / 16) * 64 + (r & 15)) * 4];
       }
   }
 }
@@ -334,13 +334,15 @@ __device__ __forceinline__ void la_load_state(la_f4 (&s)[D / 16], const LaJob& J
   asm volatile("" : "+v"(col));
   const int rs = J.flip ? 1 : a.d, cs = J.flip ? a.d : 1;
   const float f = 1.f / J.fi;
+  const float* pc = p + min(col, a.d - 1) * cs;                  // (loads that are all made: a branch around each would wait for each)
 #pragma unroll
   for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = la_row<T>(kt, i, wv.g);
-      s[kt][i] = row < a.d && col < a.d ? f * p[row * rs + col * cs] : 0.f;
-    }
+    for (int i = 0; i < 4; ++i) s[kt][i] = pc[min(la_row<T>(kt, i, wv.g), a.d - 1) * rs];
+#pragma unroll
+  for (int kt = 0; kt < D / 16; ++kt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[kt][i] = la_row<T>(kt, i, wv.g) < a.d && col < a.d ? f * s[kt][i] : 0.f;
 }
 template <typename T, int D> __device__ __forceinline__ void la_store_state(const la_f4 (&s)[D / 16], float* p, int d, float f, const LaWave<D>& wv) {
   int col = 16 * wv.cs + wv.l;

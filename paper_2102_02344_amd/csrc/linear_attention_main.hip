@@ -86,7 +86,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
   float* const sum = a.sums + (((int64_t)J.sum * a.B + at.b) * a.Hkv + hk) * a.blocks * (D * D);
   const bool scanned = a.mode == LA_SCANNED && first > 0;
-  if (scanned) la_add_sum<T, D>(s, sum + (int64_t)(at.blk - 1) * (D * D), J.turned, wave);        // (before it is known whether a sequence goes on here)
+  if (scanned) la_load_sum<T, D>(s, sum + (int64_t)(at.blk - 1) * (D * D), J.turned, wave);        // (before it is known whether a sequence goes on here)
   const float ld = la_decay(raw);
   if (t <= LA_T) {
     pw[t] = la_pow(ld, t);
@@ -128,8 +128,11 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
       const float m1 = la_powm1(ld, a.per * LA_T);
 #pragma unroll 1
       for (int k = begin / (a.per * LA_T); k < at.blk; ++k) {
+        la_f4 v[D / 16];
+        la_load_sum<T, D>(v, sum + (int64_t)k * (D * D), J.turned, wave);
         la_fade(s, m1);
-        la_add_sum<T, D>(s, sum + (int64_t)k * (D * D), J.turned, wave);
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) s[n] += v[n];
       }
     } else if (a.mode == LA_WALK) {
       // sequences are short: their rows up to here once more.  c's and b's tiles lie where the walk's will
@@ -179,15 +182,18 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
       const uint64_t rest = PIECES && p1 < LA_T ? there >> p1 << p1 : 0;
       // rows of the state's update, and whether it comes late: against the order, what comes in behind the last row has not faded there
       const int c0 = val == LA_NONE ? LA_T : PIECES ? p0 : max(val, 0), late = begins && J.S0 && rev ? 1 : 0;
+      const bool ends = keeps && (finals >> (p1 - 1) & 1);
+      int seq = 0;
       if constexpr (PIECES) {
+        if ((begins && J.S0) || ends) seq = la_sequence(off, a.nseq, m0 + (rev ? LA_T - 1 - p0 : p0));
         if (begins) {
 #pragma unroll
           for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
-          if (J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + (rev ? LA_T - 1 - p0 : p0)), hk, wv);
+          if (J.S0) la_load_state<T, D>(s, J, a, at.b, seq, hk, wave.again());
         }
       }
       const bool brings = PIECES ? !begins || J.S0 : __builtin_amdgcn_readlane(mine, 0) == -1;
-      const bool ends = keeps && (finals >> (p1 - 1) & 1), updates = c0 < LA_T && (PIECES ? ends || (p1 == LA_T && tile < last) : tile < last);
+      const bool updates = c0 < LA_T && (PIECES ? ends || (p1 == LA_T && tile < last) : tile < last);
       la_f4 acc[4];                                              // rows t = 16 n + l, columns 16 cs + 4 g + i
 #pragma unroll
       for (int n = 0; n < 4; ++n) acc[n] = la_f4{0.f, 0.f, 0.f, 0.f};
@@ -200,14 +206,16 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
           S.wt[t] = t >= c0 && t < p1 ? pw[p1 - 1 - t] : 0.f;
           S.fac[t] = PIECES ? (t >= p0 && t < p1 ? pw[t - p0 + 1 - late] : 0.f) : mine == -1 ? pw[t + 1] : 0.f;
         }
-        la_land<VEC>();
+        const bool same = PIECES && G == 1 && (there & ((1ull << p0) - 1));       // the tiles, and the products of A and B, of the last step
+        if (same) __syncthreads();
+        else la_land<VEC>();
         const bool more_h = h + 1 < G, again = rest && G > 1, more_t = !rest && tile < last;       // the next step's tiles
         if (!more_h && more_t) fetch_a(tile + 1, x ^ 1);
         const unsigned char* ta = tiles + x * Stage::BYTES;
         // a lane's piece of row l of a tile is 16 g bytes on; addresses are formed where they are needed, or they would fill the registers
         wv = wave.again();
         const uint32_t ar = (uint32_t)Tile::at(wv.l, 16 * wv.g);
-        if (there) {
+        if (there && !same) {
 #pragma unroll
           for (int u = 0; u < 6; u += WAVES) {                   // (A B^T) . D: 16 rows t by 32 rows s
             if (u + wv.cs >= 6) break;
@@ -404,9 +412,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
         if (more_h || again) fetch_bc(tile, more_h ? h + 1 : 0);
         else if (more_t) fetch_bc(tile + 1, 0);
       }
-      if (ends)
-        la_store_state<T, D>(s, J.S1 + la_state_at<T, D>(a, at.b, la_sequence(off, a.nseq, m0 + (rev ? LA_T - p1 : p1 - 1)), hk), a.d,
-                             J.fi * (rev ? pw[1] : 1.f), wv);
+      if (ends) la_store_state<T, D>(s, J.S1 + la_state_at<T, D>(a, at.b, seq, hk), a.d, J.fi * (rev ? pw[1] : 1.f), wave.again());
       if (!PIECES) break;
       p0 = rest ? __builtin_ctzll(rest) : LA_T;
     }
