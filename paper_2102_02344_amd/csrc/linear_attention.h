@@ -69,6 +69,18 @@ __device__ __forceinline__ float la_pow(float g, int n) {
 }
 __device__ __forceinline__ float la_powm1(float g, int n) { return n == 0 ? 0.f : expm1f((float)n * g); }
 
+// A staged tile: rows of D columns without padding, as the loads into LDS leave them; piece p (16 bytes) of row r lies at place p ^ key(r).  Sixteen
+// rows' reads of one piece cover all 64 banks, and so do a transpose read's eight rows of two pieces and (fp32) four rows of four.
+template <typename T, int D> struct LaTile {
+  static constexpr int ROW = D * (int)sizeof(T), PPR = ROW / 16;
+  static __device__ __forceinline__ constexpr int key(int r) {
+    if (sizeof(T) == 2)
+      return PPR == 16 ? (r & 3) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1) : PPR == 8 ? (r >> 1 & 3) << 1 | (r >> 3 & 1) : (r >> 2 & 1) << 1 | (r >> 3 & 1);
+    return PPR >= 16 ? (r >> 2 & 3) << 2 | (r & 3) : (r >> 2 & 1) << 2 | (r >> 3 & 1) << 1 | (r >> 1 & 1);
+  }
+  static __device__ __forceinline__ int at(int r, int byte) { return r * ROW + (((byte >> 4) ^ key(r)) << 4) + (byte & 15); }
+};
+
 typedef float la_f4 __attribute__((ext_vector_type(4)));
 // A wavefront's role: it has columns 16 cs + l%16 of c; a lane's quarter g = l / 16
 template <int D> struct LaWave {
@@ -95,7 +107,7 @@ template <int D> struct LaWave {
 // go through a buffer that ends with the last row, straight into LDS; a thread's pieces lie a multiple of 16 rows apart, with which the swizzle
 // repeats, so that one offset serves them all.
 template <typename T, int D, bool VEC> struct LaStage {
-  typedef PkTile<T, D> Tile;
+  typedef LaTile<T, D> Tile;
   static constexpr int NT = LaWave<D>::NT, BYTES = LA_T * Tile::ROW, PIECES = BYTES / 16, N = PIECES / NT, EPP = 16 / (int)sizeof(T), RPN = NT / Tile::PPR;
   static_assert(PIECES % NT == 0 && RPN % 16 == 0, "whole pieces for every thread, the same swizzle for all of a thread's");
   uint32_t at;                     // of the piece with the lowest offset
@@ -138,8 +150,8 @@ template <typename T, int D> __device__ __forceinline__ void la_clear(la_lds til
   typedef __attribute__((address_space(3))) pk_i4* la_i4;
 #pragma unroll
   for (int k = 0; k < 2; ++k)
-    for (int i = (int)threadIdx.x * 16; i < n * PkTile<T, D>::ROW; i += LaWave<D>::NT * 16)
-      *(la_i4)(tile + k * LA_T * PkTile<T, D>::ROW + i) = pk_i4{0, 0, 0, 0};
+    for (int i = (int)threadIdx.x * 16; i < n * LaTile<T, D>::ROW; i += LaWave<D>::NT * 16)
+      *(la_i4)(tile + k * LA_T * LaTile<T, D>::ROW + i) = pk_i4{0, 0, 0, 0};
 }
 // until the loads into LDS have landed, for all wavefronts
 template <bool VEC> __device__ __forceinline__ void la_land() {
@@ -148,7 +160,7 @@ template <bool VEC> __device__ __forceinline__ void la_land() {
 }
 
 // Where a row's sequence begins, counted in the tile's rows in the order of the walk: -1 before the tile; this: in no sequence
-constexpr int LA_NONE = 1 << 20;
+constexpr int LA_NONE = LA_T;
 
 // The sequences of a tile's rows from a lookup of LA_SPAN rows: a lane's row r of the tile (in memory) lies in [start, end).  Every
 // word of the lookup is in a lane, the last one that begins before the tile and the first one behind it come out of two ballots.
@@ -192,25 +204,22 @@ __device__ __forceinline__ uint32_t la_odd(uint32_t u) { return (u & 0x7f807f80u
 typedef __attribute__((address_space(3))) pk_s4* la_lds4;
 union LaFrag { uint32_t u[4]; pk_s4 h[2]; pk_bf8 v; bf16_raw e[8]; };
 
-// Sixteen columns of a staged bf16 tile over 32 rows as a matrix operand: a lane's slots are rows row0 + 4 g + 0..3 and 16 + 4 g + 0..3; lane l%16
-// holds column col0 + l, or (SPREAD) column col0 + 8 (l / 4) + l%4.  `at`: la_cols_at(), row0: a multiple of 32, col0: of 16 (SPREAD: of 4, in each 32 the
-// first two)
-template <int D, bool SPREAD> __device__ __forceinline__ uint32_t la_cols_at(int lane) {
+// Sixteen columns of a staged bf16 tile over 32 rows as a matrix operand: a lane's slots are rows row0 + 4 g + 0..3 and 16 + 4 g + 0..3; it holds
+// column col0 + l.  `at`: la_cols_at(), row0: a multiple of 32, col0: of 16
+template <int D> __device__ __forceinline__ uint32_t la_cols_at(int lane) {
   const int r = lane & 15;
-  uint32_t a = (uint32_t)PkTile<bf16_raw, D>::at(4 * (lane >> 4) + (r >> 2), (SPREAD ? 8 : 4) * (r & 3) * 2);
+  uint32_t a = (uint32_t)LaTile<bf16_raw, D>::at(4 * (lane >> 4) + (r >> 2), 4 * (r & 3) * 2);
   asm volatile("" : "+v"(a));                                    // (formed where it is needed)
   return a;
 }
 template <int D> __device__ __forceinline__ void la_cols(LaFrag& f, la_lds tile, uint32_t at, int row0, int col0) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)                                    // (sixteen rows on the swizzle repeats)
-    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + (at ^ (uint32_t)(col0 << 1)) + (row0 + 16 * h) * PkTile<bf16_raw, D>::ROW));
+    f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((la_lds4)(tile + (at ^ (uint32_t)(col0 << 1)) + (row0 + 16 * h) * LaTile<bf16_raw, D>::ROW));
 }
 
 // A state in the accumulators of the wavefronts: s[kt][i], column 16 cs + l of c, and of b
-template <typename T> __device__ __forceinline__ int la_row(int kt, int i, int g) {
-  return sizeof(T) == 2 ? 32 * (kt >> 1) + 8 * g + 4 * (kt & 1) + i : 16 * kt + 4 * g + i;
-}
+__device__ __forceinline__ int la_row(int kt, int i, int g) { return 16 * kt + 4 * g + i; }
 // its place in a block's sums
 template <int D> __device__ __forceinline__ la_f4* la_sum(float* sums, int cs, int kt, int lane) {
   return reinterpret_cast<la_f4*>(sums) + (cs * (D / 16) + kt) * 64 + lane;
@@ -231,13 +240,12 @@ template <typename T, int D> __device__ __forceinline__ void la_load_sum(la_f4 (
     for (int kt = 0; kt < D / 16; ++kt) s[kt] = *la_sum<D>(sum, wv.cs, kt, wv.lane);
   } else {                                                       // entry (row, column) is (column, row) of what lies there
     const int c = 16 * wv.cs + wv.l;                             // the row there, and where it lies
-    const int k = sizeof(T) == 2 ? 2 * (c >> 5) + (c >> 2 & 1) : c >> 4, g = sizeof(T) == 2 ? c >> 3 & 3 : c >> 2 & 3;
-    const float* p = sum + (k * 64 + 16 * g) * 4 + (c & 3);
+    const float* p = sum + ((c >> 4) * 64 + 16 * (c >> 2 & 3)) * 4 + (c & 3);
 #pragma unroll
     for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = la_row<T>(kt, i, wv.g);
+        const int r = la_row(kt, i, wv.g);
         s[kt][i] = p[((r >> 4) * (D / 16) * 64 + (r & 15)) * 4];
       }
   }
@@ -256,7 +264,7 @@ __device__ __forceinline__ void la_update(la_f4 (&s)[D / 16], la_lds tb, la_lds 
   int g4 = 4 * g;
   if constexpr (PART) asm volatile("" : "+v"(c0), "+v"(c1), "+v"(g4));      // (masks are formed where they are needed)
   if constexpr (sizeof(T) == 2) {
-    const uint32_t at = la_cols_at<D, false>(lane), spread = la_cols_at<D, true>(lane);
+    const uint32_t at = la_cols_at<D>(lane);
 #pragma unroll
     for (int ks = 0; ks < LA_T / 32; ++ks) {
       const int row0 = 32 * ks;
@@ -280,7 +288,7 @@ __device__ __forceinline__ void la_update(la_f4 (&s)[D / 16], la_lds tb, la_lds 
         LaFrag b[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          la_cols<D>(b[k], tb, spread, row0, 16 * k0 + 4 * k);
+          la_cols<D>(b[k], tb, at, row0, 16 * (k0 + k));
           if constexpr (PART) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) b[k].u[p] &= la_rows(row0 + g4 + 2 * (p & 1) + 16 * (p >> 1), c0, c1);
@@ -298,7 +306,7 @@ __device__ __forceinline__ void la_update(la_f4 (&s)[D / 16], la_lds tb, la_lds 
       }
     }
   } else {
-    typedef PkTile<T, D> Tile;
+    typedef LaTile<T, D> Tile;
     uint32_t at = (uint32_t)Tile::at(4 * g, wv.l * 4);           // row 16 ks + 4 g + i: other bits of the key
     asm volatile("" : "+v"(at));
 #pragma unroll 1
@@ -338,11 +346,11 @@ __device__ __forceinline__ void la_load_state(la_f4 (&s)[D / 16], const LaJob& J
 #pragma unroll
   for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[kt][i] = pc[min(la_row<T>(kt, i, wv.g), a.d - 1) * rs];
+    for (int i = 0; i < 4; ++i) s[kt][i] = pc[min(la_row(kt, i, wv.g), a.d - 1) * rs];
 #pragma unroll
   for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[kt][i] = la_row<T>(kt, i, wv.g) < a.d && col < a.d ? f * s[kt][i] : 0.f;
+    for (int i = 0; i < 4; ++i) s[kt][i] = la_row(kt, i, wv.g) < a.d && col < a.d ? f * s[kt][i] : 0.f;
 }
 template <typename T, int D> __device__ __forceinline__ void la_store_state(const la_f4 (&s)[D / 16], float* p, int d, float f, const LaWave<D>& wv) {
   int col = 16 * wv.cs + wv.l;
@@ -351,7 +359,7 @@ template <typename T, int D> __device__ __forceinline__ void la_store_state(cons
   for (int kt = 0; kt < D / 16; ++kt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = la_row<T>(kt, i, wv.g);
+      const int row = la_row(kt, i, wv.g);
       if (row < d && col < d) p[row * d + col] = f * s[kt][i];
     }
 }

@@ -5,7 +5,7 @@ namespace hfta {
 namespace {
 
 // of the wavefront's columns of c: NaN into the rows that see a value of the tile which is not finite
-template <typename T, int D> __device__ __forceinline__ void la_mark(la_f4 (&acc)[4], const unsigned char* tc, const LaWave<D>& wv, const int* rel) {
+template <typename T, int D> __device__ __forceinline__ void la_mark(la_f4 (&acc)[4], const unsigned char* tc, const LaWave<D>& wv, const signed char* rel) {
   int c0 = 16 * wv.cs + 4 * wv.g;
   asm volatile("" : "+v"(c0));                                   // (nothing of this is worth a register outside)
 #pragma unroll
@@ -16,18 +16,15 @@ template <typename T, int D> __device__ __forceinline__ void la_mark(la_f4 (&acc
       const bool sees = r >= begin && r <= t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = Elem<T>::load(reinterpret_cast<const T*>(tc + PkTile<T, D>::at(r, (c0 + i) * (int)sizeof(T)))), y = sees ? x : 0.f;
+        const float x = Elem<T>::load(reinterpret_cast<const T*>(tc + LaTile<T, D>::at(r, (c0 + i) * (int)sizeof(T)))), y = sees ? x : 0.f;
         acc[n][i] += y - y;                                      // NaN, or nothing
       }
     }
   }
 }
 
-// What a workgroup knows of a step's rows, for two steps in turn
-struct LaStep {
-  int rel[LA_T];                   // where a row's sequence begins
-  float wt[LA_T], fac[LA_T];       // a row's weight in the state's update, the state's weight in a row
-};
+// A row's weight in the state's update, and the state's weight in a row, for two steps in turn
+struct LaStep { float wt[LA_T], fac[LA_T]; };
 
 // The masked products (A B^T) . D of a tile: six blocks of 16 rows t by 32 rows s (the other two are all zeros), 16 bytes a lane as the second product
 // takes them; bf16: values, and behind them what is left; fp32: columns s of 16 each
@@ -42,14 +39,15 @@ struct LaP {
 template <typename T, int D, bool VEC, bool PIECES>
 __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 : D == 128 ? 4 : 3)) void la_main_kernel(LaArgs a) {
   typedef LaStage<T, D, VEC> Stage;
-  typedef PkTile<T, D> Tile;
+  typedef LaTile<T, D> Tile;
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NT = LaWave<D>::NT, WAVES = LaWave<D>::WAVES, ROW = Tile::ROW;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * Stage::BYTES], P[LaP::BYTES];
   __shared__ PackedRows<LA_SPAN> pr;
   __shared__ __attribute__((aligned(16))) LaStep steps[2];
-  __shared__ float dw[2 * LA_T + 1], fade[LA_T + 1];             // lambda^n behind LA_T places of nothing; lambda^n - 1
-  float* const pw = dw + LA_T;
+  __shared__ signed char rels[LA_SPAN / LA_T][LA_T];             // where the rows' sequences begin, of a span's tiles
+  __shared__ uint64_t finals[LA_SPAN / LA_T];                    // rows that are their sequence's last one in the order of the walk
+  __shared__ float pw[LA_T + 1], fade[LA_T + 1], dw[2 * LA_T + 1];      // lambda^n, lambda^n - 1; behind LA_T places of nothing lambda^n fo
   const LaWave<D> wave;
   const int t = threadIdx.x;
   const LaPlace at(a, false);
@@ -91,6 +89,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   if (t <= LA_T) {
     pw[t] = la_pow(ld, t);
     fade[t] = la_powm1(ld, t);
+    dw[LA_T + t] = J.fo * la_pow(ld, t);
   }
   if (t < LA_T) dw[t] = 0.f;
 
@@ -108,12 +107,23 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   }
 
   LaSpan span;
-  auto look = [&](int m0) __attribute__((always_inline)) {                                      // up the sequences of the rows from the tile at m0 on, in the order of the walk
-    const int t0 = rev ? m0 + LA_T - LA_SPAN : m0;
+  auto look = [&](int tile) __attribute__((always_inline)) {     // up the sequences of the rows of this tile and the next ones
+    const int t0 = rev ? row0(tile) + LA_T - LA_SPAN : row0(tile);
     pr.template scan<NT>(off, a.nseq, a.R, t0);
     span.take(pr, t0, wave.lane);
+    for (int k = wave.cs; k < LA_SPAN / LA_T && tile + k <= last; k += WAVES) {
+      const int m0 = row0(tile + k), r = rev ? LA_T - 1 - wave.lane : wave.lane;
+      int start, end;
+      const bool in = span.range(m0, r, start, end) && m0 + r < a.R;
+      rels[k][wave.lane] = (signed char)(!in ? LA_NONE : max(rev ? m0 + LA_T - end : start - m0, -1));
+      if constexpr (PIECES) {
+        const uint64_t f = __ballot(in && m0 + r == (rev ? start : end - 1));
+        if (wave.lane == 0) finals[k] = f;
+      }
+    }
+    __syncthreads();
   };
-  look(row0(first));                                             // (its barriers make pw visible too)
+  look(first);                                                   // (its barriers make the tables visible too)
 
   // what the first row's sequence brings from the blocks before
   if (first > 0) {
@@ -161,14 +171,12 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 
   int step = 0, x = 0;                                           // steps, and the place of this one's tile of A
   for (int tile = first; tile <= last; ++tile, x ^= 1) {
-    const int m0 = row0(tile);
-    if (tile > first && (tile - first) % (LA_SPAN / LA_T) == 0) look(m0);       // (behind a barrier, at the end of the last tile)
+    const int m0 = row0(tile), in_span = (tile - first) % (LA_SPAN / LA_T);
+    if (tile > first && in_span == 0) look(tile);                // (behind a barrier, at the end of the last tile)
+    const signed char* rel = rels[in_span];
     LaWave<D> wv = wave.again();
-    int start, end;
-    const int r = rev ? LA_T - 1 - wv.lane : wv.lane;            // (every wavefront for itself: a lane has a row)
-    const bool in = span.range(m0, r, start, end) && m0 + r < a.R;
-    const int mine = !in ? LA_NONE : max(rev ? m0 + LA_T - end : start - m0, -1);
-    const uint64_t there = __ballot(in), finals = PIECES ? __ballot(in && m0 + r == (rev ? start : end - 1)) : 0;
+    const int mine = rel[wv.lane];
+    const uint64_t there = __ballot(mine != LA_NONE);
     const bool mixed = __any(mine > 0);                          // rows of several sequences, or of none
     // sequence by sequence, or all rows at once (also of a tile that has none: its successor's tiles are fetched)
     for (int p0 = PIECES && there ? __builtin_ctzll(there) : 0, p1; p0 < LA_T;) {
@@ -182,7 +190,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
       const uint64_t rest = PIECES && p1 < LA_T ? there >> p1 << p1 : 0;
       // rows of the state's update, and whether it comes late: against the order, what comes in behind the last row has not faded there
       const int c0 = val == LA_NONE ? LA_T : PIECES ? p0 : max(val, 0), late = begins && J.S0 && rev ? 1 : 0;
-      const bool ends = keeps && (finals >> (p1 - 1) & 1);
+      const bool ends = keeps && (finals[in_span] >> (p1 - 1) & 1);
       int seq = 0;
       if constexpr (PIECES) {
         if ((begins && J.S0) || ends) seq = la_sequence(off, a.nseq, m0 + (rev ? LA_T - 1 - p0 : p0));
@@ -202,9 +210,8 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
         wv = wave.again();
         if (wv.cs == 0) {
           const int t = wv.lane;
-          S.rel[t] = mine;
           S.wt[t] = t >= c0 && t < p1 ? pw[p1 - 1 - t] : 0.f;
-          S.fac[t] = PIECES ? (t >= p0 && t < p1 ? pw[t - p0 + 1 - late] : 0.f) : mine == -1 ? pw[t + 1] : 0.f;
+          S.fac[t] = PIECES ? (t >= p0 && t < p1 ? dw[LA_T + t - p0 + 1 - late] : 0.f) : mine == -1 ? dw[LA_T + t + 1] : 0.f;
         }
         const bool same = PIECES && G == 1 && (there & ((1ull << p0) - 1));       // the tiles, and the products of A and B, of the last step
         if (same) __syncthreads();
@@ -244,11 +251,11 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
             const LaWave<D> wu = wave.again();
             const int self = 16 * ti + wu.l - 32 * si - 4 * wu.g;       // s counts from 32 si + 4 g: 16 k + i
             if (mixed) {
-              const int rel = S.rel[16 * ti + wu.l] - 32 * si - 4 * wu.g;
+              const int from = rel[16 * ti + wu.l] - 32 * si - 4 * wu.g;
 #pragma unroll
               for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[k][i] = 16 * k + i >= rel ? y[k][i] : 0.f;
+                for (int i = 0; i < 4; ++i) y[k][i] = 16 * k + i >= from ? y[k][i] : 0.f;
             }
             const float* decay = dw + (LA_T - 19 + self);
 #pragma unroll
@@ -273,11 +280,19 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
           }
         }
         if (brings && h == 0) {                                  // Lambda A S
+          const uint32_t as = (uint32_t)Tile::at(wv.l, 8 * wv.g);
 #pragma unroll
           for (int j = 0; j < ROW / 64; ++j) {
-            union { uint4 u; pk_bf8 v; float e[4]; } q[4];
+            union { uint4 u; uint2 h[2]; pk_bf8 v; float e[4]; } q[4];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) q[n].u = *reinterpret_cast<const uint4*>(ta + (ar ^ (uint32_t)(j << 6)) + 16 * n * ROW);
+            for (int n = 0; n < 4; ++n) {
+              if constexpr (BF) {                                // columns 32 j + 4 g + 0..3 and 16 on, as the state's rows lie
+#pragma unroll
+                for (int k = 0; k < 2; ++k) q[n].h[k] = *reinterpret_cast<const uint2*>(ta + (as ^ (uint32_t)(j << 6 | k << 5)) + 16 * n * ROW);
+              } else {
+                q[n].u = *reinterpret_cast<const uint4*>(ta + (ar ^ (uint32_t)(j << 6)) + 16 * n * ROW);
+              }
+            }
             if constexpr (BF) {
               LaFrag hi, lo;
 #pragma unroll
@@ -301,10 +316,12 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
             const int row = 16 * n + wv.l;
-            const float f = S.fac[row];
-            const bool sees = PIECES ? row >= p0 && row < p1 : S.rel[row] == -1;
+            acc[n] *= S.fac[row];
+            if (PIECES || mixed) {
+              const bool sees = PIECES ? row >= p0 && row < p1 : rel[row] == -1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[n][i] = sees ? f * acc[n][i] : 0.f;
+              for (int i = 0; i < 4; ++i) acc[n][i] = sees ? acc[n][i] : 0.f;
+            }
           }
         }
         __syncthreads();
@@ -314,7 +331,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
           if constexpr (BF) {
             LaFrag c[2];
             uint32_t odd = 0;
-            const uint32_t at_c = la_cols_at<D, false>(wv.lane);
+            const uint32_t at_c = la_cols_at<D>(wv.lane);
 #pragma unroll
             for (int k = 0; k < 2; ++k) la_cols<D>(c[k], lc, at_c, 32 * k, 16 * wv.cs);
 #pragma unroll
@@ -345,7 +362,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 #pragma unroll
               for (int i = 0; i < 2; ++i) acc[n0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[k].v, lo[i], acc[n0 + i], 0, 0, 0);
             }
-            if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, S.rel);
+            if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, rel);
           } else {
             // a column's values of the four quarters' rows 16 q + 4 g + e
             const uint32_t ac = (uint32_t)Tile::at(4 * wv.g, (16 * wv.cs + wv.l) * 4);
@@ -371,7 +388,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(c[4 * q + e], w[e], acc[n], 0, 0, 0);
               }
-            if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, S.rel);
+            if (__builtin_expect(marks, 0)) la_mark<T, D>(acc, tc, wv, rel);
           }
           if (h == G - 1) {                                      // the result's rows in place of A's
             wv = wave.again();
@@ -381,7 +398,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
               const int row = 16 * n + wv.l;
               if (PIECES && (row < p0 || row >= p1)) continue;
               unsigned char* p = tiles + x * Stage::BYTES + ao + 16 * n * ROW;
-              const la_f4 o = J.fo * acc[n];
+              const la_f4 o = acc[n];
               if constexpr (BF) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
               else *reinterpret_cast<la_f4*>(p) = o;
             }
@@ -419,7 +436,6 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
     // the tile's results, as its rows of A came in
     if (there) {
       const unsigned char* from = tiles + x * Stage::BYTES;
-      const int* rel = steps[(step + 1) & 1].rel;
       wv = wave.again();
 #pragma unroll
       for (int n = 0; n < Stage::N; ++n) {
