@@ -24,9 +24,8 @@ struct GnArgs {
   float *m1, *i1, *m2, *i2, *part;
   float eps;
   int R, E, blocks;                // blocks: workgroups of a model
-  int need_db;
 };
-constexpr int GN_MAX_BLOCKS = 512;
+constexpr int GN_MAX_BLOCKS = 1024;
 
 template <int TPR> struct GnSum {
   float lds[2][2][TPR > 64 ? TPR / 64 : 1];
@@ -146,51 +145,84 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_fwd_kernel(GnArgs 
   Row::store(reinterpret_cast<T*>(a.Y) + at, x, E);
 }
 
-// Partial sums of a workgroup's rows, in part[model][workgroup][5][E] (dw2, db2, dw1, db1, and dres in the first word of the last)
-template <typename T, int NP, int TPR, bool RMS, bool BLOCK>
-__global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs a) {
+// Partial sums of a workgroup's rows, in part[model][workgroup][4 E + 4] (dw2, db2, dw1, db1, and dres in the next word).  The next row is on its way
+// while one is computed,.  BIAS: sums of the gradients themselves are wanted
+template <typename T, int NP, int TPR, bool RMS, bool BLOCK, bool BIAS>
+__global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS || sizeof(T) == 4 || TPR == 512 ? 2 : 3)) void gn_bwd_kernel(GnArgs a) {
   typedef GnRow<T, NP, TPR> Row;
-  constexpr int N = Piece16<T>::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  typedef Piece16<T> P;
+  constexpr int N = P::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  constexpr bool AHEAD = TPR < 1024;
   __shared__ GnSum<TPR> sum;
   const int b = blockIdx.y, E = a.E;
   const float res = BLOCK && a.res ? a.res[b] : 1.f;
   const float *w1 = a.w1 + (int64_t)b * E, *b1 = a.b1 ? a.b1 + (int64_t)b * E : nullptr, *w2 = a.w2 + (int64_t)b * E;
   float dw1[NP][N], db1[NP][N], dw2[NP][N], db2[NP][N], dres = 0.f;
   GN_EACH(NP, N) dw1[p][e] = db1[p][e] = dw2[p][e] = db2[p][e] = 0.f;
-  const int part = blockIdx.x * RPB + threadIdx.x / TPR, parts = a.blocks * RPB;
-  int turn = 0;
-  for (int r = part; r < a.R; r += parts) {
-    const int64_t row = (int64_t)b * a.R + r, at = row * E;
-    float x[NP][N], f[NP][N], g[NP][N], dy[NP][N], ds[NP][N], w[NP][N], u[NP][N];
-    Row::load(x, reinterpret_cast<const T*>(a.X) + at, E);
+  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x * RPB + threadIdx.x / TPR), parts = a.blocks * RPB;
+  float w[NP][N], c[NP][N], v[NP][N];
+  auto weights = [&]() __attribute__((always_inline)) {
     if constexpr (BLOCK) {
-      Row::load(f, reinterpret_cast<const T*>(a.F) + at, E);
-      if (a.G) Row::load(g, reinterpret_cast<const T*>(a.G) + at, E);
-    }
-    Row::load(dy, reinterpret_cast<const T*>(a.dY) + at, E);
-    if (a.dS) Row::load(ds, reinterpret_cast<const T*>(a.dS) + at, E);
-    const float i2 = a.i2[row], m2 = RMS ? 0.f : a.m2[row];
-    float i1 = 0.f;
-    if constexpr (BLOCK) {
-      i1 = a.i1[row];
-      const float m1 = RMS ? 0.f : a.m1[row];
-      float c[NP][N];
       Row::weights(w, w1, E, 0.f);
       Row::weights(c, b1, E, 0.f);
+    }
+    Row::weights(v, w2, E, 0.f);
+  };
+  struct Raw { piece_u4 x[NP], f[NP], g[NP], dy[NP], ds[NP]; } in;
+  float m1 = 0.f, i1 = 0.f, m2 = 0.f, i2;
+  auto load = [&](int r) __attribute__((always_inline)) {
+    const int64_t row = (int64_t)b * a.R + r, at = row * E;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int col = Row::col(p), n = E - col;
+      const int64_t to = at + col;
+      in.x[p] = P::raw(reinterpret_cast<const T*>(a.X) + to, n);
+      if constexpr (BLOCK) {
+        in.f[p] = P::raw(reinterpret_cast<const T*>(a.F) + to, n);
+        if (a.G) in.g[p] = P::raw(reinterpret_cast<const T*>(a.G) + to, n);
+      }
+      in.dy[p] = P::raw(reinterpret_cast<const T*>(a.dY) + to, n);
+      if (a.dS) in.ds[p] = P::raw(reinterpret_cast<const T*>(a.dS) + to, n);
+    }
+    i2 = a.i2[row];
+    if (!RMS) m2 = a.m2[row];
+    if constexpr (BLOCK) {
+      i1 = a.i1[row];
+      if (!RMS) m1 = a.m1[row];
+    }
+  };
+  int turn = 0;
+  if (AHEAD && part < a.R) load(part);
+  for (int r = part; r < a.R; r += parts) {
+    const int64_t at = ((int64_t)b * a.R + r) * E;
+    if (!AHEAD) load(r);
+    float x[NP][N], f[NP][N], g[NP][N], dy[NP][N], ds[NP][N], u[NP][N];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      P::values(x[p], in.x[p]);
+      if constexpr (BLOCK) {
+        P::values(f[p], in.f[p]);
+        if (a.G) P::values(g[p], in.g[p]);
+      }
+      P::values(dy[p], in.dy[p]);
+      if (a.dS) P::values(ds[p], in.ds[p]);
+    }
+    const float mean1 = m1, inv1 = i1, mean2 = m2, inv2 = i2;
+    if (AHEAD && r + parts < a.R) load(r + parts);
+    weights();
+    if constexpr (BLOCK) {
       GN_EACH(NP, N) {
-        f[p][e] = Row::col(p) + e < E ? (f[p][e] - m1) * i1 : 0.f;
+        f[p][e] = RMS ? f[p][e] * inv1 : Row::col(p) + e < E ? (f[p][e] - mean1) * inv1 : 0.f;
         u[p][e] = fmaf(f[p][e], w[p][e], c[p][e]);
         g[p][e] = a.G ? gn_sigma(g[p][e]) : 1.f;
         x[p][e] = fmaf(res * g[p][e], u[p][e], x[p][e]);
       }
     }
     float s = 0.f, z = 0.f;
-    float v[NP][N];
-    Row::weights(v, w2, E, 0.f);
     GN_EACH(NP, N) {
-      x[p][e] = Row::col(p) + e < E ? (x[p][e] - m2) * i2 : 0.f;
+      x[p][e] = RMS ? x[p][e] * inv2 : Row::col(p) + e < E ? (x[p][e] - mean2) * inv2 : 0.f;
       dw2[p][e] = fmaf(dy[p][e], x[p][e], dw2[p][e]);
-      if (a.need_db) db2[p][e] += dy[p][e];
+      if (BIAS) db2[p][e] += dy[p][e];
       dy[p][e] *= v[p][e];
       s = fmaf(dy[p][e], x[p][e], s);
       if (!RMS) z += dy[p][e];
@@ -199,15 +231,15 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs 
     turn ^= 1;
     s /= (float)E;
     z /= (float)E;
-    GN_EACH(NP, N) ds[p][e] = i2 * (dy[p][e] - z - x[p][e] * s) + (a.dS ? ds[p][e] : 0.f);
+    GN_EACH(NP, N) ds[p][e] = inv2 * (dy[p][e] - z - x[p][e] * s) + (a.dS ? ds[p][e] : 0.f);
     Row::store(reinterpret_cast<T*>(a.dX) + at, ds, E);
     if constexpr (BLOCK) {
       s = z = 0.f;
       GN_EACH(NP, N) {
-        const float hd = Row::col(p) + e < E ? g[p][e] * ds[p][e] : 0.f, du = res * hd;      // (z makes ds not zero behind the row)
+        const float hd = RMS || Row::col(p) + e < E ? g[p][e] * ds[p][e] : 0.f, du = res * hd;       // (z makes ds not zero behind the row)
         dres = fmaf(hd, u[p][e], dres);
         dw1[p][e] = fmaf(du, f[p][e], dw1[p][e]);
-        if (a.need_db) db1[p][e] += du;
+        if (BIAS) db1[p][e] += du;
         if (a.G) g[p][e] = du * u[p][e] * (1.f - g[p][e]);       // dG
         dy[p][e] = du * w[p][e];
         s = fmaf(dy[p][e], f[p][e], s);
@@ -218,23 +250,25 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs 
       turn ^= 1;
       s /= (float)E;
       z /= (float)E;
-      GN_EACH(NP, N) dy[p][e] = i1 * (dy[p][e] - z - f[p][e] * s);
+      GN_EACH(NP, N) dy[p][e] = inv1 * (dy[p][e] - z - f[p][e] * s);
       Row::store(reinterpret_cast<T*>(a.dF) + at, dy, E);
     }
   }
   float* out = a.part + ((int64_t)b * parts + part) * (4 * (int64_t)E + 4);
-  GN_EACH(NP, N) {
-    const int c = Row::col(p) + e;
-    if (c < E) {
-      out[c] = dw2[p][e];
-      if (a.need_db) out[E + c] = db2[p][e];
-      if constexpr (BLOCK) {
-        out[2 * (int64_t)E + c] = dw1[p][e];
-        if (a.need_db) out[3 * (int64_t)E + c] = db1[p][e];
+  auto put = [&](float* to, const float (&y)[NP][N]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) {
+        const float w4[4] = {y[p][4 * q], y[p][4 * q + 1], y[p][4 * q + 2], y[p][4 * q + 3]};
+        Piece16<float>::store(to + Row::col(p) + 4 * q, w4, E - Row::col(p) - 4 * q);
       }
-    }
-  }
+  };
+  put(out, dw2);
+  if (BIAS) put(out + E, db2);
   if constexpr (BLOCK) {
+    put(out + 2 * (int64_t)E, dw1);
+    if (BIAS) put(out + 3 * (int64_t)E, db1);
     if constexpr (TPR > 64) {
       float none = 0.f;
       gn_sum<TPR>(sum, turn, dres, none);
@@ -245,10 +279,10 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_bwd_kernel(GnArgs 
   }
 }
 
-// The parts of a model added in order: a workgroup takes 64 columns, each of its wavefronts a sixteenth of the parts, eight in flight
+// The parts of a model added in order: a workgroup takes 64 columns, each of its wavefronts a sixteenth of the parts, sixteen in flight
 constexpr int GN_ADD = 1024;
 __global__ __launch_bounds__(GN_ADD) void gn_add_kernel(const float* part, int parts, int E, float* dw2, float* db2, float* dw1, float* db1, float* dres) {
-  constexpr int W = GN_ADD / 64, AHEAD = 8;
+  constexpr int W = GN_ADD / 64, AHEAD = 16;
   __shared__ double lds[W][64];
   const int b = blockIdx.y, q = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t width = 4 * (int64_t)E + 4, c = (int64_t)blockIdx.x * 64 + lane;
@@ -278,9 +312,11 @@ __global__ __launch_bounds__(GN_ADD) void gn_add_kernel(const float* part, int p
 
 constexpr int GN_MAX_E = 16384;
 int gn_rows(int E) { return E <= 512 ? 4 : 1; }                  // rows of a workgroup
-int gn_blocks(int B, int R, int E) {
+// workgroups of a model in the backward call: as many as are resident at once, `per` on each of the 256 compute units
+int gn_blocks(int B, int R, int E, int per) {
   const int rows = (R + gn_rows(E) - 1) / gn_rows(E);
-  int most = 1024 / B;
+  int most = 256 * (E <= 512 ? per : E <= 1024 ? 2 * per : E <= 2048 ? per : 1);
+  most /= B;
   if (most < 32) most = 32;
   if (most > GN_MAX_BLOCKS) most = GN_MAX_BLOCKS;
   return rows < most ? rows : most;
@@ -291,25 +327,29 @@ int gn_check(int B, int R, int E, int dtype, int norm) {
   return E > GN_MAX_E || B > 65535 || R > 0x7fffffff - 4096 || (R + gn_rows(E) - 1) / gn_rows(E) > 0x3fffff ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 
-// elements of a thread and threads of a row
-#define GN_LAUNCH(kernel, EL, TPR) \
-  hipLaunchKernelGGL((kernel<T, EL / Piece16<T>::N, TPR, RMS, BLOCK>), grid, dim3(TPR == 64 ? 256 : TPR), 0, st, a)
-#define GN_FORMS(kernel)                                 \
-  if (a.E <= 512) GN_LAUNCH(kernel, 8, 64);              \
-  else if (a.E <= 1024) GN_LAUNCH(kernel, 8, 128);       \
-  else if (a.E <= 2048) GN_LAUNCH(kernel, 8, 256);       \
-  else if (a.E <= 4096) GN_LAUNCH(kernel, 8, 512);       \
-  else if (a.E <= 8192) GN_LAUNCH(kernel, 8, 1024);      \
-  else GN_LAUNCH(kernel, 16, 1024);                      \
+// pieces of a thread and threads of a row; the other template arguments
+#define GN_LAUNCH(kernel, EL, TPR, ...) \
+  hipLaunchKernelGGL((kernel<T, EL / Piece16<T>::N, TPR, __VA_ARGS__>), grid, dim3(TPR == 64 ? 256 : TPR), 0, st, a)
+#define GN_FORMS(kernel, ...)                                       \
+  if (a.E <= 512) GN_LAUNCH(kernel, 8, 64, __VA_ARGS__);            \
+  else if (a.E <= 1024) GN_LAUNCH(kernel, 8, 128, __VA_ARGS__);     \
+  else if (a.E <= 2048) GN_LAUNCH(kernel, 8, 256, __VA_ARGS__);     \
+  else if (a.E <= 4096) GN_LAUNCH(kernel, 8, 512, __VA_ARGS__);     \
+  else if (a.E <= 8192) GN_LAUNCH(kernel, 8, 1024, __VA_ARGS__);    \
+  else GN_LAUNCH(kernel, 16, 1024, __VA_ARGS__);                    \
   return launch_status();
 
 template <typename T, bool RMS, bool BLOCK> int gn_fwd(const GnArgs& a, int B, hipStream_t st) {
   const dim3 grid((unsigned)((a.R + gn_rows(a.E) - 1) / gn_rows(a.E)), (unsigned)B);
-  GN_FORMS(gn_fwd_kernel)
+  GN_FORMS(gn_fwd_kernel, RMS, BLOCK)
 }
 template <typename T, bool RMS, bool BLOCK> int gn_bwd(const GnArgs& a, int B, hipStream_t st) {
   const dim3 grid((unsigned)a.blocks, (unsigned)B);
-  GN_FORMS(gn_bwd_kernel)
+  GN_FORMS(gn_bwd_kernel, RMS, BLOCK, false)
+}
+template <typename T, bool RMS, bool BLOCK> int gn_bwd_bias(const GnArgs& a, int B, hipStream_t st) {
+  const dim3 grid((unsigned)a.blocks, (unsigned)B);
+  GN_FORMS(gn_bwd_kernel, RMS, BLOCK, true)
 }
 #define GN_PICK(fn, a, B, st)                                                                                                \
   (dtype == HFTA_BF16 ? (norm == HFTA_NORM_RMS ? (F ? fn<bf16_raw, true, true>(a, B, st) : fn<bf16_raw, true, false>(a, B, st))    \
@@ -340,7 +380,7 @@ int hfta_gated_residual_norm_fwd(int B, int R, int E, int dtype, int norm, const
 
 size_t hfta_gated_residual_norm_bwd_workspace_bytes(int B, int R, int E) {
   if (gn_check(B, R, E, HFTA_F32, HFTA_NORM_RMS) != HFTA_OK) return 0;
-  return (size_t)B * gn_blocks(B, R, E) * gn_rows(E) * (4 * (size_t)E + 4) * sizeof(float);
+  return (size_t)B * gn_blocks(B, R, E, 3) * gn_rows(E) * (4 * (size_t)E + 4) * sizeof(float);
 }
 
 int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
@@ -361,10 +401,10 @@ int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const
   a.X = X; a.F = F; a.G = G; a.w1 = w1; a.b1 = b1; a.res = res; a.w2 = w2; a.dS = dS; a.dY = dY; a.dX = dX; a.dF = dF; a.dG = dG;
   a.m1 = const_cast<float*>(mean1); a.i1 = const_cast<float*>(inv1); a.m2 = const_cast<float*>(mean2); a.i2 = const_cast<float*>(inv2);
   a.R = R; a.E = E; a.part = reinterpret_cast<float*>(workspace);
-  a.blocks = gn_blocks(B, R, E);
-  a.need_db = db1 || db2;
+  const bool bias = db1 || db2;
+  a.blocks = gn_blocks(B, R, E, bias || dtype == HFTA_F32 ? 2 : 3);
   hipStream_t st = as_stream(stream);
-  const int r = GN_PICK(gn_bwd, a, B, st);
+  const int r = bias ? GN_PICK(gn_bwd_bias, a, B, st) : GN_PICK(gn_bwd, a, B, st);
   if (r != HFTA_OK) return r;
   const dim3 grid((unsigned)((4 * (int64_t)E + 1 + 63) / 64), (unsigned)B);
   hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks * gn_rows(E), E, dw2, db2, dw1, db1, dres);

@@ -29,6 +29,27 @@ template <typename T> struct Piece16 {
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = e < n ? Elem<T>::load(p + e) : 0.f;
   }
+  // the same in two steps: what memory holds, and its values
+  static __device__ __forceinline__ piece_u4 raw(const T* p, int n) {
+    if (n >= N) return *reinterpret_cast<const piece_u4*>(p);
+    union { piece_u4 u; T e[N]; } v;
+    v.u = piece_u4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < n) v.e[e] = p[e];
+    return v.u;
+  }
+  static __device__ __forceinline__ void values(float (&x)[N], piece_u4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+      } else {
+        x[i] = __uint_as_float(v[i]);
+      }
+    }
+  }
   static __device__ __forceinline__ void store(T* p, const float (&x)[N]) {
     piece_u4 v;
 #pragma unroll
