@@ -4,13 +4,14 @@
 namespace hfta {
 namespace {
 
-int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
-  if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || R > 0x7fffffff - 4096) return HFTA_EINVAL;
-  // (a launch has fewer than 2^32 threads: three jobs, a workgroup for each head and tile at most)
-  return d > 128 || nseq > PACKED_MAX || B > 65535 || (int64_t)B * Hq > 0x3fffff / ((R + LA_T - 1) / LA_T) ? HFTA_EUNSUPPORTED : HFTA_OK;
-}
 // Blocks of tiles: about LA_WANT of all heads together.  With R their number only grows, so that the workspace for the most rows serves fewer.
 constexpr int LA_WANT = 512, LA_SCAN = 8, LA_FEW = 64, LA_SHORT = 256;
+int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
+  if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || R > 0x7fffffff - 4096) return HFTA_EINVAL;
+  // (a launch has fewer than 2^32 threads: three jobs of up to 512 threads for each query head and block)
+  const int64_t heads = (int64_t)B * Hkv > LA_WANT ? (int64_t)B * Hkv : LA_WANT;
+  return d > 128 || nseq > PACKED_MAX || B > 65535 || heads > 0x1fffff / (Hq / Hkv) ? HFTA_EUNSUPPORTED : HFTA_OK;
+}
 int64_t la_limit(int B, int Hkv, int want) { return (int64_t)B * Hkv < want ? want / ((int64_t)B * Hkv) : 1; }
 void la_cut(LaArgs& a, int Hq, int dtype) {
   a.by_heads = PkDiv((uint32_t)(a.B * Hq));

@@ -6,6 +6,9 @@
 // d.  A workgroup takes one token and key head with all query heads of its group.  A row of the state lies across lanes, four columns
 // each, and a lane's share of it (16 rows at d = 128) is in flight at once; the sums over rows pass through LDS.
 //
+// lambda goes in as its fp32 value and the rest: a rounded lambda alone would change the rate at which a state forgets by 2^-25 / |log_decay|, the
+// same way in every step.
+//
 // Rows of a call that name the same slot are tokens of one sequence, in order: the workgroup of the first takes them all, the others
 // find an earlier one and end.  (No two workgroups touch one state.)
 #include "pieces.h"
@@ -43,6 +46,7 @@ template <typename T, int D, int W> __global__ __launch_bounds__(256) void ls_ke
   const float* src = a.S + at;
   float* dst = a.S2 + at;
   const float g = a.ld[(int64_t)b * a.Hkv + hk], lambda = expf(g > 0.f ? 0.f : g);
+  const float rest = lambda >= 0.5f ? expm1f(g > 0.f ? 0.f : g) - (lambda - 1.f) : 0.f;       // (the difference is exact)
   const bool has = c0 < d;                                       // (W divides d, or is 1)
   vec st[RPT];
 #pragma unroll
@@ -79,7 +83,7 @@ template <typename T, int D, int W> __global__ __launch_bounds__(256) void ls_ke
     for (int j = 0; j < RPT; ++j) {
       const int r = rg + j * GROUPS;
       if (has && r < d) {
-        st[j] = lambda * st[j] + sk[r] * vv;
+        st[j] = lambda * st[j] + (rest * st[j] + sk[r] * vv);
         *reinterpret_cast<vec*>(dst + r * d + c0) = st[j];
       }
     }

@@ -116,6 +116,42 @@ def test_values_and_gradients(hb, dtype, lengths, heads, d):
         c.check()
 
 
+BLOCKS = {  # B, lengths, Hq, Hkv: how rows are cut into blocks of tiles, and blocks of more than eight tiles
+    "one block": (4, [[1100, 0, 80], [3, 1200, 1], [640, 500, 5], [64, 64, 1000]], 65, 65),
+    "one block, groups": (4, [[900, 0, 80], [3, 700, 1], [640, 300, 5], [64, 64, 800]], 130, 65),
+    "sums of few rows": (1, [[500, 3]], 4, 2),
+    "sums of long blocks": (2, [[2600, 0, 1, 2300], [4990, 2, 3, 4]], 40, 40),
+    "sums of long blocks, groups": (2, [[2600, 0, 1, 1300], [3500, 2, 3, 4]], 80, 40),
+    "sums along the sequences": (1, [[1000, 40, 4000, 0, 3600]], 64, 32),
+    "short ones, long blocks": (2, [[70, 200, 0, 1, 64, 128, 900, 30, 7, 99, 500, 2], [50] * 11 + [1500]], 100, 100),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("d", [24, 64, 128])
+@pytest.mark.parametrize("blocks", list(BLOCKS))
+def test_blocks_of_tiles(hb, dtype, states, d, blocks):
+    """Some heads of calls with so many that rows fall into few blocks.  Memories that last, so that every block's sum matters."""
+    B, lengths, Hq, Hkv = BLOCKS[blocks]
+    g = torch.Generator().manual_seed(d)
+    c = Case(dtype, B, lengths, Hq, Hkv, d, first=3, behind=5, seed=d, decay=-(torch.rand(B, Hkv, generator=g) * 4 - 10).exp(), states=states)
+    c.fwd(hb)
+    c.bwd(hb)
+    torch.cuda.synchronize()
+    G = Hq // Hkv
+    for b, h in ((0, 0), (B - 1, Hkv - 1), (B // 2, Hkv // 3)):
+        part = object.__new__(Case)
+        part.dtype, part.R, part.off, part.scale, part.ld = dtype, c.R, c.off[b:b + 1], c.scale, c.ld[b:b + 1, h:h + 1]
+        for names, lo, n in ((("q", "dctx", "ctx", "dq"), h * G, G), (("k", "v", "dk", "dv"), h, 1)):
+            for m in names:
+                setattr(part, m, getattr(c, m)[b:b + 1, :, lo:lo + n])
+        for m in ("s0", "dsf", "s1", "ds0"):
+            t = getattr(c, m)
+            setattr(part, m, t[b:b + 1, :, h:h + 1] if states else None)
+        part.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["heads", "odd"])
 @pytest.mark.parametrize("d", [13, 48, 64, 128])
