@@ -8,10 +8,13 @@
 //   ds = dS + N'(dY w2, sh, i2),   dX = ds,   du = res h ds,   dF = N'(du w1, fh, i1),   dG = res ds u h (1 - h)
 //   dw1 = sum du fh,  db1 = sum du,  dw2 = sum dY sh,  db2 = sum dY,  dres = sum h u ds      (sums over rows)
 //
-// Bound by memory: a row is read once and stays in registers, a thread's share of 8 or 16 elements, through both norms; a wavefront or a
-// workgroup has a row.  The backward call forms S again from X, F and G rather than read its rounded copy (as many bytes, and the
-// gradients are those of what Y was made of).  Sums over rows stay in registers across a workgroup's rows, pass through the
-// workspace and are added in order.
+// Bound by memory: a row is read once and stays in registers, a thread's share of 8 elements (16 past 8192 columns), through both norms; a row has as many
+// threads as that takes: 8 or 32 lanes, a wavefront, 128 to 1024 threads.  5 x 9633 rows, bf16, both directions: 40 us at 16 columns and 86 at 200, where
+// a wavefront for each row took 125 and 132; 32 lanes for 16 columns would leave three quarters of them idle.  The backward call forms S
+// again from X, F and G rather than read its rounded copy (as many bytes, and the gradients are those of what Y was made of).  Sums over rows stay in
+// registers across a workgroup's rows, pass through the workspace and are added in order.
+//
+// 2 x 8192 rows of 2048 bf16, gate, without means: forward 77 us (10 bytes an element, 4.4 TB/s), backward 130 (16 bytes, 4.1 TB/s), sums 15.
 #include "pieces.h"
 
 namespace hfta {
@@ -26,14 +29,21 @@ struct GnArgs {
   int R, E, blocks;                // blocks: workgroups of a model
 };
 constexpr int GN_MAX_BLOCKS = 1024;
+constexpr int gn_threads(int tpr) { return tpr < 256 && tpr != 128 ? 256 : tpr; }      // of a workgroup, by the threads of a row
 
 template <int TPR> struct GnSum {
   float lds[2][2][TPR > 64 ? TPR / 64 : 1];
 };
+// the sum over a row's lanes of a wavefront
+template <int TPR> __device__ __forceinline__ float gn_lanes(float x) {
+#pragma unroll
+  for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
 // two sums over the TPR threads of a row; `turn` alternates between calls, so that one barrier is enough
 template <int TPR> __device__ __forceinline__ void gn_sum(GnSum<TPR>& s, int turn, float& x, float& y) {
-  x = wave_sum(x);
-  y = wave_sum(y);
+  x = gn_lanes<TPR>(x);
+  y = gn_lanes<TPR>(y);
   if constexpr (TPR > 64) {
     const int w = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) { s.lds[turn][0][w] = x; s.lds[turn][1][w] = y; }
@@ -103,13 +113,13 @@ __device__ __forceinline__ void gn_stats(GnSum<TPR>& sum, int& turn, float (&x)[
 __device__ __forceinline__ float gn_sigma(float x) { return 1.f / (1.f + expf(-x)); }
 
 template <typename T, int NP, int TPR, bool RMS, bool BLOCK>
-__global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_fwd_kernel(GnArgs a) {
+__global__ __launch_bounds__(gn_threads(TPR)) void gn_fwd_kernel(GnArgs a) {
   typedef GnRow<T, NP, TPR> Row;
-  constexpr int N = Piece16<T>::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  constexpr int N = Piece16<T>::N, NT = gn_threads(TPR), RPB = NT / TPR;
   __shared__ GnSum<TPR> sum;
   const int b = blockIdx.y, E = a.E;
   const int r = blockIdx.x * RPB + threadIdx.x / TPR;
-  if (r >= a.R) return;                                          // (a whole wavefront; workgroups of one row never)
+  if (r >= a.R) return;                                          // (all lanes of a row; workgroups of one row never)
   const int64_t row = (int64_t)b * a.R + r, at = row * E;
   int turn = 0;
   float f[NP][N], x[NP][N];
@@ -146,12 +156,15 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR)) void gn_fwd_kernel(GnArgs 
 }
 
 // Partial sums of a workgroup's rows, in part[model][workgroup][4 E + 4] (dw2, db2, dw1, db1, and dres in the next word).  The next row is on its way
-// while one is computed,.  BIAS: sums of the gradients themselves are wanted
+// while one is computed (the case
+// above: 227 -> 130 us; with four wavefronts a SIMD instead of three its registers spill).  1024 threads leave a thread 128 registers, too few to
+// hold a second row, and past 8192 columns too few for one: those rows pass through scratch memory.  BIAS: sums of the gradients themselves are wanted;
+// without them (a norm without biases) 16 registers are free.
 template <typename T, int NP, int TPR, bool RMS, bool BLOCK, bool BIAS>
-__global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS || sizeof(T) == 4 || TPR == 512 ? 2 : 3)) void gn_bwd_kernel(GnArgs a) {
+__global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(T) == 4 || TPR == 512 ? 2 : 3)) void gn_bwd_kernel(GnArgs a) {
   typedef GnRow<T, NP, TPR> Row;
   typedef Piece16<T> P;
-  constexpr int N = P::N, NT = TPR == 64 ? 256 : TPR, RPB = NT / TPR;
+  constexpr int N = P::N, NT = gn_threads(TPR), RPB = NT / TPR;
   constexpr bool AHEAD = TPR < 1024;
   __shared__ GnSum<TPR> sum;
   const int b = blockIdx.y, E = a.E;
@@ -159,7 +172,9 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS ||
   const float *w1 = a.w1 + (int64_t)b * E, *b1 = a.b1 ? a.b1 + (int64_t)b * E : nullptr, *w2 = a.w2 + (int64_t)b * E;
   float dw1[NP][N], db1[NP][N], dw2[NP][N], db2[NP][N], dres = 0.f;
   GN_EACH(NP, N) dw1[p][e] = db1[p][e] = dw2[p][e] = db2[p][e] = 0.f;
-  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x * RPB + threadIdx.x / TPR), parts = a.blocks * RPB;
+  int first = blockIdx.x * RPB + threadIdx.x / TPR;
+  if (TPR >= 64) first = __builtin_amdgcn_readfirstlane(first);
+  const int step = a.blocks * RPB;
   float w[NP][N], c[NP][N], v[NP][N];
   auto weights = [&]() __attribute__((always_inline)) {
     if constexpr (BLOCK) {
@@ -192,8 +207,8 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS ||
     }
   };
   int turn = 0;
-  if (AHEAD && part < a.R) load(part);
-  for (int r = part; r < a.R; r += parts) {
+  if (AHEAD && first < a.R) load(first);
+  for (int r = first; r < a.R; r += step) {
     const int64_t at = ((int64_t)b * a.R + r) * E;
     if (!AHEAD) load(r);
     float x[NP][N], f[NP][N], g[NP][N], dy[NP][N], ds[NP][N], u[NP][N];
@@ -208,7 +223,7 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS ||
       if (a.dS) P::values(ds[p], in.ds[p]);
     }
     const float mean1 = m1, inv1 = i1, mean2 = m2, inv2 = i2;
-    if (AHEAD && r + parts < a.R) load(r + parts);
+    if (AHEAD && r + step < a.R) load(r + step);
     weights();
     if constexpr (BLOCK) {
       GN_EACH(NP, N) {
@@ -254,6 +269,21 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS ||
       Row::store(reinterpret_cast<T*>(a.dF) + at, dy, E);
     }
   }
+  if constexpr (TPR < 64) {                                      // a wavefront's rows
+    auto rows = [](float& x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int o = TPR; o < 64; o <<= 1) x += __shfl_xor(x, o, 64);
+    };
+    GN_EACH(NP, N) {
+      rows(dw2[p][e]);
+      if (BIAS) rows(db2[p][e]);
+      if (BLOCK) rows(dw1[p][e]);
+      if (BLOCK && BIAS) rows(db1[p][e]);
+    }
+    if (BLOCK) rows(dres);
+  }
+  const int part = TPR < 64 ? blockIdx.x * (NT / 64) + threadIdx.x / 64 : first, parts = TPR < 64 ? a.blocks * (NT / 64) : step;
+  if (TPR < 64 && (threadIdx.x & 63) >= TPR) return;             // (no barriers below)
   float* out = a.part + ((int64_t)b * parts + part) * (4 * (int64_t)E + 4);
   auto put = [&](float* to, const float (&y)[NP][N]) __attribute__((always_inline)) {
 #pragma unroll
@@ -273,7 +303,7 @@ __global__ __launch_bounds__((TPR == 64 ? 256 : TPR), (TPR == 1024 ? 4 : BIAS ||
       float none = 0.f;
       gn_sum<TPR>(sum, turn, dres, none);
     } else {
-      dres = wave_sum(dres);
+      dres = gn_lanes<TPR>(dres);
     }
     if (threadIdx.x % TPR == 0) out[4 * (int64_t)E] = dres;
   }
@@ -311,7 +341,8 @@ __global__ __launch_bounds__(GN_ADD) void gn_add_kernel(const float* part, int p
 }
 
 constexpr int GN_MAX_E = 16384;
-int gn_rows(int E) { return E <= 512 ? 4 : 1; }                  // rows of a workgroup
+int gn_rows(int E) { return E <= 64 ? 32 : E <= 256 ? 8 : E <= 512 ? 4 : 1; }     // rows of a workgroup
+int gn_parts(int E) { return E <= 512 ? 4 : 1; }                 // and its partial sums
 // workgroups of a model in the backward call: as many as are resident at once, `per` on each of the 256 compute units
 int gn_blocks(int B, int R, int E, int per) {
   const int rows = (R + gn_rows(E) - 1) / gn_rows(E);
@@ -329,9 +360,11 @@ int gn_check(int B, int R, int E, int dtype, int norm) {
 
 // pieces of a thread and threads of a row; the other template arguments
 #define GN_LAUNCH(kernel, EL, TPR, ...) \
-  hipLaunchKernelGGL((kernel<T, EL / Piece16<T>::N, TPR, __VA_ARGS__>), grid, dim3(TPR == 64 ? 256 : TPR), 0, st, a)
+  hipLaunchKernelGGL((kernel<T, EL / Piece16<T>::N, TPR, __VA_ARGS__>), grid, dim3(gn_threads(TPR)), 0, st, a)
 #define GN_FORMS(kernel, ...)                                       \
-  if (a.E <= 512) GN_LAUNCH(kernel, 8, 64, __VA_ARGS__);            \
+  if (a.E <= 64) GN_LAUNCH(kernel, 8, 8, __VA_ARGS__);              \
+  else if (a.E <= 256) GN_LAUNCH(kernel, 8, 32, __VA_ARGS__);       \
+  else if (a.E <= 512) GN_LAUNCH(kernel, 8, 64, __VA_ARGS__);       \
   else if (a.E <= 1024) GN_LAUNCH(kernel, 8, 128, __VA_ARGS__);     \
   else if (a.E <= 2048) GN_LAUNCH(kernel, 8, 256, __VA_ARGS__);     \
   else if (a.E <= 4096) GN_LAUNCH(kernel, 8, 512, __VA_ARGS__);     \
@@ -380,7 +413,7 @@ int hfta_gated_residual_norm_fwd(int B, int R, int E, int dtype, int norm, const
 
 size_t hfta_gated_residual_norm_bwd_workspace_bytes(int B, int R, int E) {
   if (gn_check(B, R, E, HFTA_F32, HFTA_NORM_RMS) != HFTA_OK) return 0;
-  return (size_t)B * gn_blocks(B, R, E, 3) * gn_rows(E) * (4 * (size_t)E + 4) * sizeof(float);
+  return (size_t)B * gn_blocks(B, R, E, 3) * gn_parts(E) * (4 * (size_t)E + 4) * sizeof(float);
 }
 
 int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
@@ -407,7 +440,7 @@ int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const
   const int r = bias ? GN_PICK(gn_bwd_bias, a, B, st) : GN_PICK(gn_bwd, a, B, st);
   if (r != HFTA_OK) return r;
   const dim3 grid((unsigned)((4 * (int64_t)E + 1 + 63) / 64), (unsigned)B);
-  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks * gn_rows(E), E, dw2, db2, dw1, db1, dres);
+  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks * gn_parts(E), E, dw2, db2, dw1, db1, dres);
   return launch_status();
 }
 
