@@ -4,7 +4,9 @@
 namespace hfta {
 namespace {
 
-// Blocks of tiles: about LA_WANT of all heads together.  With R their number only grows, so that the workspace for the most rows serves fewer.
+// Blocks of tiles: about LA_WANT of all heads together, which is two or three workgroups on each compute unit; half as many where a compute unit holds one
+// (128 columns of fp32 or with states: 80 KB of LDS, or registers for one) and in the backward call, whose three jobs run side by side (8 x 2048 rows, 4
+// heads of 64 bf16, both directions: 57 us with 512 for each job, 51 with 256, 62 with 170; 2 x 16384 rows, 8 heads of 128: 437, 412, 429).  With R their number only grows, so that the workspace for the most rows serves fewer.
 constexpr int LA_WANT = 512, LA_SCAN = 8, LA_FEW = 64, LA_SHORT = 256;
 int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || R > 0x7fffffff - 4096) return HFTA_EINVAL;
@@ -20,12 +22,13 @@ void la_cut(LaArgs& a, int Hq, int dtype) {
   a.by_hkv = PkDiv((uint32_t)a.Hkv);
   bool states = false;
   for (int j = 0; j < a.jobs; ++j) states = states || a.job[j].S0 || a.job[j].S1;
-  const int64_t most = la_limit(a.B, a.Hkv, a.d > 64 && (dtype == HFTA_F32 || states) ? LA_WANT / 2 : LA_WANT);
+  const int64_t most = la_limit(a.B, a.Hkv, a.jobs > 1 || (a.d > 64 && (dtype == HFTA_F32 || states)) ? LA_WANT / 2 : LA_WANT);
   a.tiles = (a.R + LA_T - 1) / LA_T;
   a.per = (int)((a.tiles + most - 1) / most);
   a.blocks = (a.tiles + a.per - 1) / a.per;
-  // Short sequences are walked up to a block once more instead of summed: no launches for states.  A long one among them costs its tiles again,
-  // so that this is left to batches of few rows.
+  // Short sequences are walked up to a block once more instead of summed: no launches for states (the first of the cases above: 74 us with states).  A
+  // long one among them costs its tiles again, so that this is left to batches of few rows.  Sums of up to eight blocks are added up by the blocks
+  // themselves; more are scanned, since that work grows with their square.
   a.mode = a.blocks == 1 ? LA_ALONE : a.tiles <= LA_FEW && a.R / a.nseq <= LA_SHORT ? LA_WALK : a.blocks > LA_SCAN ? LA_SCANNED : LA_SUMS;
 }
 size_t la_workspace(int B, int R, int Hkv, int d, int sums) {

@@ -50,6 +50,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   __shared__ float pw[LA_T + 1], fade[LA_T + 1], dw[2 * LA_T + 1];      // lambda^n, lambda^n - 1; behind LA_T places of nothing lambda^n fo
   const LaWave<D> wave;
   const int t = threadIdx.x;
+  la_touch(a);
   const LaPlace at(a, false);
   if (at.none) return;
   const LaJob& J = a.job[at.job];
@@ -71,12 +72,13 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   auto fetch_a = [&](int tile, int x) __attribute__((always_inline)) { sa.fetch(l0 + x * Stage::BYTES, pa + row0(tile) * lda, lda, a.R - row0(tile), a.d, rev); };
   const la_lds lb = l0 + 2 * Stage::BYTES, lc = l0 + 3 * Stage::BYTES;
   const unsigned char *tb = tiles + 2 * Stage::BYTES, *tc = tiles + 3 * Stage::BYTES;
-  auto fetch_bc = [&](int tile, int h) __attribute__((always_inline)) {
+  auto fetch_bc = [&](int tile, int h, int back = 0) __attribute__((always_inline)) {        // back: two tiles before their places
     const int m0 = row0(tile);
-    sb.fetch(lb, pb + h * J.bs.h + m0 * ldb, ldb, a.R - m0, a.d, rev);
-    sc.fetch(lc, pc + h * J.cs.h + m0 * ldc, ldc, a.R - m0, a.d, rev);
+    sb.fetch(lb - back, pb + h * J.bs.h + m0 * ldb, ldb, a.R - m0, a.d, rev);
+    sc.fetch(lc - back, pc + h * J.cs.h + m0 * ldc, ldc, a.R - m0, a.d, rev);
   };
   const float raw = a.ld[(int64_t)at.b * a.Hkv + hk];
+  const int32_t warm = off[min(t, a.nseq)];                      // (on their way while the tables are formed)
   fetch_a(first, 0);
   if (a.mode != LA_WALK) fetch_bc(first, 0);
   la_f4 s[D / 16];
@@ -92,6 +94,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
     dw[LA_T + t] = J.fo * la_pow(ld, t);
   }
   if (t < LA_T) dw[t] = 0.f;
+  asm volatile("" :: "v"(warm));
 
   if constexpr (PIECES) {
     if (keeps)                                                   // sequences without rows, by all wavefronts
@@ -145,26 +148,32 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
         for (int n = 0; n < D / 16; ++n) s[n] += v[n];
       }
     } else if (a.mode == LA_WALK) {
-      // sequences are short: their rows up to here once more.  c's and b's tiles lie where the walk's will
+      // sequences are short: their rows up to here once more.  b's and c's tiles lie where the walk's will, and in the places of A's in turn
       if (PIECES && J.S0) la_load_state<T, D>(s, J, a, at.b, la_sequence(off, a.nseq, m0 + r), hk, wave);
+      int tile = begin / LA_T, h = 0, i = 0;
+      bool more;
+      fetch_bc(tile, 0);
 #pragma unroll 1
-      for (int tile = begin / LA_T; tile < first; ++tile) {
-        const int c0 = max(begin - tile * LA_T, 0), n = LA_T - c0 - (PIECES && J.S0 && rev && tile == begin / LA_T ? 1 : 0);
-        la_fade(s, fade[n]);
-#pragma unroll 1
-        for (int h = 0; h < G; ++h) {
-          __syncthreads();
-          if (t < LA_T) steps[0].wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
-          fetch_bc(tile, h);
-          la_land<VEC>();
-          if (c0 > 0) {
-            la_clear<T, D>(lb, c0);
-            __syncthreads();
-          }
-          la_update<T, D, false, PIECES>(s, lb, lc, steps[0].wt, 0, LA_T, wave);
+      do {
+        const int c0 = max(begin - tile * LA_T, 0), n = LA_T - c0 - (PIECES && J.S0 && rev && tile == begin / LA_T ? 1 : 0), back = (i & 1) * 2 * Stage::BYTES;
+        if (h == 0) la_fade(s, fade[n]);
+        if (t < LA_T) steps[i & 1].wt[t] = t >= c0 ? pw[LA_T - 1 - t] : 0.f;
+        la_land<VEC>();
+        if (++h == G) {
+          h = 0;
+          ++tile;
         }
-      }
+        more = tile < first;
+        if (more) fetch_bc(tile, h, 2 * Stage::BYTES - back);
+        if (c0 > 0) {
+          la_clear<T, D>(lb - back, c0);
+          __syncthreads();
+        }
+        la_update<T, D, false, PIECES>(s, lb - back, lc - back, steps[i & 1].wt, 0, LA_T, wave);
+        ++i;
+      } while (more);
       __syncthreads();
+      if (i > 1) fetch_a(first, 0);
     }
   }
   if (a.mode == LA_WALK) fetch_bc(first, 0);
