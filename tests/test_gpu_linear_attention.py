@@ -122,7 +122,9 @@ BLOCKS = {  # B, lengths, Hq, Hkv: how rows are cut into blocks of tiles, and bl
     "sums of few rows": (1, [[500, 3]], 4, 2),
     "sums of long blocks": (2, [[2600, 0, 1, 2300], [4990, 2, 3, 4]], 40, 40),
     "sums of long blocks, groups": (2, [[2600, 0, 1, 1300], [3500, 2, 3, 4]], 80, 40),
-    "sums along the sequences": (1, [[1000, 40, 4000, 0, 3600]], 64, 32),
+    "sums of many blocks": (1, [[1000, 40, 4000, 0, 3600]], 64, 32),
+    "sums along the sequences": (1, [[2500, 40, 30, 3000, 0, 3100]], 4, 2),
+    "sums along the sequences, one head": (1, [[4200, 4130]], 2, 1),
     "short ones, long blocks": (2, [[70, 200, 0, 1, 64, 128, 900, 30, 7, 99, 500, 2], [50] * 11 + [1500]], 100, 100),
 }
 
@@ -140,7 +142,7 @@ def test_blocks_of_tiles(hb, dtype, states, d, blocks):
     c.bwd(hb)
     torch.cuda.synchronize()
     G = Hq // Hkv
-    for b, h in ((0, 0), (B - 1, Hkv - 1), (B // 2, Hkv // 3)):
+    for b, h in {(0, 0), (B - 1, Hkv - 1), (B // 2, Hkv // 3)}:
         part = object.__new__(Case)
         part.dtype, part.R, part.off, part.scale, part.ld = dtype, c.R, c.off[b:b + 1], c.scale, c.ld[b:b + 1, h:h + 1]
         for names, lo, n in ((("q", "dctx", "ctx", "dq"), h * G, G), (("k", "v", "dk", "dv"), h, 1)):
