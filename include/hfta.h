@@ -755,7 +755,8 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
  *   SC 2011) of counter (i / 4 low, i / 4 high, site, *step) under the key seed[b] (low word first) is at least 2^32 p[b].  seed: 64 bits [B], step: 32
  *   bits [1] (NULL: 0), device, so that a captured graph draws anew when the caller counts `step` on; site tells calls of one
  *   step apart.  The same call on dY is the backward.  Y may be X itself.
- * EUNSUPPORTED above 65535 models, 2^24 - 2 sequences of a model, and launches of 2^24 workgroups or more.
+ * EUNSUPPORTED above 65535 models, 2^24 - 2 sequences of a model, 2^21 - 1 query heads of all models (linear_attention), and launches of 2^24
+ * workgroups or 2^32 threads or more.
  * ---------------------------------------------------------------------- */
 int hfta_rotary_packed(int B, int R, int nseq, int H, int d, int dtype, const void* X, const int64_t xs[3], const int32_t* positions,
                        int naxes, const int32_t* axis, int pairs, const float* freq, int interleaved, const int32_t* seq_offsets,

@@ -12,13 +12,18 @@
 //
 // Tiles are stretches of the packed rows, whatever sequences they hold: D sees rows of one sequence, Lambda rows of the one that came
 // from the tile before, W rows of the one that goes on into the next.  Against the order everything is mirrored: row j of a tile is its
-// row 63 - j in memory.  Blocks of tiles run side by side: a first launch forms the state that each block's last sequence
-// takes with it, a second adds them up along each sequence, or, where blocks are few, the third does that for itself before it walks its tiles.
+// row 63 - j in memory.  Blocks of tiles run side by side.  What a block's first row brings from the blocks before it comes, by a rule on sizes: from a
+// first launch, which forms the state that each block's last sequence takes with it, added up by each block or, where there are many, along
+// the sequences by a second launch; or, where sequences are short, from their rows in those blocks, walked once more.
 //
 // A wavefront keeps 16 columns of c of the state in the matrix instruction's accumulators, fp32, for the whole walk (D / 16 wavefronts are a
 // workgroup); they are the operand of the product with A without a shuffle, because the update gives b's columns to the accumulator's rows in
 // the order in which rows of A are read.  (A B^T) . D passes through LDS.  bf16: what is rounded to bf16 as an operand (S, W C, the masked
 // products) goes in as two words, value and rest, and W C as three where states are returned: results have the error of their own rounding alone.
+//
+// Nothing bounds it alone.  2 x 16384 rows, 8 heads of 128 bf16, backward, 238 us: rows and results pass at 3.4 TB/s, LDS is active 37 % of the time, matrix
+// instructions 21 %; 44 % of wavefront cycles wait for memory, LDS or a barrier and 26 % for an instruction to issue, along the chain
+// products -> LDS -> products -> state of a tile.  Two workgroups of 128 columns or three of 64 on a compute unit fill each other's waits.
 //
 // Entries that a row does not see are taken out by selects; values of C that are not finite and lie in a tile beside rows that do
 // not see them are taken out of the product and put back as NaN into the rows that do.

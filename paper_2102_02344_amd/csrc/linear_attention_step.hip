@@ -4,7 +4,8 @@
 //
 // A state is d x d fp32 and is read and written whole for each token, which is all that bounds this: 8 d^2 bytes beside a few rows of
 // d.  A workgroup takes one token and key head with all query heads of its group.  A row of the state lies across lanes, four columns
-// each, and a lane's share of it (16 rows at d = 128) is in flight at once; the sums over rows pass through LDS.
+// each, and a lane's share of it (16 rows at d = 128) is in flight at once; the sums over rows pass through LDS.  8 x 96 tokens, 16 heads of 128 over 8,
+// bf16: 168 us, 4.8 TB/s, the rate of a large copy; 2 x 3 tokens of 4 heads of 64: 8.7 us, of which the kernel 5.
 //
 // lambda goes in as its fp32 value and the rest: a rounded lambda alone would change the rate at which a state forgets by 2^-25 / |log_decay|, the
 // same way in every step.
