@@ -731,7 +731,7 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
  *   seq_offsets: the row).  seq_offsets NULL: all rows, nseq is not looked at.  inverse != 0 turns the other way: the gradient.
  * linear_attention: per key head a state S [d][d], S_t = lambda S_t-1 + k_t v_t^T, ctx_t = scale q_t S_t for each query head of its group,
  *   lambda = exp(log_decay[b][h]) (fp32 [B][Hkv], device; -infinity: no memory; above 0 counts as 0), scale > 0 with a finite inverse
- *   (EINVAL).  Heads, strides and alignment as in attention_packed, d <= 128 (EUNSUPPORTED).  In front of sequence s a state is
+ *   (EINVAL), in [2^-32, 2^32] (EUNSUPPORTED).  Heads, strides and alignment as in attention_packed, d <= 128 (EUNSUPPORTED).  In front of sequence s a state is
  *   state_in[b][s][h] (fp32 [B][nseq][Hkv][d][d]; NULL: zeros), behind it state_out[b][s][h] (NULL: not wanted; an empty sequence's
  *   state_in); state_out may not overlap state_in (EINVAL where it is state_in).  bwd: gradients of Q, K, V from the same state_in and, where state_out is used
  *   further, its gradient dstate_out (or NULL); dstate_in (or NULL) gets the gradient of state_in, and may not overlap dstate_out (EINVAL).

@@ -14,6 +14,8 @@ int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   const int64_t heads = (int64_t)B * Hkv > LA_WANT ? (int64_t)B * Hkv : LA_WANT;
   return d > 128 || nseq > PACKED_MAX || B > 65535 || heads > 0x1fffff / (Hq / Hkv) ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
+// Against the order a state is held divided by the scale, which is why that has to lie well inside the range of fp32
+bool la_scale(float scale) { return scale >= 0x1p-32f && scale <= 0x1p32f; }
 int64_t la_limit(int B, int Hkv, int want) { return (int64_t)B * Hkv < want ? want / ((int64_t)B * Hkv) : 1; }
 void la_cut(LaArgs& a, int Hq, int dtype) {
   a.by_heads = PkDiv((uint32_t)(a.B * Hq));
@@ -95,6 +97,7 @@ int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
       (state_out && state_out == state_in))
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
+  if (!la_scale(scale)) return HFTA_EUNSUPPORTED;
   if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 1))) return HFTA_EWORKSPACE;
   LaArgs a{};
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = a.nsums = 1;
@@ -116,6 +119,7 @@ int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
       !dQ || !dqs || !dK || !dV || !dkvs || (dstate_in && dstate_in == dstate_out))
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
+  if (!la_scale(scale)) return HFTA_EUNSUPPORTED;
   if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 2))) return HFTA_EWORKSPACE;
   LaArgs a{};
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3; a.nsums = 2;

@@ -7,22 +7,10 @@
 namespace hfta {
 
 typedef uint32_t piece_u4 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t piece_u2 __attribute__((ext_vector_type(2), aligned(2)));
 
 template <typename T> struct Piece16 {
   static constexpr int N = 16 / (int)sizeof(T);
-  static __device__ __forceinline__ void load(float (&x)[N], const T* p) {
-    const piece_u4 v = *reinterpret_cast<const piece_u4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 2) {
-        x[2 * i] = __uint_as_float(v[i] << 16);
-        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-      } else {
-        x[i] = __uint_as_float(v[i]);
-      }
-    }
-  }
+  static __device__ __forceinline__ void load(float (&x)[N], const T* p) { values(x, *reinterpret_cast<const piece_u4*>(p)); }
   // the first n elements; zeros behind them
   static __device__ __forceinline__ void load(float (&x)[N], const T* p, int n) {
     if (n >= N) return load(x, p);

@@ -118,7 +118,7 @@ def test_linear_attention_refusals(lib):
         assert fwd(**bad) == lib.EINVAL, bad
     for bad in sizes + more + [dict(dctx=None), dict(dQ=None), dict(dqs=None), dict(dK=None), dict(dV=None), dict(dkvs=None), dict(d0=ONE, d1=ONE)]:
         assert bwd(**bad) == lib.EINVAL, bad
-    for bad in (dict(d=129), dict(nseq=1 << 24), dict(B=65536), dict(B=60000, Hq=64, Hkv=64)):
+    for bad in (dict(d=129), dict(nseq=1 << 24), dict(B=65536), dict(B=60000, Hq=64, Hkv=64), dict(scale=1e-10), dict(scale=1e10)):
         assert fwd(**bad) == lib.EUNSUPPORTED and bwd(**bad) == lib.EUNSUPPORTED, bad
     for call, need in ((fwd, lib.linear_attention_fwd_workspace_bytes(2, 1000, 3, 4, 2, 16, 1)),
                        (bwd, lib.linear_attention_bwd_workspace_bytes(2, 1000, 3, 4, 2, 16, 1))):

@@ -247,6 +247,38 @@ def test_values_that_are_not_finite(hb, dtype, d):
                 assert bool((~torch.isfinite(c.ctx[0, fwd_hit.cuda()][:, head].float())).any(1).all()), (what, row, bad)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_gradients_and_states_that_are_not_finite(hb, dtype, d):
+    """A context gradient reaches its own query and the keys and values up to its row; a state its own sequence."""
+    for states in (False, True):
+        for bad in (math.nan, -math.inf):
+            for row in (33, 148):
+                c, good = (Case(dtype, 1, [[20, 130, 30]], 2, 1, d, behind=3, seed=2, states=states) for _ in range(2))
+                c.dctx[0, row, 0, 0] = bad
+                for x in (c, good):
+                    x.bwd(hb)
+                t = torch.arange(c.R)
+                seq = (t >= 20) & (t < 150)
+                for n, h in (("dq", t == row), ("dk", seq & (t <= row)), ("dv", seq & (t <= row))):
+                    assert same(getattr(c, n)[0, (~h).cuda()], getattr(good, n)[0, (~h).cuda()]), (n, row, bad, states)
+                    assert not bool(torch.isfinite(getattr(c, n)[0, h.cuda()][:, 0].float()).all(-1).any()), (n, row, bad, states)
+    for bad in (math.nan, math.inf):
+        c, good = (Case(dtype, 1, [[20, 130, 30]], 2, 1, d, behind=3, seed=2, states=True) for _ in range(2))
+        c.s0[0, 1, 0, 0, 0] = bad
+        c.dsf[0, 1, 0, 0, 0] = bad
+        for x in (c, good):
+            x.fwd(hb)
+            x.bwd(hb)
+        other = (torch.arange(c.R) < 20) | (torch.arange(c.R) >= 150)
+        for n in ("ctx", "dq", "dk", "dv"):
+            assert same(getattr(c, n)[0, other.cuda()], getattr(good, n)[0, other.cuda()]), (n, bad)
+        for n in ("s1", "ds0"):
+            a, b = getattr(c, n), getattr(good, n)
+            assert torch.equal(a[:, ::2], b[:, ::2]) and not bool(torch.isfinite(a[0, 1, 0, 0, 0])), (n, bad)
+        assert not bool(torch.isfinite(c.ctx[0, 20:150, 0].float()).all(-1).any()) and not bool(torch.isfinite(c.dk[0, 20:150, 0].float()).all(-1).any()), bad
+
+
 def test_rows_outside_do_not_matter(hb):
     for dtype in ("f32", "bf16"):
         c = Case(dtype, 2, [[60, 0, 9], [3, 40, 1]], 2, 2, 32, first=7, behind=80, seed=4)
