@@ -125,6 +125,8 @@ BLOCKS = {  # B, lengths, Hq, Hkv: how rows are cut into blocks of tiles, and bl
     "sums of many blocks": (1, [[1000, 40, 4000, 0, 3600]], 64, 32),
     "sums along the sequences": (1, [[2500, 40, 30, 3000, 0, 3100]], 4, 2),
     "sums along the sequences, one head": (1, [[4200, 4130]], 2, 1),
+    "short ones": (2, [[70, 20, 0, 1, 64, 12, 400, 30, 7, 9, 50, 2, 80, 33, 90, 5, 61, 140, 3, 64], [25] * 19 + [600]], 50, 50),
+    "short ones, groups": (2, [[70, 200, 0, 1, 64, 128, 500, 30, 7, 99, 100, 2], [50] * 11 + [700]], 80, 40),
     "short ones, long blocks": (2, [[70, 200, 0, 1, 64, 128, 900, 30, 7, 99, 500, 2], [50] * 11 + [1500]], 100, 100),
 }
 
