@@ -282,30 +282,59 @@ __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(
     }
     if (BLOCK) rows(dres);
   }
-  const int part = TPR < 64 ? blockIdx.x * (NT / 64) + threadIdx.x / 64 : first, parts = TPR < 64 ? a.blocks * (NT / 64) : step;
-  if (TPR < 64 && (threadIdx.x & 63) >= TPR) return;             // (no barriers below)
-  float* out = a.part + ((int64_t)b * parts + part) * (4 * (int64_t)E + 4);
-  auto put = [&](float* to, const float (&y)[NP][N]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int q = 0; q < N / 4; ++q) {
-        const float w4[4] = {y[p][4 * q], y[p][4 * q + 1], y[p][4 * q + 2], y[p][4 * q + 3]};
-        Piece16<float>::store(to + Row::col(p) + 4 * q, w4, E - Row::col(p) - 4 * q);
+  float* out = a.part + ((int64_t)b * a.blocks + blockIdx.x) * (4 * (int64_t)E + 4);
+  if constexpr (TPR <= 64) {                                     // and a workgroup's
+    constexpr int WAVES = NT / 64;
+    __shared__ float lds[WAVES][TPR * NP * N];
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    auto put = [&](float* to, const float (&y)[NP][N]) __attribute__((always_inline)) {
+      __syncthreads();
+      if (lane < TPR) {
+        GN_EACH(NP, N) lds[wv][Row::col(p) + e] = y[p][e];
       }
-  };
-  put(out, dw2);
-  if (BIAS) put(out + E, db2);
-  if constexpr (BLOCK) {
-    put(out + 2 * (int64_t)E, dw1);
-    if (BIAS) put(out + 3 * (int64_t)E, db1);
-    if constexpr (TPR > 64) {
+      __syncthreads();
+      for (int c = threadIdx.x; c < E; c += NT) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x += lds[w][c];
+        to[c] = x;
+      }
+    };
+    put(out, dw2);
+    if (BIAS) put(out + E, db2);
+    if constexpr (BLOCK) {
+      put(out + 2 * (int64_t)E, dw1);
+      if (BIAS) put(out + 3 * (int64_t)E, db1);
+      dres = gn_lanes<TPR>(dres);
+      __syncthreads();
+      if (lane == 0) lds[wv][0] = dres;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x += lds[w][0];
+        out[4 * (int64_t)E] = x;
+      }
+    }
+  } else {
+    auto put = [&](float* to, const float (&y)[NP][N]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) {
+          const float w4[4] = {y[p][4 * q], y[p][4 * q + 1], y[p][4 * q + 2], y[p][4 * q + 3]};
+          Piece16<float>::store(to + Row::col(p) + 4 * q, w4, E - Row::col(p) - 4 * q);
+        }
+    };
+    put(out, dw2);
+    if (BIAS) put(out + E, db2);
+    if constexpr (BLOCK) {
+      put(out + 2 * (int64_t)E, dw1);
+      if (BIAS) put(out + 3 * (int64_t)E, db1);
       float none = 0.f;
       gn_sum<TPR>(sum, turn, dres, none);
-    } else {
-      dres = gn_lanes<TPR>(dres);
+      if (threadIdx.x == 0) out[4 * (int64_t)E] = dres;
     }
-    if (threadIdx.x % TPR == 0) out[4 * (int64_t)E] = dres;
   }
 }
 
@@ -342,7 +371,6 @@ __global__ __launch_bounds__(GN_ADD) void gn_add_kernel(const float* part, int p
 
 constexpr int GN_MAX_E = 16384;
 int gn_rows(int E) { return E <= 64 ? 32 : E <= 256 ? 8 : E <= 512 ? 4 : 1; }     // rows of a workgroup
-int gn_parts(int E) { return E <= 512 ? 4 : 1; }                 // and its partial sums
 // workgroups of a model in the backward call: as many as are resident at once, `per` on each of the 256 compute units
 int gn_blocks(int B, int R, int E, int per) {
   const int rows = (R + gn_rows(E) - 1) / gn_rows(E);
@@ -413,7 +441,7 @@ int hfta_gated_residual_norm_fwd(int B, int R, int E, int dtype, int norm, const
 
 size_t hfta_gated_residual_norm_bwd_workspace_bytes(int B, int R, int E) {
   if (gn_check(B, R, E, HFTA_F32, HFTA_NORM_RMS) != HFTA_OK) return 0;
-  return (size_t)B * gn_blocks(B, R, E, 3) * gn_parts(E) * (4 * (size_t)E + 4) * sizeof(float);
+  return (size_t)B * gn_blocks(B, R, E, 3) * (4 * (size_t)E + 4) * sizeof(float);
 }
 
 int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const void* X, const void* F, const void* G, const float* w1,
@@ -440,7 +468,7 @@ int hfta_gated_residual_norm_bwd(int B, int R, int E, int dtype, int norm, const
   const int r = bias ? GN_PICK(gn_bwd_bias, a, B, st) : GN_PICK(gn_bwd, a, B, st);
   if (r != HFTA_OK) return r;
   const dim3 grid((unsigned)((4 * (int64_t)E + 1 + 63) / 64), (unsigned)B);
-  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks * gn_parts(E), E, dw2, db2, dw1, db1, dres);
+  hipLaunchKernelGGL(gn_add_kernel, grid, dim3(GN_ADD), 0, st, a.part, a.blocks, E, dw2, db2, dw1, db1, dres);
   return launch_status();
 }
 
