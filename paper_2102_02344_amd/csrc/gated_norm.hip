@@ -9,7 +9,7 @@
 //   dw1 = sum du fh,  db1 = sum du,  dw2 = sum dY sh,  db2 = sum dY,  dres = sum h u ds      (sums over rows)
 //
 // Bound by memory: a row is read once and stays in registers, a thread's share of 8 elements (16 past 8192 columns), through both norms; a row has as many
-// threads as that takes: 8 or 32 lanes, a wavefront, 128 to 1024 threads.  5 x 9633 rows, bf16, both directions: 40 us at 16 columns and 86 at 200, where
+// threads as that takes: 8 or 32 lanes, a wavefront, 128 to 1024 threads.  5 x 9633 rows, bf16, both directions: 30 us at 16 columns and 76 at 200, where
 // a wavefront for each row took 125 and 132; 32 lanes for 16 columns would leave three quarters of them idle.  The backward call forms S
 // again from X, F and G rather than read its rounded copy (as many bytes, and the gradients are those of what Y was made of).  Sums over rows stay in
 // registers across a workgroup's rows, pass through the workspace and are added in order.

@@ -389,14 +389,15 @@ template <int N> __device__ __forceinline__ void la_fade(la_f4 (&s)[N], float m1
     for (int i = 0; i < 4; ++i) s[n][i] = fmaf(s[n][i], m1, s[n][i]);
 }
 
-// Workgroup -> (job, model, head of the job, block).  Jobs with as many heads as each other take turns, eight workgroups each, so that a head's and
-// block's jobs, which read the same tiles, follow each other on the same XCD.
 // every line of a launch's arguments at once: what is looked up in them by the job would wait for each of them in turn
 __device__ __forceinline__ void la_touch(const LaArgs& a) {
   const uint32_t* p = reinterpret_cast<const uint32_t*>(&a);
   static_assert(sizeof(LaArgs) > 640 && sizeof(LaArgs) <= 704, "eleven lines");
   asm volatile("" ::"s"(p[0]), "s"(p[16]), "s"(p[32]), "s"(p[48]), "s"(p[64]), "s"(p[80]), "s"(p[96]), "s"(p[112]), "s"(p[128]), "s"(p[144]), "s"(p[160]));
 }
+
+// Workgroup -> (job, model, head of the job, block).  Jobs with as many heads as each other take turns, eight workgroups each, so that a head's and
+// block's jobs, which read the same tiles, follow each other on the same XCD.
 struct LaPlace {
   int job, b, h, blk;
   bool none;                       // past the last place
