@@ -66,13 +66,19 @@ int la_states(const LaArgs& a, const LaForm& f, hipStream_t st); // linear_atten
 int la_main(const LaArgs& a, const LaForm& f, hipStream_t st);   // linear_attention_main.hip
 static inline int la_pad(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-// lambda^n and lambda^n - 1 with the argument's rounding made good; n = 0: 1 and 0 whatever lambda
+// lambda^n with the argument's rounding made good; n = 0: 1 whatever lambda
 __device__ __forceinline__ float la_decay(float ld) { return ld > 0.f ? 0.f : ld; }      // (a NaN stays one)
 __device__ __forceinline__ float la_pow(float g, int n) {
   const float x = (float)n * g, e = fmaf((float)n, g, -x), y = expf(x);
   return n == 0 ? 1.f : x < -100.f ? 0.f : fmaf(y, e, y);
 }
-__device__ __forceinline__ float la_powm1(float g, int n) { return n == 0 ? 0.f : expm1f((float)n * g); }
+// What a state is multiplied by, in one number: lambda^n - 1 (at most 0) where at least half of the state is left, which a rounded lambda^n would
+// make forget at another rate, the same way in every tile; lambda^n itself (above 0) where less is left, of which beside -1 only 2^-25 / lambda^n would be
+// right.  Nothing left: -1.
+__device__ __forceinline__ float la_faded(float g, int n) {
+  const float y = la_pow(g, n);
+  return y >= 0.5f ? n == 0 ? 0.f : expm1f((float)n * g) : y == 0.f ? -1.f : y;
+}
 
 // A staged tile: rows of D columns without padding, as the loads into LDS leave them; piece p (16 bytes) of row r lies at place p ^ key(r).  Sixteen
 // rows' reads of one piece cover all 64 banks, and so do a transpose read's eight rows of two pieces and (fp32) four rows of four.
@@ -382,11 +388,20 @@ __device__ __forceinline__ int la_sequence(const int32_t* off, int nseq, int r) 
   return lo;
 }
 
-template <int N> __device__ __forceinline__ void la_fade(la_f4 (&s)[N], float m1) {       // s times 1 + m1
+// s times what `f` (la_faded) stands for, the same in all lanes
+template <int N> __device__ __forceinline__ void la_fade(la_f4 (&s)[N], float f) {
+  f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f)));
+  if (f > 0.f) {
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n) s[n] *= f;
+  }
+  asm volatile("" : "+s"(f));                                    // (two branches: as one, its ends would take registers of their own)
+  if (!(f > 0.f)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[n][i] = fmaf(s[n][i], m1, s[n][i]);
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] = fmaf(s[n][i], f, s[n][i]);
+  }
 }
 
 // every line of a launch's arguments at once: what is looked up in them by the job would wait for each of them in turn

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   __shared__ __attribute__((aligned(16))) LaStep steps[2];
   __shared__ signed char rels[LA_SPAN / LA_T][LA_T];             // where the rows' sequences begin, of a span's tiles
   __shared__ uint64_t finals[LA_SPAN / LA_T];                    // rows that are their sequence's last one in the order of the walk
-  __shared__ float pw[LA_T + 1], fade[LA_T + 1], dw[2 * LA_T + 1];      // lambda^n, lambda^n - 1; behind LA_T places of nothing lambda^n fo
+  __shared__ float pw[LA_T + 1], fade[LA_T + 1], dw[2 * LA_T + 1];      // lambda^n, la_faded(n); behind LA_T places of nothing lambda^n fo
   const LaWave<D> wave;
   const int t = threadIdx.x;
   la_touch(a);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
   const float ld = la_decay(raw);
   if (t <= LA_T) {
     pw[t] = la_pow(ld, t);
-    fade[t] = la_powm1(ld, t);
+    fade[t] = la_faded(ld, t);
     dw[LA_T + t] = J.fo * la_pow(ld, t);
   }
   if (t < LA_T) dw[t] = 0.f;
@@ -138,12 +138,12 @@ __global__ __launch_bounds__(4 * D, (sizeof(T) == 4 || (PIECES && D == 128) ? 2 
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) s[n] = la_f4{0.f, 0.f, 0.f, 0.f};
     } else if (a.mode == LA_SUMS) {
-      const float m1 = la_powm1(ld, a.per * LA_T);
+      const float f = la_faded(ld, a.per * LA_T);
 #pragma unroll 1
       for (int k = begin / (a.per * LA_T); k < at.blk; ++k) {
         la_f4 v[D / 16];
         la_load_sum<T, D>(v, sum + (int64_t)k * (D * D), J.turned, wave);
-        la_fade(s, m1);
+        la_fade(s, f);
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) s[n] += v[n];
       }

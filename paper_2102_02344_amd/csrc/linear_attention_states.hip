@@ -38,13 +38,13 @@ template <typename T, int D, bool VEC, bool PIECES> __global__ __launch_bounds__
   sb.init(J.bs.r, a.d, rev);
   sc.init(J.cs.r, a.d, rev);
   const la_lds lb = (la_lds)tiles, lc = (la_lds)tiles + Stage::BYTES;
-  const float m64 = la_powm1(ld, LA_T);
+  const float f64 = la_faded(ld, LA_T);
 #pragma unroll 1
   for (int tile = fresh ? begin / LA_T : first; tile <= last; ++tile) {
     const int c0 = max(begin - tile * LA_T, 0), m0 = (rev ? a.tiles - 1 - tile : tile) * LA_T;
     // against the order, what comes in behind the last row has not faded when that row is taken
     const int n = LA_T - c0 - (PIECES && J.S0 && rev && fresh && tile == begin / LA_T ? 1 : 0);
-    la_fade(s, n == LA_T ? m64 : la_powm1(ld, n));
+    la_fade(s, n == LA_T ? f64 : la_faded(ld, n));
 #pragma unroll 1
     for (int h = 0; h < J.gb; ++h) {
       __syncthreads();
@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, int entries) {
   const int hk = (int)(state % a.Hkv), b = (int)(jb % a.B);
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= entries) return;
-  const float m1 = la_powm1(la_decay(a.ld[(int64_t)b * a.Hkv + hk]), a.per * LA_T);
+  const float f = la_faded(la_decay(a.ld[(int64_t)b * a.Hkv + hk]), a.per * LA_T);
+  const bool less = f > 0.f;
   const int* spans = a.spans + jb * a.blocks;
   float4* p = reinterpret_cast<float4*>(a.sums) + (state * a.blocks) * entries + i;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -88,10 +89,10 @@ __global__ __launch_bounds__(256) void la_scan_kernel(LaArgs a, int entries) {
     for (int k = 0; k < AHEAD; ++k)
       if (sp[k]) {
         if (sp[k] == 2) {
-          v[k].x += fmaf(s.x, m1, s.x);
-          v[k].y += fmaf(s.y, m1, s.y);
-          v[k].z += fmaf(s.z, m1, s.z);
-          v[k].w += fmaf(s.w, m1, s.w);
+          v[k].x += fmaf(s.x, f, less ? 0.f : s.x);
+          v[k].y += fmaf(s.y, f, less ? 0.f : s.y);
+          v[k].z += fmaf(s.z, f, less ? 0.f : s.z);
+          v[k].w += fmaf(s.w, f, less ? 0.f : s.w);
           p[(int64_t)(k0 + k) * entries] = v[k];
         }
         s = v[k];

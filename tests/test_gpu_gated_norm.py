@@ -112,6 +112,39 @@ def test_constant_rows_and_eps(hb):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [False, True])
+def test_gates_far_open_and_far_closed(hb, dtype, rms):
+    """The gate's gradient keeps its digits on both sides: sigma' = h (1 - h) is e^-|g| / (1 + e^-|g|)^2, even."""
+    c = Case(2, 40, 96, dtype, rms, seed=9)
+    sides = torch.tensor([-60.0, -20, -17.5, -16, -12, -10, -8, -4, 4, 8, 10, 12, 16, 17.5, 20, 60], device="cuda")
+    c.gate.copy_(sides.repeat(12)[torch.randperm(192, generator=torch.Generator().manual_seed(1)).cuda()].repeat(40).view(2, 40, 96))
+    c.fwd(hb)
+    c.bwd(hb)
+    c.check()
+    h = lambda t: t.double().cpu()
+    names = ("x", "f", "gate", "w1", "b1", "res", "w2", "b2")
+    p = [h(getattr(c, n)) for n in names]
+    x, f, g, w1, b1, res, w2, b2 = p
+    bound = dr.gated_norm_bounds(rms, *p, EPS, h(c.ds), h(c.dy))
+    q = [t.clone().requires_grad_() for t in p]
+    s, y = dr.gated_norm(rms, *q, EPS)
+    ((y * h(c.dy)).sum() + (s * h(c.ds)).sum()).backward()
+    e = torch.exp(-g.abs())
+    slope = res[:, None, None] * e / (1 + e) ** 2
+    # dG = slope ds u.  ds and u as counted for the other gradients; an exponential of 2 roundings, two quotients and four products: 16
+    fc = f if rms else f - f.mean(-1, keepdim=True)
+    i1 = 1 / torch.sqrt((fc * fc).mean(-1, keepdim=True) + EPS)
+    fh = fc * i1
+    u = fh * w1[:, None] + b1[:, None]
+    eu = w1.abs()[:, None] * 60 * dr.U * (i1 * f.abs().amax(-1, keepdim=True) + 1) * (1 + fh.abs()) + 4 * dr.U * ((fh * w1[:, None]).abs() + b1.abs()[:, None])
+    dsm = q[0].grad
+    want = slope * dsm * u
+    b = slope * (bound["dx"] * u.abs() + dsm.abs() * eu + 16 * dr.U * (dsm * u).abs())
+    bad = (h(c.dg) - want).abs() - dr.stored(want, b, dtype)
+    assert float(bad.max()) <= 0, (float(bad.max()), c.gate.flatten()[int(bad.argmax())])
+
+
 def test_rows_that_are_not_finite(hb):
     for rms in (False, True):
         c = Case(2, 21, 100, "bf16", rms, seed=2)

@@ -178,6 +178,34 @@ def test_decays(hb, dtype):
         c.check()
 
 
+FADES = {  # B, lengths, d: one block of tiles, few long ones, sums added up by each block and along the sequences, short sequences walked again
+    "one block": (90, [[200, 0, 61]], 16),
+    "few blocks": (40, [[330, 1, 50]], 32),
+    "sums": (1, [[1100, 20]], 32),
+    "sums along the sequences": (1, [[2300, 30]], 128),
+    "walked": (2, [[100, 90, 150, 7, 64], [64, 128, 30, 1, 70]], 64),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("case", list(FADES))
+def test_what_is_left_of_a_state(hb, dtype, states, case):
+    """Rows that add nothing: a state, and the gradient of one, has faded by many times its own size and keeps its digits.  Without states in and out
+    only a sequence's first keys and last context gradients are not zero."""
+    B, lengths, d = FADES[case]
+    decay = torch.tensor([[-0.05, -0.1, -0.15, -0.2, -0.27, -0.5]])
+    c = Case(dtype, B, lengths * (B // len(lengths)), 6, 6, d, first=3, behind=5, seed=d, decay=decay, states=states)
+    for b in range(B):
+        for lo, hi in zip(c.off[b, :-1].tolist(), c.off[b, 1:].tolist()):
+            n = 0 if states else 5
+            c.k[b, lo + n:hi] = 0.0
+            c.dctx[b, lo:max(hi - n, lo)] = 0.0
+    c.fwd(hb)
+    c.bwd(hb)
+    c.check()
+
+
 def test_a_decay_that_is_no_number(hb):
     decay = torch.tensor([[-0.1, math.nan]])
     c = Case("f32", 2, [[30, 9], [20, 1]], 2, 2, 16, decay=decay)
