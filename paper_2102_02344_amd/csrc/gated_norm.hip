@@ -17,6 +17,8 @@
 // 2 x 8192 rows of 2048 bf16, gate, without means: forward 77 us (10 bytes an element, 4.4 TB/s), backward 130 (16 bytes, 4.1 TB/s), sums 15.
 #include "pieces.h"
 
+#include <type_traits>
+
 namespace hfta {
 namespace {
 
@@ -111,6 +113,30 @@ __device__ __forceinline__ void gn_stats(GnSum<TPR>& sum, int& turn, float (&x)[
 }
 
 __device__ __forceinline__ float gn_sigma(float x) { return 1.f / (1.f + expf(-x)); }
+// A gate h = sigma(x) and 1 - h, each with its own digits (1 - h of an open gate, subtracted from one, has none left past x = 17)
+struct GnTwo {
+  float h, shut;
+  __device__ __forceinline__ void set(float x) {
+    const float e = expf(-x);
+    h = 1.f / (1.f + e);
+    shut = x > 0.f ? e * h : 1.f - h;
+  }
+  __device__ __forceinline__ void none() { h = 1.f; }
+  __device__ __forceinline__ float open() const { return h; }
+  __device__ __forceinline__ float closed() const { return shut; }
+};
+// the same in one register: the smaller of the two, 1 - h with its sign set
+struct GnOne {
+  float v;
+  __device__ __forceinline__ void set(float x) {
+    const float e = expf(-fabsf(x)), y = 1.f / (1.f + e);
+    v = copysignf(e * y, -x);
+  }
+  __device__ __forceinline__ void none() { v = 1.f; }
+  __device__ __forceinline__ int side() const { return __float_as_int(v) >> 31; }
+  __device__ __forceinline__ float open() const { return __int_as_float(side() & 0x3f800000) + v; }
+  __device__ __forceinline__ float closed() const { return __int_as_float(~side() & 0x3f800000) - v; }
+};
 
 template <typename T, int NP, int TPR, bool RMS, bool BLOCK>
 __global__ __launch_bounds__(gn_threads(TPR)) void gn_fwd_kernel(GnArgs a) {
@@ -156,16 +182,19 @@ __global__ __launch_bounds__(gn_threads(TPR)) void gn_fwd_kernel(GnArgs a) {
 }
 
 // Partial sums of a workgroup's rows, in part[model][workgroup][4 E + 4] (dw2, db2, dw1, db1, and dres in the next word).  The next row is on its way
-// while one is computed (the case
-// above: 227 -> 130 us; with four wavefronts a SIMD instead of three its registers spill).  1024 threads leave a thread 128 registers, too few to
-// hold a second row, and past 8192 columns too few for one: those rows pass through scratch memory.  BIAS: sums of the gradients themselves are wanted;
-// without them (a norm without biases) 16 registers are free.
+// while one is computed (the case above: 227 -> 130 us; with four wavefronts a SIMD instead of three its registers spill).  1024 threads leave a thread
+// 128 registers, too few to hold a second row, and with the block's norm too few for one: from 4097 columns on 40 to 160 bytes of a thread pass through
+// scratch memory, past 8192 500 to 780.  BIAS: sums of the gradients themselves are wanted; without them (a norm without biases) 16 registers are free.
 template <typename T, int NP, int TPR, bool RMS, bool BLOCK, bool BIAS>
 __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(T) == 4 || TPR == 512 ? 2 : 3)) void gn_bwd_kernel(GnArgs a) {
   typedef GnRow<T, NP, TPR> Row;
   typedef Piece16<T> P;
   constexpr int N = P::N, NT = gn_threads(TPR), RPB = NT / TPR;
   constexpr bool AHEAD = TPR < 1024;
+  // Registers for 1 - h: without biases, and with the few of 1024 threads, u is formed again rather than held, past 8192 columns from biases loaded again,
+  // and with 1024 threads a gate is one register (2 x 2048 rows of 8192 bf16, both directions: 279 us, with two 303; 5 x 9633 rows of 200: 99 and 95)
+  constexpr bool AGAIN = TPR == 1024 || !BIAS, LOADS = BIAS && NP * N > 8;
+  typedef std::conditional_t<TPR == 1024, GnOne, GnTwo> Gate;
   __shared__ GnSum<TPR> sum;
   const int b = blockIdx.y, E = a.E;
   const float res = BLOCK && a.res ? a.res[b] : 1.f;
@@ -179,7 +208,7 @@ __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(
   auto weights = [&]() __attribute__((always_inline)) {
     if constexpr (BLOCK) {
       Row::weights(w, w1, E, 0.f);
-      Row::weights(c, b1, E, 0.f);
+      if (BIAS) Row::weights(c, b1, E, 0.f);
     }
     Row::weights(v, w2, E, 0.f);
   };
@@ -211,26 +240,40 @@ __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(
   for (int r = first; r < a.R; r += step) {
     const int64_t at = ((int64_t)b * a.R + r) * E;
     if (!AHEAD) load(r);
-    float x[NP][N], f[NP][N], g[NP][N], dy[NP][N], ds[NP][N], u[NP][N];
+    float x[NP][N], f[NP][N], gx[NP][N], dy[NP][N], ds[NP][N];
+    Gate g[NP][N];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       P::values(x[p], in.x[p]);
       if constexpr (BLOCK) {
         P::values(f[p], in.f[p]);
-        if (a.G) P::values(g[p], in.g[p]);
+        if constexpr (AHEAD) {                                    // (gates are formed with the next row's loads on their way)
+          if (a.G) P::values(gx[p], in.g[p]);
+        } else if (a.G) {
+          float raw[N];
+          P::values(raw, in.g[p]);
+#pragma unroll
+          for (int e = 0; e < N; ++e) g[p][e].set(raw[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) g[p][e].none();
+        }
       }
       P::values(dy[p], in.dy[p]);
       if (a.dS) P::values(ds[p], in.ds[p]);
     }
+    auto block = [&](int p, int e) __attribute__((always_inline)) { return BIAS ? fmaf(f[p][e], w[p][e], c[p][e]) : f[p][e] * w[p][e]; };     // u
     const float mean1 = m1, inv1 = i1, mean2 = m2, inv2 = i2;
     if (AHEAD && r + step < a.R) load(r + step);
     weights();
     if constexpr (BLOCK) {
       GN_EACH(NP, N) {
         f[p][e] = RMS ? f[p][e] * inv1 : Row::col(p) + e < E ? (f[p][e] - mean1) * inv1 : 0.f;
-        u[p][e] = fmaf(f[p][e], w[p][e], c[p][e]);
-        g[p][e] = a.G ? gn_sigma(g[p][e]) : 1.f;
-        x[p][e] = fmaf(res * g[p][e], u[p][e], x[p][e]);
+        if constexpr (AHEAD) {
+          if (a.G) g[p][e].set(gx[p][e]);
+          else g[p][e].none();
+        }
+        x[p][e] = fmaf(res * g[p][e].open(), block(p, e), x[p][e]);
       }
     }
     float s = 0.f, z = 0.f;
@@ -250,17 +293,22 @@ __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(
     Row::store(reinterpret_cast<T*>(a.dX) + at, ds, E);
     if constexpr (BLOCK) {
       s = z = 0.f;
+      if constexpr (LOADS) Row::weights(c, b1, E, 0.f);
+      if constexpr (AGAIN) {
+        GN_EACH(NP, N) asm volatile("" : "+v"(f[p][e]));
+      }
       GN_EACH(NP, N) {
-        const float hd = RMS || Row::col(p) + e < E ? g[p][e] * ds[p][e] : 0.f, du = res * hd;       // (z makes ds not zero behind the row)
-        dres = fmaf(hd, u[p][e], dres);
+        const float u = block(p, e);
+        const float hd = RMS || Row::col(p) + e < E ? g[p][e].open() * ds[p][e] : 0.f, du = res * hd;       // (z makes ds not zero behind the row)
+        dres = fmaf(hd, u, dres);
         dw1[p][e] = fmaf(du, f[p][e], dw1[p][e]);
         if (BIAS) db1[p][e] += du;
-        if (a.G) g[p][e] = du * u[p][e] * (1.f - g[p][e]);       // dG
+        ds[p][e] = du * u * g[p][e].closed();                     // dG
         dy[p][e] = du * w[p][e];
         s = fmaf(dy[p][e], f[p][e], s);
         if (!RMS) z += dy[p][e];
       }
-      if (a.G) Row::store(reinterpret_cast<T*>(a.dG) + at, g, E);
+      if (a.G) Row::store(reinterpret_cast<T*>(a.dG) + at, ds, E);
       gn_sum<TPR>(sum, turn, s, z);
       turn ^= 1;
       s /= (float)E;
