@@ -431,7 +431,10 @@ int gn_blocks(int B, int R, int E, int per) {
 
 int gn_check(int B, int R, int E, int dtype, int norm) {
   if (B <= 0 || R <= 0 || E <= 0 || !valid_dtype(dtype) || (norm != HFTA_NORM_RMS && norm != HFTA_NORM_LAYER)) return HFTA_EINVAL;
-  return E > GN_MAX_E || B > 65535 || R > 0x7fffffff - 4096 || (R + gn_rows(E) - 1) / gn_rows(E) > 0x3fffff ? HFTA_EUNSUPPORTED : HFTA_OK;
+  if (E > GN_MAX_E || B > 65535) return HFTA_EUNSUPPORTED;
+  const int64_t threads = E <= 512 ? 256 : E <= 1024 ? 128 : E <= 2048 ? 256 : E <= 4096 ? 512 : 1024;       // of a workgroup
+  const int64_t blocks = ((int64_t)R + gn_rows(E) - 1) / gn_rows(E);
+  return blocks > 0xffffff || blocks * threads > 0xffffffff ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 
 // pieces of a thread and threads of a row; the other template arguments

@@ -220,3 +220,28 @@ def test_past_2_31_elements(hb):
     # 60 roundings of fp32 and one of bf16
     assert float(((y[:, -2:].double().cpu() - want).abs() - (2.0 ** -8 + 120 * dr.U) * want.abs()).max()) <= 0
     assert not bool(y[0, -4:-2].any())
+
+
+def test_millions_of_rows(hb):
+    """Rows of 128 threads, more than 2^22 of them; the last ones, behind a long stretch of zeros."""
+    R, E, n = 5000000, 600, 3
+    g = torch.Generator().manual_seed(4)
+    x, dy = (torch.zeros(1, R, E, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, dy):
+        t[0, -n:] = torch.randn(n, E, generator=g).bfloat16().cuda()
+    y, dx = (torch.full_like(x, 7.0) for _ in range(2))
+    w = (torch.randn(1, E, generator=g) * 0.3 + 1).cuda()
+    inv, dw = torch.empty(R, device="cuda"), torch.empty(1, E, device="cuda")
+    ws = torch.empty(hb.gated_residual_norm_bwd_workspace_bytes(1, R, E), dtype=torch.uint8, device="cuda")
+    hb.gated_residual_norm_fwd(1, R, E, 1, 1, x, None, None, None, None, None, w, None, EPS, None, y, None, None, None, inv)
+    hb.gated_residual_norm_bwd(1, R, E, 1, 1, x, None, None, None, None, None, w, None, None, None, inv, None, dy, dx, None, None, None, None, dw,
+                               None, None, ws)
+    h = lambda t: t[:, -n:].double().cpu()
+    p = [h(x), None, None, None, None, None, w.double().cpu(), None]
+    q = [None if t is None else t.clone().requires_grad_() for t in p]
+    (dr.gated_norm(True, *q, EPS)[1] * h(dy)).sum().backward()
+    bound = dr.gated_norm_bounds(True, *p, EPS, None, h(dy))
+    want = dr.gated_norm(True, *p, EPS)[1]
+    for got, v, b, t in ((h(y), want, bound["y"], "bf16"), (h(dx), q[0].grad, bound["dx"], "bf16"), (dw.double().cpu(), q[6].grad, bound["dw2"], "f32")):
+        assert float(((got - v).abs() - dr.stored(v, b, t)).max()) <= 0
+    assert not bool(y[0, :-n].any()) and not bool(dx[0, :-n].any())
