@@ -7,16 +7,18 @@ namespace {
 // Blocks of tiles: about LA_WANT of all heads together, which is two or three workgroups on each compute unit; half as many where a compute unit holds one
 // (128 columns of fp32 or with states: 80 KB of LDS, or registers for one) and in the backward call, whose three jobs run side by side (8 x 2048 rows, 4
 // heads of 64 bf16, both directions: 57 us with 512 for each job, 51 with 256, 62 with 170; 2 x 16384 rows, 8 heads of 128: 437, 412, 429).  With R their number only grows, so that the workspace for the most rows serves fewer.
+constexpr int LA_MOST = 0x1fffff;        // query heads and blocks: a launch has fewer than 2^32 threads, three jobs of up to 512 for each
 constexpr int LA_WANT = 512, LA_SCAN = 32 * 128 * 128, LA_FEW = 64 * 64, LA_SHORT = 512;
 int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
   if (B <= 0 || R <= 0 || nseq <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || Hq % Hkv || !valid_dtype(dtype) || R > 0x7fffffff - 4096) return HFTA_EINVAL;
-  // (a launch has fewer than 2^32 threads: three jobs of up to 512 threads for each query head and block)
-  const int64_t heads = (int64_t)B * Hkv > LA_WANT ? (int64_t)B * Hkv : LA_WANT;
-  return d > 128 || nseq > PACKED_MAX || B > 65535 || heads > 0x1fffff / (Hq / Hkv) ? HFTA_EUNSUPPORTED : HFTA_OK;
+  return d > 128 || nseq > PACKED_MAX || B > 65535 || (int64_t)B * Hq > LA_MOST ? HFTA_EUNSUPPORTED : HFTA_OK;
 }
 // Against the order a state is held divided by the scale, which is why that has to lie well inside the range of fp32
 bool la_scale(float scale) { return scale >= 0x1p-32f && scale <= 0x1p32f; }
-int64_t la_limit(int B, int Hkv, int want) { return (int64_t)B * Hkv < want ? want / ((int64_t)B * Hkv) : 1; }
+int64_t la_limit(int B, int Hq, int Hkv, int want) {
+  const int64_t blocks = (int64_t)B * Hkv < want ? want / ((int64_t)B * Hkv) : 1, most = LA_MOST / ((int64_t)B * Hq);
+  return blocks < most ? blocks : most;
+}
 void la_cut(LaArgs& a, int Hq, int dtype) {
   a.by_heads = PkDiv((uint32_t)(a.B * Hq));
   a.by_hq = PkDiv((uint32_t)Hq);
@@ -24,7 +26,7 @@ void la_cut(LaArgs& a, int Hq, int dtype) {
   a.by_hkv = PkDiv((uint32_t)a.Hkv);
   bool states = false;
   for (int j = 0; j < a.jobs; ++j) states = states || a.job[j].S0 || a.job[j].S1;
-  const int64_t most = la_limit(a.B, a.Hkv, a.jobs > 1 || (a.d > 64 && (dtype == HFTA_F32 || states)) ? LA_WANT / 2 : LA_WANT);
+  const int64_t most = la_limit(a.B, Hq, a.Hkv, a.jobs > 1 || (a.d > 64 && (dtype == HFTA_F32 || states)) ? LA_WANT / 2 : LA_WANT);
   a.tiles = (a.R + LA_T - 1) / LA_T;
   a.per = (int)((a.tiles + most - 1) / most);
   a.blocks = (a.tiles + a.per - 1) / a.per;
@@ -40,8 +42,8 @@ void la_cut(LaArgs& a, int Hq, int dtype) {
   const int64_t again = (int64_t)(a.R / a.nseq) * (a.jobs > 1 ? Hq / a.Hkv : 1);
   a.mode = a.blocks == 1 ? LA_ALONE : (int64_t)a.tiles * D <= LA_FEW && again <= rows ? LA_WALK : a.blocks * D * D > LA_SCAN ? LA_SCANNED : LA_SUMS;
 }
-size_t la_workspace(int B, int R, int Hkv, int d, int sums) {
-  const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hkv, LA_WANT), n = tiles < most ? tiles : most;
+size_t la_workspace(int B, int R, int Hq, int Hkv, int d, int sums) {
+  const int64_t tiles = (R + LA_T - 1) / LA_T, most = la_limit(B, Hq, Hkv, LA_WANT), n = tiles < most ? tiles : most;
   if (n == 1) return 0;
   const int64_t D = la_pad(d);
   return (size_t)(sums * n * B * Hkv * D * D * 4 + (sums * n * B * 4 + 15) / 16 * 16);
@@ -84,10 +86,10 @@ using namespace hfta;
 extern "C" {
 
 size_t hfta_linear_attention_fwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
-  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 1) : 0;
+  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hq, Hkv, d, 1) : 0;
 }
 size_t hfta_linear_attention_bwd_workspace_bytes(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
-  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hkv, d, 2) : 0;
+  return la_check(B, R, nseq, Hq, Hkv, d, dtype) == HFTA_OK ? la_workspace(B, R, Hq, Hkv, d, 2) : 0;
 }
 
 int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype, const void* Q, const int64_t qs[3], const void* K,
@@ -100,7 +102,7 @@ int hfta_linear_attention_fwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
   if (!la_scale(scale)) return HFTA_EUNSUPPORTED;
-  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 1))) return HFTA_EWORKSPACE;
+  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hq, Hkv, d, 1))) return HFTA_EWORKSPACE;
   LaArgs a{};
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = a.nsums = 1;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs);
@@ -122,7 +124,7 @@ int hfta_linear_attention_bwd(int B, int R, int nseq, int Hq, int Hkv, int d, in
     return HFTA_EINVAL;
   if (rc != HFTA_OK) return rc;
   if (!la_scale(scale)) return HFTA_EUNSUPPORTED;
-  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hkv, d, 2))) return HFTA_EWORKSPACE;
+  if (!la_ws_ok(workspace, ws_bytes, la_workspace(B, R, Hq, Hkv, d, 2))) return HFTA_EWORKSPACE;
   LaArgs a{};
   a.off = seq_offsets; a.ld = log_decay; a.B = B; a.R = R; a.nseq = nseq; a.Hkv = Hkv; a.d = d; a.jobs = 3; a.nsums = 2;
   const PkStr q = la_str(qs), kv = la_str(kvs), c = la_str(cs), dq = la_str(dqs), dkv = la_str(dkvs);

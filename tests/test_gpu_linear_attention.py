@@ -309,6 +309,51 @@ def test_gradients_and_states_that_are_not_finite(hb, dtype, d):
         assert not bool(torch.isfinite(c.ctx[0, 20:150, 0].float()).all(-1).any()) and not bool(torch.isfinite(c.dk[0, 20:150, 0].float()).all(-1).any()), bad
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_thousands_of_query_heads_on_one_key_head(hb, dtype):
+    for states in (False, True):
+        c = Case(dtype, 1, [[140, 9]], 4096, 1, 16, first=1, behind=2, seed=8, decay=-0.03, states=states)
+        c.fwd(hb)
+        c.bwd(hb)
+        torch.cuda.synchronize()
+        rows = slice(0, 4096, 4095 // 12)                         # some of the query heads; keys, values and states of all of them
+        part = object.__new__(Case)
+        part.__dict__.update(c.__dict__)
+        for m in ("q", "dctx", "ctx", "dq"):
+            setattr(part, m, getattr(c, m)[:, :, rows])
+        part.check(("ctx", "dq", "s1"))
+    h = lambda t: t.double().cpu()
+    # dk = sum over heads of lambda^(t - s) (v_s . dctx_t) q_t scale: the heads' sum is one product of matrices
+    lo, hi = c.off[0, 0].item(), c.off[0, 1].item()
+    t = torch.arange(hi - lo, dtype=torch.float64)
+    D = torch.exp(h(c.ld)[0, 0] * (t[:, None] - t).clamp(min=0)).tril()
+    q, dctx, k, v, dsf = (h(x) for x in (c.q[0, lo:hi], c.dctx[0, lo:hi], c.k[0, lo:hi, 0], c.v[0, lo:hi, 0], c.dsf[0, 0, 0]))
+    down = torch.exp(h(c.ld)[0, 0] * (t.numel() - 1 - t))[:, None]
+    base = (2 * 16 + (2 + 4096) * (hi - lo) + 40) * dr.U + (3 * 2.0 ** -16 if dtype == "bf16" else 0.0)
+    for got, a, b, x, st in ((c.dk, v, dctx, q, dsf.T), (c.dv, k, q, dctx, dsf)):
+        f = lambda a, b, x, st: sum(c.scale * (D.T * (a @ b[:, i].T)) @ x[:, i] for i in range(b.shape[1])) + down * (a @ st)
+        want, bound = f(a, b, x, st), base * f(a.abs(), b.abs(), x.abs(), st.abs())
+        assert float(((h(got[0, lo:hi, 0]) - want).abs() - dr.stored(want, bound, dtype)).max()) <= 0
+
+
+def test_as_many_heads_and_blocks_as_a_launch_takes(hb):
+    """Query heads that leave room for fewer blocks than there are tiles."""
+    H, d, lengths = 40000, 8, [[2000, 5, 1800]]
+    g = torch.Generator(device="cuda").manual_seed(2)
+    off = dr.offsets(lengths)
+    R = int(off.max())
+    q = torch.randn(1, R, H, d, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(1, R, 1, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    ctx, ld = torch.full_like(q, MARK), torch.full((1, 1), -0.01, device="cuda")
+    size = (1, R, 3, H, 1, d, 1)
+    ws = torch.empty(hb.linear_attention_fwd_workspace_bytes(*size), dtype=torch.uint8, device="cuda")
+    hb.linear_attention_fwd(*size, q, (R * H * d, H * d, d), k, v, (R * d, d, d), off.cuda(), ld, 0.3, None, ctx, (R * H * d, H * d, d), None, ws)
+    some = [0, 1, 777, 20000, H - 1]
+    args = (q[:, :, some].double().cpu(), k.double().cpu(), v.double().cpu(), off, ld.cpu(), 0.3)
+    want, bound = dr.linear_attention(*args)["ctx"], dr.linear_attention_bounds(*args, dtype="bf16")["ctx"]
+    assert float(((ctx[:, :, some].double().cpu() - want).abs() - dr.stored(want, bound, "bf16")).max()) <= 0
+
+
 def test_rows_outside_do_not_matter(hb):
     for dtype in ("f32", "bf16"):
         c = Case(dtype, 2, [[60, 0, 9], [3, 40, 1]], 2, 2, 32, first=7, behind=80, seed=4)
