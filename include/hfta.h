@@ -735,17 +735,18 @@ int hfta_preference_loss(int B, int R, int K, int npairs, int dtype, const void*
  *   state_in[b][s][h] (fp32 [B][nseq][Hkv][d][d]; NULL: zeros), behind it state_out[b][s][h] (NULL: not wanted; an empty sequence's
  *   state_in); state_out may not overlap state_in (EINVAL where it is state_in).  bwd: gradients of Q, K, V from the same state_in and, where state_out is used
  *   further, its gradient dstate_out (or NULL); dstate_in (or NULL) gets the gradient of state_in, and may not overlap dstate_out (EINVAL).
- *   log_decay is a hyper-parameter without a gradient.  Workspaces *_workspace_bytes, 16-byte aligned (EWORKSPACE); one for the most rows and sequences serves
- *   every smaller batch.  A value that is not finite reaches the rows that see it, as an infinity or a NaN, and no others.
- *   States and sums are fp32.
+ *   log_decay is a hyper-parameter without a gradient.  Workspaces *_workspace_bytes, 16-byte aligned (EWORKSPACE); one for the most rows and
+ *   sequences serves every smaller batch.  R / nseq tells the library whether sequences are short: places that stay empty cost time, not results.
+ *   A value that is not finite reaches the rows that see it, as an infinity or a NaN, and no others.  States and sums are fp32.
  * linear_attention_step: one token of each of n rows: Q, CTX [Hq], K, V [Hkv] heads at s[0] b + s[1] i + s[2] h + c, the state of row i in place
  *   slot[b][i] (int32 [B][n], device; NULL: place i) of state, fp32 [B][slots][Hkv][d][d], and the new one in the same place of new_state,
- *   which may be state itself.  A row whose slot lies outside [0, slots) takes no part: its CTX is left as it was, as are new
+ *   which may be state itself; scale: any finite number.  A row whose slot lies outside [0, slots) takes no part: its CTX is left as it was, as are new
  *   states that no row names.  Rows that name the same slot are tokens of one sequence, in order of i.
  * gated_residual_norm: u = N(F) w1 + b1;  S = X + res sigma(G) u;  Y = N(S) w2 + b2, N over the last dimension of [B][R][E] (contiguous),
  *   with or without the mean (`norm`), E <= 16384 (EUNSUPPORTED).  w1, b1, w2, b2: fp32 [B][E]; res: fp32 [B]; G: [B][R][E].  b1, b2, res, G may
  *   be NULL (0, 0, 1, a gate of 1).  F NULL: the norm in front of a first block alone, Y = N(X) w2 + b2; then G, w1, b1, res, S and
- *   what belongs to them below are NULL.  Y is made of S before S is rounded to the storage dtype.  mean1, inv1, mean2, inv2 (fp32
+ *   what belongs to them below are NULL (hfta_layernorm_* is that norm with means and biases, hfta_add_layernorm_fwd with a sum in front,
+ *   for rows of any width; this one also goes without either and adds dS to its gradient).  Y is made of S before S is rounded to the storage dtype.  mean1, inv1, mean2, inv2 (fp32
  *   [B][R]): what the backward call reads (RMS: means are not looked at).
  *   bwd: dS (or NULL): the gradient that reaches S on the residual path; dX: the whole gradient of S, which is X's; dF; dG (exactly where G
  *   is); dw1, dw2; db1 (exactly where b1 is), db2 (or NULL); dres [B] (or NULL).  dX may be dS itself.  Sums over rows are added in a fixed order.

@@ -192,7 +192,8 @@ __global__ __launch_bounds__(gn_threads(TPR), (TPR == 1024 ? 4 : BIAS || sizeof(
   constexpr int N = P::N, NT = gn_threads(TPR), RPB = NT / TPR;
   constexpr bool AHEAD = TPR < 1024;
   // Registers for 1 - h: without biases, and with the few of 1024 threads, u is formed again rather than held, past 8192 columns from biases loaded again,
-  // and with 1024 threads a gate is one register (2 x 2048 rows of 8192 bf16, both directions: 279 us, with two 303; 5 x 9633 rows of 200: 99 and 95)
+  // and with 1024 threads a gate is one register (2 x 2048 rows of 8192 bf16, both directions: 279 us, with two 303; 5 x 9633 rows of 200, means
+  // and biases: 99 and 95)
   constexpr bool AGAIN = TPR == 1024 || !BIAS, LOADS = BIAS && NP * N > 8;
   typedef std::conditional_t<TPR == 1024, GnOne, GnTwo> Gate;
   __shared__ GnSum<TPR> sum;

@@ -5,8 +5,9 @@ namespace hfta {
 namespace {
 
 // Blocks of tiles: about LA_WANT of all heads together, which is two or three workgroups on each compute unit; half as many where a compute unit holds one
-// (128 columns of fp32 or with states: 80 KB of LDS, or registers for one) and in the backward call, whose three jobs run side by side (8 x 2048 rows, 4
-// heads of 64 bf16, both directions: 57 us with 512 for each job, 51 with 256, 62 with 170; 2 x 16384 rows, 8 heads of 128: 437, 412, 429).  With R their number only grows, so that the workspace for the most rows serves fewer.
+// (128 columns of fp32, which take 143 KB of LDS, or of bf16 with states, whose registers leave room for one) and in the backward call, whose three jobs run
+// side by side (8 x 2048 rows, 4 heads of 64 bf16, both directions: 57 us with 512 for each job, 51 with 256, 62 with 170; 2 x 16384 rows, 8 heads of 128: 437,
+// 412, 429).  With R their number only grows, so that the workspace for the most rows serves fewer.
 constexpr int LA_MOST = 0x1fffff;        // query heads and blocks: a launch has fewer than 2^32 threads, three jobs of up to 512 for each
 constexpr int LA_WANT = 512, LA_SCAN = 32 * 128 * 128, LA_FEW = 64 * 64, LA_SHORT = 512;
 int la_check(int B, int R, int nseq, int Hq, int Hkv, int d, int dtype) {
@@ -34,7 +35,9 @@ void la_cut(LaArgs& a, int Hq, int dtype) {
   // directions: sequences of 200 rows 66 us with sums and 52 walked, of 400 63 and 59, of 800 75 and 80.  Backward each query head of a group is walked:
   // 3 x 930 rows, 12 heads of 80 over 3, backward alone walked or not: of 50 rows 62 and 66, of 100 69 and 68, of 200 85 and 76.  fp32 takes longer for a
   // tile, the more the wider (3 x 777, 3 heads of 48: of 100 rows 41 and 38, of 200 46 and 57).  One long sequence among short ones costs its tiles again in
-  // each of its blocks, so that this is left to few rows (three quarters of the rows in one: 66 and 80, of 8192 rows 105 and 200).
+  // each of its blocks, so that this is left to few rows (three quarters of the rows in one: 66 and 80, of 8192 rows 105 and 200).  Places of sequences that are empty count as
+  // short ones: 8 models of 4 heads of 32, 300 places and all rows in one of them, forward: 2048 rows bf16 25 us with sums and 37 walked, 8192 rows 60 and 128, fp32 94
+  // and 240; in 80 sequences of 100 instead 52 and 45, fp32 82 and 75.
   // Sums are added up by each block for itself while those before it are up to 2 MB (16384 rows of one sequence, both directions: 2 x 4 heads of 64, 64 blocks
   // forward: 136 us, with a launch that adds them along the sequences 158; 2 x 8 heads of 128, 32 blocks: 395 and 410; 2 x 4, 64 blocks: 296 and 249; 1 x 1,
   // 256 blocks: 1040 and 279).

@@ -6,8 +6,9 @@
 // angle is formed in 64 bits, in turns, and only the rest of less than half a turn goes on in fp32.
 //
 // Bound by memory: a lane forms the angles of a piece of 16 bytes once and turns that piece in all heads of its row.  The first four heads are on
-// their way while the angles are formed, and a head is fetched as one is stored: 2 x 40000 rows, 10 heads of 128 bf16, three axes: 90 us, 4.5 TB/s,
-// against 114 with loads four heads at a time.  Where few rows would leave compute units without work the heads are split over workgroups too.
+// their way while the angles are formed, and a head is fetched as one is stored: 2 x 40000 rows, 10 heads of 128 bf16, three axes: 90 to 96 us
+// from card to card, 4.3 to 4.5 TB/s, against 114 with loads four heads at a time.  Where few rows would leave compute units without work the heads are
+// split over workgroups too.
 #include "packed_rows.h"
 #include "pieces.h"
 
