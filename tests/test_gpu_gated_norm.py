@@ -114,20 +114,23 @@ def test_constant_rows_and_eps(hb):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rms", [False, True])
-def test_gates_far_open_and_far_closed(hb, dtype, rms):
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("R,E", [(40, 96), (9, 1500), (5, 5000), (3, 9001)])
+def test_gates_far_open_and_far_closed(hb, dtype, rms, bias, R, E):
     """The gate's gradient keeps its digits on both sides: sigma' = h (1 - h) is e^-|g| / (1 + e^-|g|)^2, even."""
-    c = Case(2, 40, 96, dtype, rms, seed=9)
+    c = Case(2, R, E, dtype, rms, seed=9, bias=bias)
     sides = torch.tensor([-60.0, -20, -17.5, -16, -12, -10, -8, -4, 4, 8, 10, 12, 16, 17.5, 20, 60], device="cuda")
-    c.gate.copy_(sides.repeat(12)[torch.randperm(192, generator=torch.Generator().manual_seed(1)).cuda()].repeat(40).view(2, 40, 96))
+    c.gate.copy_(sides[torch.randint(16, (2, R, E), generator=torch.Generator().manual_seed(1)).cuda()])
     c.fwd(hb)
     c.bwd(hb)
     c.check()
-    h = lambda t: t.double().cpu()
+    h = lambda t: None if t is None else t.double().cpu()
     names = ("x", "f", "gate", "w1", "b1", "res", "w2", "b2")
     p = [h(getattr(c, n)) for n in names]
     x, f, g, w1, b1, res, w2, b2 = p
+    b1 = torch.zeros_like(w1) if b1 is None else b1
     bound = dr.gated_norm_bounds(rms, *p, EPS, h(c.ds), h(c.dy))
-    q = [t.clone().requires_grad_() for t in p]
+    q = [None if t is None else t.clone().requires_grad_() for t in p]
     s, y = dr.gated_norm(rms, *q, EPS)
     ((y * h(c.dy)).sum() + (s * h(c.ds)).sum()).backward()
     e = torch.exp(-g.abs())
@@ -143,6 +146,22 @@ def test_gates_far_open_and_far_closed(hb, dtype, rms):
     b = slope * (bound["dx"] * u.abs() + dsm.abs() * eu + 16 * dr.U * (dsm * u).abs())
     bad = (h(c.dg) - want).abs() - dr.stored(want, b, dtype)
     assert float(bad.max()) <= 0, (float(bad.max()), c.gate.flatten()[int(bad.argmax())])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E", [96, 1500, 5000, 9001])
+def test_gates_without_end(hb, dtype, E):
+    """Gates of plus and minus infinity are those of 200: open or shut, with a slope of nothing."""
+    c, d = (Case(2, 5, E, dtype, False, seed=3) for _ in range(2))
+    sign = torch.where(torch.rand(2, 5, E, generator=torch.Generator().manual_seed(2)) < 0.5, -1.0, 1.0).cuda()
+    c.gate.copy_(sign * math.inf)
+    d.gate.copy_(sign * 200.0)
+    for x in (c, d):
+        x.fwd(hb)
+        x.bwd(hb)
+    for n in c.OUT:
+        assert torch.equal(getattr(c, n), getattr(d, n)) and bool(torch.isfinite(getattr(c, n)).all()), n
+    assert not bool(c.dg.any())
 
 
 def test_rows_that_are_not_finite(hb):
